@@ -215,6 +215,62 @@ RAZOR_API int razor_decode_attention_multi(razor_cache_t* cache, int32_t layer, 
                                  int32_t n_tokens, void* stream);
 
 /*
+ * Speculative decoding: a draft model (or a lookup in the prompt) proposes a TREE of tokens per sequence, the target
+ * model scores all of them in one pass, and one path of the tree is kept.  The paper is silent on it; the reading taken:
+ * nothing is evicted while drafts are being judged.
+ *   razor_decode_attention_tree   the attention of that pass, per layer.  The cache is read and left as it is.
+ *   razor_verify_tree             which path is kept, and the token after it.  Needs no cache.
+ *   razor_append_tree             the kept path's K and V appended, per layer: exactly what n_accept[b] razor_append
+ *                                 calls would leave in sequence b (Algorithm 1, Eq. 4).
+ * A tree: parent, device int32 [B, n_nodes].  parent[t] is the node that t follows, -1 when it follows the sequence
+ * itself; a parent precedes its node.  A node whose parent lies outside [-1, t), and every node under one, is absent
+ * (sequences with fewer drafts than the others).  1 <= n_nodes <= RAZOR_TREE_MAX_NODES.
+ * q, k_draft, v_draft: device, config.dtype, [B, n_nodes, Hq (Hkv), D] with element strides stride_b and stride_t (the
+ * column ranges of one fused projection will do); the heads of a node are contiguous; bases 16-byte aligned, strides
+ * multiples of 16 bytes, and at least a node's heads long.
+ *
+ * razor_decode_attention_tree: out device fp32 [B, n_nodes, Hq, D] contiguous, 16-byte aligned.  Node t attends to every
+ * kept token of its KV head, to the compensation token with its count (Eq. 5), and to itself and its ancestors.  An
+ * absent node's rows of out are left as they were.  With ALiBi (razor_cache_set_alibi) a node's position is the tokens
+ * seen so far plus its depth.  q, k_draft, v_draft, parent may be written by the kernel directly before this call; they,
+ * and out, must not change until it has run.  Captured in a CUDA graph, a replay attends to the cache as it then is.
+ *
+ * razor_append_tree: path device int32 [B, n_nodes]: node path[b][i] is the i-th token appended to sequence b, for
+ * i < n_accept[b] (razor_verify_tree's path); NULL: the nodes 0, 1, .. themselves.  Entries outside [0, n_nodes) read
+ * the nearest node.  n_accept host [B], 0 .. n_nodes (the host mirrors every length, so the counts are read back after
+ * verification, once for all layers).
+ *
+ * razor_verify_tree: target device [B, rows, vocab], dtype RAZOR_F32 or RAZOR_BF16, element strides target_stride_b and
+ * target_stride_row: row 0 holds the target's probabilities for the token after the sequence, row 1 + t those for the
+ * token after node t.  draft: the same layout (rows of nodes without children are never read), the distribution a
+ * node's children were drawn from, without replacement and in index order; NULL for drafts that were not drawn at
+ * random.  tokens device int32 [B, n_nodes]; u_accept device fp32 [B, n_nodes] and u_sample device fp32 [B], uniform in
+ * [0, 1).  From the root down, the children of the current node are tried in index order: child x is accepted when
+ *   u Q(x) < P(x),  P the target's row at first; after a rejection P becomes max(P - Q, 0), normalised, and Q loses the
+ * rejected child and is normalised (draft NULL: Q(x) = 1, and P just loses the child).  The walk goes on at an accepted
+ * child; where none is, the next token is the first one whose running sum of P exceeds u_sample times the whole sum (at
+ * a leaf that is the target's own row).  The tokens kept so are distributed as the target's own would be.  Rows are
+ * taken as they are (sums of one are not checked); entries that are negative or not finite count as zero; where nothing
+ * is left of P the target's own row is used.  A node with a token outside [0, vocab) is never accepted.
+ *   n_accepted device int32 [B]; path device int32 [B, n_nodes], -1 behind the accepted nodes; next_token device int32
+ *   [B], -1 when the row has no positive entry.  Sums are taken in 64 bits, in a fixed order.
+ * Errors: NULL_PTR, INVALID_ARG, UNSUPPORTED_DIM (dtype), MISALIGNED, NOT_COMPRESSED, CAPACITY (append beyond
+ * max_new_tokens in any sequence), CUDA.
+ */
+#define RAZOR_TREE_MAX_NODES 128
+RAZOR_API int razor_decode_attention_tree(razor_cache_t* cache, int32_t layer, const void* q, int64_t q_stride_b,
+                                int64_t q_stride_t, const void* k_draft, const void* v_draft, int64_t kv_stride_b,
+                                int64_t kv_stride_t, const int32_t* parent, int32_t n_nodes, float* out, void* stream);
+RAZOR_API int razor_append_tree(razor_cache_t* cache, int32_t layer, const void* k_draft, const void* v_draft,
+                                int64_t kv_stride_b, int64_t kv_stride_t, const int32_t* path, int32_t n_nodes,
+                                const int32_t* n_accept, void* stream);
+RAZOR_API int razor_verify_tree(const void* target, int64_t target_stride_b, int64_t target_stride_row, const void* draft,
+                                int64_t draft_stride_b, int64_t draft_stride_row, int32_t dtype, const int32_t* tokens,
+                                const int32_t* parent, const float* u_accept, const float* u_sample, int32_t batch,
+                                int32_t n_nodes, int32_t vocab, int32_t* n_accepted, int32_t* path, int32_t* next_token,
+                                void* stream);
+
+/*
  * Read back the compressed state of one (layer, sequence, KV head) in LOGICAL order (ascending
  * original position), whatever the physical slot order is.  Device outputs, any of which may be
  * NULL: kept_pos int32[n_kept]; K, V [n_kept, D] in config.dtype; comp_mean_k/v and comp_sum_k/v

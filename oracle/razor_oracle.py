@@ -322,3 +322,87 @@ def select_retrieval_heads(echo: Sequence[float], induction: Sequence[float], fr
     mask[np.argsort(-induction, kind="stable")[:k_i]] = 1
     mask[np.argsort(-echo, kind="stable")[:k_e]] = 1
     return mask
+
+
+# --------------------------------------------------------------------------- trees of drafted tokens
+def tree_lines(parent: Sequence[int]) -> List[Optional[List[int]]]:
+    """For every node of a tree of drafts the nodes from the root down to it, itself last; None for an absent node (its
+    parent is outside [-1, t), or absent itself).  parent[t] = -1: the node follows the sequence directly."""
+    lines: List[Optional[List[int]]] = []
+    for t, a in enumerate(parent):
+        if a == -1:
+            lines.append([t])
+        elif 0 <= a < t and lines[a] is not None:
+            lines.append(lines[a] + [t])
+        else:
+            lines.append(None)
+    return lines
+
+
+def tree_attention(qs: np.ndarray, hc: HeadCache, k_draft: np.ndarray, v_draft: np.ndarray, parent: Sequence[int],
+                   scale: float, use_compensation: bool = True, slope: float = 0.0) -> np.ndarray:
+    """Attention of the nodes of a tree of drafts; reading taken where the paper is silent: nothing is evicted while drafts
+    are judged, so node t attends to the cache as it stands (kept tokens, compensation token with its count: Eq. 5) and
+    to the drafts on its line.  With a slope, Eq. 1's penalty: node t stands at position (tokens seen) + depth.
+
+    qs, k_draft, v_draft: [T, D] of one query head and its KV head.  Rows of absent nodes are NaN."""
+    qs, k_draft, v_draft = (np.asarray(x, dtype=np.float64) for x in (qs, k_draft, v_draft))
+    seen = len(hc.kept_pos) + hc.n_drop
+    out = np.full(qs.shape, np.nan)
+    for t, line in enumerate(tree_lines(parent)):
+        if line is None:
+            continue
+        K, V = np.concatenate([np.asarray(hc.K, np.float64), k_draft[line]]), np.concatenate([np.asarray(hc.V, np.float64), v_draft[line]])
+        if slope:
+            pos = np.concatenate([hc.kept_pos, seen + np.arange(len(line))])
+            out[t] = alibi_attention(qs[t], K, V, pos, seen + len(line) - 1, slope, scale)
+        else:
+            out[t] = compensated_attention(qs[t], K, V, hc.k_hat, hc.v_hat, hc.n_drop if use_compensation else 0, scale)
+    return out
+
+
+def verify_tree(target: np.ndarray, draft: Optional[np.ndarray], tokens: Sequence[int], parent: Sequence[int],
+                u: Sequence[float], r: float) -> Tuple[List[int], int]:
+    """Which path of a tree of drafts is kept, and the token after it: rejection sampling against the target's own
+    distribution, child after child.  target [T + 1, V], draft the same or None; row 0 belongs to the sequence, row
+    1 + t to node t.  A rejected child leaves P <- norm(max(P - Q, 0)) and Q <- norm(Q without the child); without draft
+    probabilities Q is one at the child.  Returns (accepted nodes, next token); the token is -1 when the row is empty."""
+    def clean(x):
+        x = np.asarray(x, dtype=np.float64)
+        with np.errstate(invalid="ignore"):
+            return np.where((x > 0) & np.isfinite(x), x, 0.0)
+
+    V, at, path = target.shape[1], -1, []
+    while True:
+        own = clean(target[at + 1])
+        p, q = own.copy(), clean(draft[at + 1]) if draft is not None else None
+        mass, found = 1.0, None      # mass: what P adds up to before it is normalised
+        rest = 1.0                   # draft probability of the children still possible
+        for t in range(len(tokens)):
+            x = int(tokens[t])
+            if parent[t] != at or not -1 <= parent[t] < t or not 0 <= x < V:
+                continue
+            qx = 1.0 if q is None else q[x] / rest if rest > 0 else 0.0
+            accepted = float(u[t]) * qx * mass < p[x] if rest > 0 else False
+            if accepted:
+                found = t
+                break
+            if q is None:
+                mass = max(mass - p[x], 0.0)
+            else:
+                if rest > 0:
+                    p = np.maximum(p - q * (mass / rest), 0.0)
+                rest -= q[x]
+                q[x] = 0.0
+            p[x] = 0.0
+            if q is not None:
+                mass = p.sum()
+        if found is None:
+            break
+        path.append(found)
+        at = found
+    w = p if p.sum() > 0 else own
+    upto = np.cumsum(w)
+    over = np.nonzero((upto > float(r) * upto[-1]) & (w > 0))[0]
+    with_weight = np.nonzero(w > 0)[0]
+    return path, int(over[0]) if len(over) else int(with_weight[-1]) if len(with_weight) else -1

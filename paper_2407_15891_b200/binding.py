@@ -26,7 +26,8 @@ STATUS = {
 # every symbol include/razor.h declares
 SYMBOLS = [
     "razor_query_bytes", "razor_cache_create", "razor_compress", "razor_compress_seq", "razor_append",
-    "razor_decode_attention", "razor_decode_step", "razor_append_many", "razor_append_plan", "razor_decode_attention_multi", "razor_cache_export", "razor_cache_stats", "razor_schedule_plan",
+    "razor_decode_attention", "razor_decode_step", "razor_append_many", "razor_append_plan", "razor_decode_attention_multi",
+    "razor_decode_attention_tree", "razor_append_tree", "razor_verify_tree", "razor_cache_export", "razor_cache_stats", "razor_schedule_plan",
     "razor_schedule_query", "razor_schedule_combine_heads", "razor_cache_set_option", "razor_cache_device_status", "razor_cache_wait_selftest", "razor_cache_set_alibi", "razor_cache_set_head_windows",
     "razor_compensation_mean_static", "razor_head_scores_scratch_bytes", "razor_head_scores",
     "razor_select_retrieval_heads", "razor_cache_reset", "razor_cache_destroy", "razor_status_string",
@@ -76,6 +77,9 @@ def load() -> C.CDLL:
     lib.razor_append_many.argtypes = [vp, i32, vp, vp, i32, vp]
     lib.razor_append_plan.argtypes = [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp]
     lib.razor_decode_attention_multi.argtypes = [vp, i32, vp, vp, i32, vp]
+    lib.razor_decode_attention_tree.argtypes = [vp, i32, vp, i64, i64, vp, vp, i64, i64, vp, i32, vp, vp]
+    lib.razor_append_tree.argtypes = [vp, i32, vp, vp, i64, i64, vp, i32, vp, vp]
+    lib.razor_verify_tree.argtypes = [vp, i64, i64, vp, i64, i64, i32, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]
     lib.razor_cache_export.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp, C.POINTER(i32),
                                        C.POINTER(i32), vp]
     lib.razor_cache_stats.argtypes = [vp, i32, C.POINTER(sz), C.POINTER(sz)]
@@ -215,6 +219,49 @@ def razor_append_plan(len_: int, n_drop: int, ring_head: int, window: int, n_sin
 def razor_decode_attention_multi(cache: int, layer: int, q, out, n_tokens: int, stream=None) -> None:
     _check(load().razor_decode_attention_multi(cache, layer, _ptr(q), _ptr(out), n_tokens, _stream(stream)),
            "razor_decode_attention_multi")
+
+
+TREE_MAX_NODES = 128
+
+
+def razor_decode_attention_tree(cache: int, layer: int, q, q_stride_b: int, q_stride_t: int, k_draft, v_draft,
+                                kv_stride_b: int, kv_stride_t: int, parent, n_nodes: int, out, stream=None) -> None:
+    _check(load().razor_decode_attention_tree(cache, layer, _ptr(q), q_stride_b, q_stride_t, _ptr(k_draft),
+                                              _ptr(v_draft), kv_stride_b, kv_stride_t, _ptr(parent), n_nodes, _ptr(out),
+                                              _stream(stream)), "razor_decode_attention_tree")
+
+
+def razor_append_tree(cache: int, layer: int, k_draft, v_draft, kv_stride_b: int, kv_stride_t: int, path, n_nodes: int,
+                      n_accept, stream=None) -> None:
+    a = _i32(n_accept)
+    _check(load().razor_append_tree(cache, layer, _ptr(k_draft), _ptr(v_draft), kv_stride_b, kv_stride_t, _ptr(path),
+                                    n_nodes, a.ctypes.data, _stream(stream)), "razor_append_tree")
+
+
+def razor_verify_tree(target: torch.Tensor, draft: Optional[torch.Tensor], tokens: torch.Tensor, parent: torch.Tensor,
+                      u_accept: torch.Tensor, u_sample: torch.Tensor, stream=None):
+    """target, draft (or None): fp32 or bf16 device tensors [B, n_nodes + 1, vocab], innermost dimension contiguous;
+    tokens, parent int32 and u_accept fp32 [B, n_nodes], u_sample fp32 [B], contiguous.
+    -> dict(accepted int32 [B], path int32 [B, n_nodes] (-1 behind the accepted nodes), token int32 [B])."""
+    B, T = tokens.shape
+    V = target.shape[2]
+    dt = {torch.float32: RAZOR_F32, torch.bfloat16: RAZOR_BF16}[target.dtype]
+    assert target.shape[0] == B and target.shape[1] >= T + 1 and (V == 1 or target.stride(2) == 1)
+    # (the rows of a tree's leaves are not read: a chain's draft rows may be T of them)
+    assert draft is None or (draft.dtype == target.dtype and draft.shape[0] == B and draft.shape[1] >= T
+                             and draft.shape[2] == V and (V == 1 or draft.stride(2) == 1))
+    for x, shape, dtype in ((tokens, (B, T), torch.int32), (parent, (B, T), torch.int32),
+                            (u_accept, (B, T), torch.float32), (u_sample, (B,), torch.float32)):
+        assert x.shape == shape and x.dtype == dtype and x.is_contiguous()
+    assert all(x is None or x.device == target.device for x in (draft, tokens, parent, u_accept, u_sample))
+    res = torch.empty((B, T + 2), dtype=torch.int32, device=target.device)   # one allocation for the three results
+    flat = res.view(-1)
+    accepted, token, path = flat[:B], flat[B:2 * B], flat[2 * B:].view(B, T)
+    d_strides = (draft.stride(0), draft.stride(1)) if draft is not None else (0, 0)
+    _check(load().razor_verify_tree(_ptr(target), target.stride(0), target.stride(1), _ptr(draft), *d_strides, dt,
+                                    _ptr(tokens), _ptr(parent), _ptr(u_accept), _ptr(u_sample), B, T, V, _ptr(accepted),
+                                    _ptr(path), _ptr(token), _stream(stream)), "razor_verify_tree")
+    return dict(accepted=accepted, path=path, token=token)
 
 
 def razor_cache_export(cache: int, layer: int, b: int, kv_head: int, kept_pos=None, K=None, V=None, comp_mean_k=None,
@@ -416,6 +463,41 @@ class RazorCache:
             out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
         razor_decode_attention_multi(self.handle, layer, q, out, q.shape[1])
         return out
+
+    def decode_tree(self, layer: int, q: torch.Tensor, k_draft: torch.Tensor, v_draft: torch.Tensor,
+                    parent: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """q [B, T, Hq, D], k_draft, v_draft [B, T, Hkv, D] (strided over b and t), parent int32 [B, T] -> out fp32
+        [B, T, Hq, D].  Rows of absent nodes are left as they are (zeros when `out` is not given)."""
+        self._check_draft(k_draft, v_draft)
+        T = k_draft.shape[1]
+        shape = (self.cfg.batch, T, self.cfg.n_q_heads, self.cfg.head_dim)
+        assert q.shape == shape and q.dtype == self.tdtype and self._heads_contiguous(q)
+        assert parent.shape == (self.cfg.batch, T) and parent.dtype == torch.int32 and parent.is_contiguous()
+        if out is None:
+            out = torch.zeros(shape, dtype=torch.float32, device=q.device)
+        assert out.shape == shape and out.dtype == torch.float32 and out.is_contiguous()
+        razor_decode_attention_tree(self.handle, layer, q, q.stride(0), q.stride(1), k_draft, v_draft,
+                                    k_draft.stride(0), k_draft.stride(1), parent, T, out)
+        return out
+
+    def append_tree(self, layer: int, k_draft: torch.Tensor, v_draft: torch.Tensor, path: Optional[torch.Tensor],
+                    n_accept) -> None:
+        """Append the accepted path: rows path[b, :n_accept[b]] of k_draft, v_draft [B, T, Hkv, D].  path int32 [B, T]
+        (or None: the first rows), n_accept [B] on the host."""
+        self._check_draft(k_draft, v_draft)
+        T = k_draft.shape[1]
+        assert path is None or (path.shape == (self.cfg.batch, T) and path.dtype == torch.int32 and path.is_contiguous())
+        assert len(n_accept) == self.cfg.batch
+        razor_append_tree(self.handle, layer, k_draft, v_draft, k_draft.stride(0), k_draft.stride(1), path, T, n_accept)
+
+    @staticmethod
+    def _heads_contiguous(x: torch.Tensor) -> bool:
+        return (x.shape[3] == 1 or x.stride(3) == 1) and (x.shape[2] == 1 or x.stride(2) == x.shape[3])
+
+    def _check_draft(self, k: torch.Tensor, v: torch.Tensor) -> None:
+        assert k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and self._heads_contiguous(k)
+        assert k.shape[0] == self.cfg.batch and k.shape[2:] == (self.cfg.n_kv_heads, self.cfg.head_dim)
+        assert k.dtype == self.tdtype and v.dtype == self.tdtype
 
     def export(self, layer: int, b: int, kv_head: int):
         """-> dict(kept_pos, K, V, mean_k, mean_v, sum_k, sum_v, n_drop) in logical order (device tensors)."""

@@ -106,7 +106,8 @@ struct LayerHost {
   std::vector<uint8_t> seq_done;    // [B]
   std::vector<HeadState> hs;        // [B*Hkv] mirror of the device state
   std::vector<long long> region_start, region_count;   // pages owned by (layer, b)
-  int appended = 0;
+  std::vector<int32_t> appended;    // [B] tokens appended to a sequence since its compression
+  int appended_max() const { return appended.empty() ? 0 : *std::max_element(appended.begin(), appended.end()); }
   // decode schedule
   bool sched_valid = false;
   int n_items = 0, n_jobs = 0, n_spans = 0, n_multi = 0, chunk_pages = 0, growth_tokens = 0, sched_rows = 0;
@@ -300,6 +301,7 @@ int razor_cache_create(razor_cache_t** out, const razor_config_t* cfg, void* poo
     LayerHost& L = c->layers[l];
     L.retr.assign(cfg->n_kv_heads, 0);
     L.seq_done.assign(cfg->batch, 0);
+    L.appended.assign(cfg->batch, 0);
     L.hs.assign((size_t)dv.n_heads, HeadState{0, 0, 0, 0});
     L.region_start.assign(cfg->batch, 0);
     L.region_count.assign(cfg->batch, 0);
@@ -317,7 +319,7 @@ int razor_cache_reset(razor_cache_t* c) {
   for (LayerHost& L : c->layers) {
     L.any = false;
     L.n_done = 0;
-    L.appended = 0;
+    std::fill(L.appended.begin(), L.appended.end(), 0);
     L.sched_valid = false;
     std::fill(L.seq_done.begin(), L.seq_done.end(), 0);
     std::fill(L.region_count.begin(), L.region_count.end(), 0);
@@ -522,10 +524,10 @@ int compress_impl(razor_cache* c, int layer, const std::vector<SeqIn>& seqs, con
     }
     for (int g = 0; g < H; ++g) L.hs[(size_t)b * H + g] = new_hs[i * (size_t)H + g];
     if (!L.seq_done[b]) { L.seq_done[b] = 1; L.n_done += 1; }
+    L.appended[b] = 0;
   }
   L.retr = flags;
   L.any = true;
-  L.appended = 0;
   L.sched_valid = false;
   // With the layer complete, its decode schedule is planned and sent to the device here, behind the compression
   // kernels, rather than in front of the layer's first decode launch, where the copies would sit between two
@@ -637,7 +639,7 @@ int razor_append(razor_cache_t* c, int32_t layer, const void* k_new, const void*
   if (rc) return rc;
   if (((uintptr_t)k_new | (uintptr_t)v_new) & 15) return RAZOR_E_MISALIGNED;
   LayerHost& L = c->layers[layer];
-  if (L.appended >= c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
+  if (L.appended_max() >= c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
   const int early_reads = c->last_writer_layer != layer;
   RZ_CUDA(launch_append(c->dv, c->cfg.dtype, layer, k_new, v_new, early_reads, (cudaStream_t)stream));
   c->note_write(layer, razor_cache::kWriteOneToken);
@@ -653,7 +655,7 @@ int razor_append(razor_cache_t* c, int32_t layer, const void* k_new, const void*
       h.ring_head = (h.ring_head + 1 == h.window) ? 0 : h.ring_head + 1;
     }
   }
-  L.appended += 1;
+  for (int32_t& n : L.appended) n += 1;
   L.growth_tokens += 1;
   return RAZOR_OK;
 }
@@ -666,7 +668,7 @@ int razor_append_many(razor_cache_t* c, int32_t layer, const void* k_new, const 
   if (n_tokens < 1) return RAZOR_E_INVALID_ARG;
   if (((uintptr_t)k_new | (uintptr_t)v_new) & 15) return RAZOR_E_MISALIGNED;
   LayerHost& L = c->layers[layer];
-  if ((long long)L.appended + n_tokens > c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
+  if ((long long)L.appended_max() + n_tokens > c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
   // Long runs go to the kernel that is parallel over the tokens: about eight CTAs per SM in all, slices of
   // at least 32 tokens, no more slice sums than the scratch holds.
   int slices = 0;
@@ -691,8 +693,109 @@ int razor_append_many(razor_cache_t* c, int32_t layer, const void* k_new, const 
   c->note_write(layer, razor_cache::kWriteBulk);
   const int n_sink = c->cfg.n_sink;
   for (HeadState& h : L.hs) h = state_after_run(h, n_sink, n_tokens);   // host mirror of the kernels' state update
-  L.appended += n_tokens;
+  for (int32_t& n : L.appended) n += n_tokens;
   L.growth_tokens += n_tokens;
+  return RAZOR_OK;
+}
+
+// The draft buffers of a tree call: 16-byte aligned rows, and no two rows of a sequence or of different sequences in
+// the same place (`row` elements each).  A stride that separates nothing is not looked at.
+static int check_draft_strides(int64_t stride_b, int64_t stride_t, int64_t row, int batch, int n_nodes, size_t es) {
+  if (n_nodes > 1) {
+    if ((stride_t * (int64_t)es) & 15) return RAZOR_E_MISALIGNED;
+    if (stride_t < row || stride_t > (1LL << 36)) return RAZOR_E_INVALID_ARG;
+  }
+  if (batch > 1) {
+    if ((stride_b * (int64_t)es) & 15) return RAZOR_E_MISALIGNED;
+    if (stride_b < row || stride_b > (1LL << 36)) return RAZOR_E_INVALID_ARG;
+  }
+  return RAZOR_OK;
+}
+
+int razor_append_tree(razor_cache_t* c, int32_t layer, const void* k_draft, const void* v_draft, int64_t kv_stride_b,
+                      int64_t kv_stride_t, const int32_t* path, int32_t n_nodes, const int32_t* n_accept, void* stream) {
+  if (!c || !k_draft || !v_draft || !n_accept) return RAZOR_E_NULL_PTR;
+  int rc = layer_ready(c, layer);
+  if (rc) return rc;
+  if (n_nodes < 1 || n_nodes > kTreeMaxNodes) return RAZOR_E_INVALID_ARG;
+  if (((uintptr_t)k_draft | (uintptr_t)v_draft) & 15) return RAZOR_E_MISALIGNED;
+  if ((uintptr_t)path & 3) return RAZOR_E_MISALIGNED;
+  const razor_config_t& cfg = c->cfg;
+  rc = check_draft_strides(kv_stride_b, kv_stride_t, (int64_t)cfg.n_kv_heads * cfg.head_dim, cfg.batch, n_nodes, esz(cfg));
+  if (rc) return rc;
+  LayerHost& L = c->layers[layer];
+  int most = 0;
+  for (int b = 0; b < cfg.batch; ++b) {
+    if (n_accept[b] < 0 || n_accept[b] > n_nodes) return RAZOR_E_INVALID_ARG;
+    if ((long long)L.appended[b] + n_accept[b] > cfg.max_new_tokens) return RAZOR_E_CAPACITY;
+    most = std::max(most, n_accept[b]);
+  }
+  if (most == 0) return RAZOR_OK;
+  RZ_CUDA(launch_append_tree(c->dv, cfg.dtype, layer, k_draft, v_draft, kv_stride_b, kv_stride_t, path, n_nodes, n_accept,
+                             cfg.batch, (cudaStream_t)stream));
+  c->note_write(layer, razor_cache::kWriteBulk);
+  for (int b = 0; b < cfg.batch; ++b) {   // host mirror of the kernel's state update
+    if (n_accept[b] == 0) continue;
+    for (int g = 0; g < cfg.n_kv_heads; ++g) {
+      HeadState& h = L.hs[(size_t)b * cfg.n_kv_heads + g];
+      h = state_after_run(h, cfg.n_sink, n_accept[b]);
+    }
+    L.appended[b] += n_accept[b];
+  }
+  L.growth_tokens += most;
+  return RAZOR_OK;
+}
+
+int razor_decode_attention_tree(razor_cache_t* c, int32_t layer, const void* q, int64_t q_stride_b, int64_t q_stride_t,
+                                const void* k_draft, const void* v_draft, int64_t kv_stride_b, int64_t kv_stride_t,
+                                const int32_t* parent, int32_t n_nodes, float* out, void* stream) {
+  if (!c || !q || !k_draft || !v_draft || !parent || !out) return RAZOR_E_NULL_PTR;
+  int rc = layer_ready(c, layer);
+  if (rc) return rc;
+  if (n_nodes < 1 || n_nodes > kTreeMaxNodes) return RAZOR_E_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)k_draft | (uintptr_t)v_draft | (uintptr_t)out) & 15) return RAZOR_E_MISALIGNED;
+  if ((uintptr_t)parent & 3) return RAZOR_E_MISALIGNED;
+  const razor_config_t& cfg = c->cfg;
+  rc = check_draft_strides(q_stride_b, q_stride_t, (int64_t)cfg.n_q_heads * cfg.head_dim, cfg.batch, n_nodes, esz(cfg));
+  if (!rc) rc = check_draft_strides(kv_stride_b, kv_stride_t, (int64_t)cfg.n_kv_heads * cfg.head_dim, cfg.batch, n_nodes, esz(cfg));
+  if (rc) return rc;
+  int longest = 0;
+  for (const HeadState& h : c->layers[layer].hs) longest = std::max(longest, h.len);
+  TreeCall tc = {};
+  tc.q = q; tc.k = k_draft; tc.v = v_draft; tc.parent = parent; tc.out = out;
+  tc.q_stride_b = q_stride_b; tc.q_stride_t = q_stride_t; tc.kv_stride_b = kv_stride_b; tc.kv_stride_t = kv_stride_t;
+  tc.n_nodes = n_nodes;
+  RZ_CUDA(launch_tree(c->dv, cfg.dtype, layer, tc, longest, (long long)c->lay.max_items * kMaxGroup, c->n_sms,
+                      (cudaStream_t)stream));
+  c->last_writer_layer = -1;
+  c->writes_since_decode.clear();   // an ordinary launch: everything before it has completed when it starts
+  c->writes_overflow = false;
+  return RAZOR_OK;
+}
+
+int razor_verify_tree(const void* target, int64_t target_stride_b, int64_t target_stride_row, const void* draft,
+                      int64_t draft_stride_b, int64_t draft_stride_row, int32_t dtype, const int32_t* tokens,
+                      const int32_t* parent, const float* u_accept, const float* u_sample, int32_t batch, int32_t n_nodes,
+                      int32_t vocab, int32_t* n_accepted, int32_t* path, int32_t* next_token, void* stream) {
+  if (!target || !tokens || !parent || !u_accept || !u_sample || !n_accepted || !path || !next_token)
+    return RAZOR_E_NULL_PTR;
+  if (dtype != RAZOR_F32 && dtype != RAZOR_BF16) return RAZOR_E_UNSUPPORTED_DIM;
+  if (batch < 1 || batch > (1 << 20) || n_nodes < 1 || n_nodes > kTreeMaxNodes || vocab < 1 || vocab > (1 << 30))
+    return RAZOR_E_INVALID_ARG;
+  if (target_stride_row < vocab || target_stride_b < 0) return RAZOR_E_INVALID_ARG;
+  if (draft && (draft_stride_row < vocab || draft_stride_b < 0)) return RAZOR_E_INVALID_ARG;
+  const uintptr_t es = dtype == RAZOR_BF16 ? 2 : 4;
+  if (((uintptr_t)target | (uintptr_t)draft) & (es - 1)) return RAZOR_E_MISALIGNED;
+  if (((uintptr_t)tokens | (uintptr_t)parent | (uintptr_t)u_accept | (uintptr_t)u_sample | (uintptr_t)n_accepted |
+       (uintptr_t)path | (uintptr_t)next_token) & 3)
+    return RAZOR_E_MISALIGNED;
+  VerifyCall vc = {};
+  vc.target = target; vc.draft = draft; vc.tokens = tokens; vc.parent = parent; vc.u_accept = u_accept;
+  vc.u_sample = u_sample; vc.n_accepted = n_accepted; vc.path = path; vc.next_token = next_token;
+  vc.target_stride_b = target_stride_b; vc.target_stride_row = target_stride_row;
+  vc.draft_stride_b = draft_stride_b; vc.draft_stride_row = draft_stride_row;
+  vc.batch = batch; vc.n_nodes = n_nodes; vc.vocab = vocab;
+  RZ_CUDA(launch_verify(vc, dtype, (cudaStream_t)stream));
   return RAZOR_OK;
 }
 
@@ -929,7 +1032,7 @@ int razor_decode_step(razor_cache_t* c, int32_t layer, const void* k_new, const 
   if (rc) return rc;
   if (((uintptr_t)k_new | (uintptr_t)v_new) & 15) return RAZOR_E_MISALIGNED;
   LayerHost& L = c->layers[layer];
-  if (L.appended >= c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
+  if (L.appended_max() >= c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
   // A head with no recent window at all drops the new token at once (nothing is stored, only the sums change):
   // that corner stays with the two separate kernels.
   bool plain = false;
@@ -950,12 +1053,12 @@ int razor_decode_step(razor_cache_t* c, int32_t layer, const void* k_new, const 
       h.ring_head = (h.ring_head + 1 == h.window) ? 0 : h.ring_head + 1;
     }
   }
-  L.appended += 1;
+  for (int32_t& n : L.appended) n += 1;
   L.growth_tokens += 1;
   rc = decode_impl(c, layer, q, out, 1, 1, 0, stream, k_new, v_new);
   if (rc) {
     L.hs = before;
-    L.appended -= 1;
+    for (int32_t& n : L.appended) n -= 1;
     L.growth_tokens -= 1;
     L.sched_valid = false;
     return rc;

@@ -512,6 +512,87 @@ __global__ void append_chunk_finalize_kernel(DeviceView dv, int layer, int n_tok
 }
 
 // ---------------------------------------------------------------------------------------------
+// Append of the accepted path of a tree of drafts: n_b tokens of sequence b, picked out of the drafts' K and V by
+// path[b][0 .. n_b), each sequence its own number.  The state afterwards is what n_b single appends would leave
+// (append_fate decides per token, as in append_chunk_kernel; the folded rows are summed thread group by thread group in
+// a fixed order).  The runs are short - a handful of rows of 256 bytes per head - so the kernel is a chain of
+// latencies (state, path, rows, sums); one CTA per head, the loads of a group's rows independent of one another.
+constexpr int kAppendTreeChunk = 1024;   // sequences of a launch: their counts travel as a kernel argument
+struct AppendCounts {
+  uint8_t n[kAppendTreeChunk];
+};
+template <typename T, int D>
+__global__ void __launch_bounds__(128) append_tree_kernel(DeviceView dv, int layer, const T* __restrict__ k,
+                                                          const T* __restrict__ v, int64_t stride_b, int64_t stride_t,
+                                                          const int32_t* __restrict__ path, int n_nodes, int b0,
+                                                          const __grid_constant__ AppendCounts counts) {
+  using Geo = RowGeom<T, D>;
+  constexpr int LPR = Geo::kLpr, EPL = Geo::kEpl, NGRP = 128 / LPR;
+  __shared__ float red[NGRP][2][D];
+  const int n_tok = counts.n[blockIdx.y];
+  cudaGridDependencySynchronize();
+  cudaTriggerProgrammaticLaunchCompletion();
+  if (n_tok == 0) return;
+  const int b = b0 + blockIdx.y, g = blockIdx.x, head = b * dv.n_kv_heads + g;
+  const size_t hs = (size_t)layer * dv.n_heads + head;
+  const HeadState st = dv.state[hs];
+  const int32_t* pt = dv.page_table + hs * dv.max_pages;
+  const int lir = threadIdx.x % LPR, grp = threadIdx.x / LPR;
+  float accK[EPL], accV[EPL];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) accK[i] = accV[i] = 0.f;
+  for (int a = grp; a < n_tok; a += NGRP) {
+    // (an index that is no node of the tree reads the nearest node: never outside the buffers)
+    const int src = path ? min(max(path[(size_t)b * n_nodes + a], 0), n_nodes - 1) : a;
+    const size_t off = (size_t)b * stride_b + (size_t)src * stride_t + (size_t)g * D;
+    const uint4 kf = ((const uint4*)(k + off))[lir], vf = ((const uint4*)(v + off))[lir];
+    const AppendFate fate = append_fate(st, dv.n_sink, n_tok, a);
+    uint4 fk = kf, fv = vf;
+    bool fold = fate.slot < 0;
+    if (fate.slot >= 0) {
+      uint4* dst = (uint4*)(dv.pool + (size_t)pt[fate.slot >> 4] * dv.page_bytes + (size_t)(fate.slot & 15) * Geo::kRowBytes) + swz(fate.slot, lir);
+      if (fate.evicts_old) {
+        fold = true;
+        fk = dst[0];
+        fv = dst[kPageTokens * LPR];
+      }
+      dst[0] = kf;
+      dst[kPageTokens * LPR] = vf;
+    }
+    if (fold) {
+      float x[EPL], y[EPL];
+      Elem<T>::unpack(fk, x);
+      Elem<T>::unpack(fv, y);
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) { accK[i] += x[i]; accV[i] += y[i]; }
+    }
+  }
+  const int n_evict = n_tok - append_run_fits(st, dv.n_sink, n_tok);
+  if (n_evict > 0) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      red[grp][0][lir * EPL + i] = accK[i];
+      red[grp][1][lir * EPL + i] = accV[i];
+    }
+  }
+  __syncthreads();   // (also: every thread has read the old state)
+  if (n_evict > 0) {
+    const float cnt = (float)(st.n_drop + n_evict);
+    for (int e = threadIdx.x; e < 2 * D; e += 128) {
+      float s = dv.comp_sum[hs * 2 * D + e];
+#pragma unroll
+      for (int r = 0; r < NGRP; ++r) s += (&red[r][0][0])[e];
+      dv.comp_sum[hs * 2 * D + e] = s;
+      dv.comp_mean[hs * 2 * D + e] = __fdiv_rn(s, cnt);
+    }
+  }
+  if (threadIdx.x == 0) {
+    dv.state[hs] = state_after_run(st, dv.n_sink, n_tok);
+    dv.ring_valid[hs] = 0;   // the window's content changed and its sum was not kept up
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
 // Export in logical order (ascending original position).  With T = len + n_drop tokens seen so far:
 // logical index i < N0 (or any i while nothing has been dropped) is position i in slot i; otherwise
 // j = i - N0 is the j-th oldest recent token: slot N0 + (ring_head + j) mod W, position T - W + j.
@@ -555,9 +636,9 @@ __global__ void __launch_bounds__(256) export_kernel(DeviceView dv, int layer, i
 // kernel touches at most memory that the library itself wrote whole kernels earlier; the caller's buffers
 // are read, and everything is written, only after that wait.
 template <typename... KArgs, typename... Args>
-static cudaError_t launch_dependent(void (*kernel)(KArgs...), int grid, int block, cudaStream_t s, Args... args) {
+static cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, int block, cudaStream_t s, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(block);
   cfg.dynamicSmemBytes = 0;
   cfg.stream = s;
@@ -639,6 +720,31 @@ cudaError_t launch_append_many(const DeviceView& dv, int dtype, int layer, const
   }
   return dv.head_dim == 128 ? append_many_t<float, 128>(dv, layer, k, v, n_tok, n_slices, s)
                             : append_many_t<float, 64>(dv, layer, k, v, n_tok, n_slices, s);
+}
+
+template <typename T, int D>
+static cudaError_t append_tree_t(const DeviceView& dv, int layer, const void* k, const void* v, int64_t stride_b,
+                                 int64_t stride_t, const int32_t* path, int n_nodes, const int32_t* n_accept, int batch,
+                                 cudaStream_t s) {
+  for (int b0 = 0; b0 < batch; b0 += kAppendTreeChunk) {
+    AppendCounts counts;
+    const int n = std::min(batch - b0, kAppendTreeChunk);
+    for (int i = 0; i < n; ++i) counts.n[i] = (uint8_t)n_accept[b0 + i];
+    const cudaError_t e = launch_dependent(append_tree_kernel<T, D>, dim3(dv.n_kv_heads, n), 128, s, dv, layer,
+                                           (const T*)k, (const T*)v, stride_b, stride_t, path, n_nodes, b0, counts);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_append_tree(const DeviceView& dv, int dtype, int layer, const void* k, const void* v, int64_t stride_b,
+                               int64_t stride_t, const int32_t* path, int n_nodes, const int32_t* n_accept, int batch,
+                               cudaStream_t s) {
+  if (dtype == RAZOR_BF16)
+    return dv.head_dim == 128 ? append_tree_t<__nv_bfloat16, 128>(dv, layer, k, v, stride_b, stride_t, path, n_nodes, n_accept, batch, s)
+                              : append_tree_t<__nv_bfloat16, 64>(dv, layer, k, v, stride_b, stride_t, path, n_nodes, n_accept, batch, s);
+  return dv.head_dim == 128 ? append_tree_t<float, 128>(dv, layer, k, v, stride_b, stride_t, path, n_nodes, n_accept, batch, s)
+                            : append_tree_t<float, 64>(dv, layer, k, v, stride_b, stride_t, path, n_nodes, n_accept, batch, s);
 }
 
 template <typename T, int D>

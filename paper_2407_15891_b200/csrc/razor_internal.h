@@ -253,6 +253,42 @@ struct RoundJobs {
 };
 cudaError_t launch_round(const DeviceView& dv, long long pool_pages, int layer, const RoundJobs& jb, const void* q,
                          float* out, int n_sms, cudaStream_t stream);
+// ---- speculative decoding (razor_tree.cu, razor_verify.cu, append_tree_kernel in razor_cache_kernels.cu)
+constexpr int kTreeMaxNodes = RAZOR_TREE_MAX_NODES;
+// One razor_decode_attention_tree call.  Strides in elements, between sequences (b) and between nodes (t).
+struct TreeCall {
+  const void* q;
+  const void* k;
+  const void* v;
+  const int32_t* parent;   // device [B, n_nodes]
+  float* out;
+  int64_t q_stride_b, q_stride_t, kv_stride_b, kv_stride_t;
+  int32_t n_nodes;
+  int32_t n_splits;        // parts of a head's tokens, chosen by the launcher
+  int32_t rec_rows;        // rows of a partial record
+};
+// longest: tokens of the longest head (sizes the parts); rec_rows: rows the record area of the workspace has.
+cudaError_t launch_tree(const DeviceView& dv, int dtype, int layer, const TreeCall& call, int longest, long long rec_rows,
+                        int n_sms, cudaStream_t stream);
+// Appends n_accept[b] (host, [B]) rows of k, v to every sequence, picked by path (device [B, n_nodes] or NULL).
+cudaError_t launch_append_tree(const DeviceView& dv, int dtype, int layer, const void* k, const void* v, int64_t kv_stride_b,
+                               int64_t kv_stride_t, const int32_t* path, int n_nodes, const int32_t* n_accept, int batch,
+                               cudaStream_t stream);
+struct VerifyCall {
+  const void* target;
+  const void* draft;       // NULL: the drafts were not drawn at random
+  const int32_t* tokens;
+  const int32_t* parent;
+  const float* u_accept;
+  const float* u_sample;
+  int32_t* n_accepted;
+  int32_t* path;
+  int32_t* next_token;
+  int64_t target_stride_b, target_stride_row, draft_stride_b, draft_stride_row;   // elements
+  int32_t batch, n_nodes, vocab;
+  int32_t seg_len;         // set by the launcher
+};
+cudaError_t launch_verify(const VerifyCall& call, int dtype, cudaStream_t stream);
 cudaError_t launch_wait_selftest(const DeviceView& dv, unsigned long long limit_ns, cudaStream_t stream);
 cudaError_t launch_export(const DeviceView& dv, int dtype, int layer, int head, int32_t* kept_pos, void* K, void* V,
                           float* mean_k, float* mean_v, float* sum_k, float* sum_v, cudaStream_t stream);

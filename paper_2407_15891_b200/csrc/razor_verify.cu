@@ -1,0 +1,301 @@
+// Verification of drafted tokens against the target's probabilities (the accept / reject walk of speculative
+// decoding, for a tree of drafts).
+//
+// At a node with target row p and draft row q its children are tried in index order.  With W = p, S = 1, Z = 1, A = 0
+// at the first child, child x is accepted when u q(x) S < W(x) Z - that is u < P(x) / Q(x) for the residual target
+// P = W / S and the draft distribution Q = q / Z without the children rejected so far.  A rejected child moves both
+// on: A += S / Z, Z -= q(x), and, because a maximum of maxima subtracting a growing multiple of q collapses into one,
+//     W(y) = max(p(y) - A q(y), 0), zero at the rejected children;   S = sum_y W(y).
+// Without draft probabilities (drafts that were looked up, not drawn) q is one at the child: W = p without the
+// rejected children and S = 1 - their probabilities, no pass over the row needed.  Where the walk ends, the next token
+// is the first y whose running sum of W exceeds r sum(W).
+//
+// What bounds it: one read of the last node's rows (one more out of L2 for every further rejected child there), and a
+// chain of dependent steps.  So a sequence is a cluster of CTAs that share the row: each takes a contiguous run of
+// segments, keeps the segment sums in shared memory, and the CTAs trade one partial sum per pass through distributed
+// shared memory.  The walk itself runs in every CTA of the cluster on values fetched up front (one p and one q value
+// per node), with the same arithmetic on the same operands, so all of them take the same decisions without talking.
+// The token is found by the CTA whose run the threshold falls into: it scans its segment sums and reads one segment
+// again.  Everything is summed in 64 bits: a running sum in 32 would move the border between two tokens by more than
+// a rare token's whole probability.
+#include <cooperative_groups.h>
+#include <math_constants.h>
+
+#include <algorithm>
+
+#include "razor_common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace razor {
+namespace {
+
+constexpr int kVerifyThreads = 512;
+constexpr int kVerifyWarps = kVerifyThreads / 32;
+constexpr int kVerifyCluster = 8;       // CTAs that share a sequence (the portable cluster size)
+constexpr int kMaxSegs = 1024;          // segments of a CTA's share of a row
+constexpr int kUnroll = 8;              // values of a row in flight per lane
+constexpr int kSegUnit = 32 * kUnroll;  // a segment is a multiple of this
+
+__device__ __forceinline__ float raw_prob(const float* x) { return __ldg(x); }
+__device__ __forceinline__ float raw_prob(const __nv_bfloat16* x) {
+  return __uint_as_float((uint32_t)__ldg((const unsigned short*)x) << 16);
+}
+// What is not a positive finite number counts as zero.
+__device__ __forceinline__ double prob(float x) { return x > 0.f && x < CUDART_INF_F ? (double)x : 0.0; }
+
+struct VerifySmem {
+  double seg_sum[kMaxSegs];
+  double warp_sum[kVerifyWarps];
+  double part[2][kVerifyCluster];   // sum of every CTA's share, written by its owner; passes take turns
+  float p_child[kTreeMaxNodes], q_child[kTreeMaxNodes], u[kTreeMaxNodes];
+  int32_t parent[kTreeMaxNodes], token[kTreeMaxNodes];
+  int32_t gone[kTreeMaxNodes];      // rejected children of the current node
+  int32_t path[kTreeMaxNodes];
+  int32_t n_gone, row;              // row: the current node + 1
+  int32_t draw;                     // 1: the walk has ended and the segment sums are those of its last W
+  double minus;                     // A
+};
+
+// W at position i of the current row.
+template <typename T>
+__device__ __forceinline__ double weight_at(const VerifySmem& sm, const T* p_row, const T* q_row, double a, int i) {
+  double w = prob(raw_prob(p_row + i));
+  if (q_row) w = fmax(w - a * prob(raw_prob(q_row + i)), 0.0);
+  for (int j = 0; j < sm.n_gone; ++j)
+    if (sm.gone[j] == i) w = 0.0;
+  return w;
+}
+
+// Sum of x over the lanes at or below this one.
+__device__ __forceinline__ double running_sum(double x, int lane) {
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const double y = __shfl_up_sync(0xffffffffu, x, off);
+    if (lane >= off) x += y;
+  }
+  return x;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyCall vc) {
+  __shared__ VerifySmem sm;
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank(), n_ranks = (int)cluster.num_blocks();
+  const int b = blockIdx.x / n_ranks;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int n_nodes = vc.n_nodes, V = vc.vocab;
+  const T* target = (const T*)vc.target + (size_t)b * vc.target_stride_b;
+  const T* draft = vc.draft ? (const T*)vc.draft + (size_t)b * vc.draft_stride_b : nullptr;
+
+  // ---- the values the walk compares, all at once
+  for (int t = tid; t < n_nodes; t += kVerifyThreads) {
+    const int a = vc.parent[(size_t)b * n_nodes + t], x = vc.tokens[(size_t)b * n_nodes + t];
+    const bool ok = a >= -1 && a < t && x >= 0 && x < V;   // otherwise it is nobody's child
+    sm.parent[t] = ok ? a : -2;
+    sm.token[t] = x;
+    sm.u[t] = vc.u_accept[(size_t)b * n_nodes + t];
+    sm.p_child[t] = ok ? raw_prob(target + (size_t)(a + 1) * vc.target_stride_row + x) : 0.f;
+    sm.q_child[t] = ok && draft ? raw_prob(draft + (size_t)(a + 1) * vc.draft_stride_row + x) : 1.f;
+  }
+  // this CTA's share of a row: n_segs segments of seg_len values from segment seg0 on
+  const int seg_len = vc.seg_len, all_segs = (V + seg_len - 1) / seg_len;
+  const int per = (all_segs + n_ranks - 1) / n_ranks;
+  const int seg0 = min(all_segs, rank * per), n_segs = min(all_segs, seg0 + per) - seg0;
+  cluster.sync();   // the values are there, and every CTA of the cluster runs (its shared memory may be written)
+
+  // ---- walk and passes.  The walk's state lives in warp 0, the same in every lane and in every CTA.
+  int cur = -1, last = -1, taken = 0, n_gone = 0;
+  double minus = 0.0, left = 1.0, total = 1.0;
+  bool fresh = false, whole = false;   // the segment sums belong to the current W; the residual was empty
+  unsigned pass = 0;
+  for (;; ++pass) {
+    if (warp == 0) {
+      bool draw = false;
+      double sum = 0.0;   // of the last pass
+      if (pass > 0)
+        for (int r = 0; r < n_ranks; ++r) sum += sm.part[(pass - 1) & 1][r];
+      if (fresh && draft && !whole) total = sum;
+      for (;;) {
+        int t = -1;       // the next child of `cur` behind `last`
+        for (int base = 0; base < n_nodes && t < 0; base += 32) {
+          const int i = base + lane;
+          const unsigned hit = __ballot_sync(0xffffffffu, i < n_nodes && i > last && sm.parent[i] == cur);
+          if (hit) t = base + __ffs(hit) - 1;
+        }
+        if (t < 0) {
+          draw = fresh;
+          if (fresh && !(sum > 0.0) && !whole) {   // nothing left (p nowhere above A q): the target's own row
+            whole = true;
+            draw = false;
+            n_gone = 0;
+            minus = 0.0;
+          }
+          fresh = true;   // (after the pass that follows)
+          break;
+        }
+        last = t;
+        const int x = sm.token[t];
+        bool was = false;
+        for (int i = lane; i < n_gone; i += 32) was |= sm.gone[i] == x;
+        was = __any_sync(0xffffffffu, was);
+        const double px = prob(sm.p_child[t]);
+        const double qx = !draft ? 1.0 : was ? 0.0 : prob(sm.q_child[t]);
+        const double w = was ? 0.0 : draft ? fmax(px - minus * qx, 0.0) : px;
+        if ((double)sm.u[t] * qx * total < w * left) {   // accepted: its children are next
+          if (lane == 0) sm.path[taken] = t;
+          taken += 1;
+          cur = t;
+          n_gone = 0;
+          minus = 0.0;
+          left = total = 1.0;
+          fresh = false;
+          continue;
+        }
+        if (!was) {
+          if (lane == 0) sm.gone[n_gone] = x;
+          n_gone += 1;
+          __syncwarp();
+        }
+        if (draft) {
+          minus += left > 0.0 ? total / left : 0.0;
+          left -= qx;
+          fresh = true;   // after the pass for its S
+          break;
+        }
+        total = fmax(total - w, 0.0);
+        fresh = false;
+      }
+      if (lane == 0) {
+        sm.draw = draw;
+        sm.row = cur + 1;
+        sm.minus = minus;
+        sm.n_gone = n_gone;
+      }
+    }
+    __syncthreads();
+    if (sm.draw) break;
+    // ---- one pass over this CTA's share of the row: segment sums of W
+    const double a = sm.minus;
+    const int gone = sm.n_gone;
+    const T* p_row = target + (size_t)sm.row * vc.target_stride_row;
+    const T* q_row = a != 0.0 ? draft + (size_t)sm.row * vc.draft_stride_row : nullptr;
+    double mine = 0.0;
+    for (int s = warp; s < n_segs; s += kVerifyWarps) {
+      const int lo = (seg0 + s) * seg_len, hi = min(V, lo + seg_len);
+      bool has_gone = false;
+      for (int i = lane; i < gone; i += 32) has_gone |= sm.gone[i] >= lo && sm.gone[i] < hi;
+      has_gone = __any_sync(0xffffffffu, has_gone);
+      double sum = 0.0;
+      for (int i0 = lo + lane; i0 < hi; i0 += kSegUnit) {
+        float pv[kUnroll], qv[kUnroll];
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+          const int i = i0 + 32 * k;
+          pv[k] = i < hi ? raw_prob(p_row + i) : 0.f;
+          qv[k] = q_row && i < hi ? raw_prob(q_row + i) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+          double w = prob(pv[k]);
+          if (q_row) w = fmax(w - a * prob(qv[k]), 0.0);
+          if (has_gone)
+            for (int j = 0; j < gone; ++j)
+              if (sm.gone[j] == i0 + 32 * k) w = 0.0;
+          sum += w;
+        }
+      }
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      if (lane == 0) sm.seg_sum[s] = sum;
+      mine += sum;
+    }
+    if (lane == 0) sm.warp_sum[warp] = mine;
+    __syncthreads();
+    if (tid < n_ranks) {   // this CTA's sum to every CTA of the cluster
+      double sum = 0.0;
+      for (int w = 0; w < kVerifyWarps; ++w) sum += sm.warp_sum[w];
+      *cluster.map_shared_rank(&sm.part[pass & 1][rank], tid) = sum;
+    }
+    cluster.sync();   // (no CTA writes the same half of part[] again before all have come through the next pass's)
+  }
+
+  // ---- results
+  if (rank == 0 && warp == 0) {
+    if (lane == 0) vc.n_accepted[b] = taken;
+    for (int t = lane; t < n_nodes; t += 32) vc.path[(size_t)b * n_nodes + t] = t < taken ? sm.path[t] : -1;
+  }
+  // The draw: the token is in the share of the first CTA whose running sum exceeds the threshold.  (Sums taken in
+  // another order may differ in the last bit, so the last one with any weight stands in where none does.)
+  if (warp != 0) return;
+  const double* part = sm.part[(pass - 1) & 1];   // (the walk draws after at least one pass)
+  double sum = 0.0;
+  for (int r = 0; r < n_ranks; ++r) sum += part[r];
+  const double threshold = (double)vc.u_sample[b] * sum;
+  double run = 0.0, before = 0.0, before_last = 0.0;
+  int owner = -1, last_with = -1;
+  for (int r = 0; r < n_ranks && owner < 0; ++r) {
+    if (part[r] > 0.0) {
+      last_with = r;
+      before_last = run;
+      if (run + part[r] > threshold) { owner = r; before = run; }
+    }
+    run += part[r];
+  }
+  if (owner < 0) { owner = last_with; before = before_last; }
+  if (owner < 0 && rank == 0 && lane == 0) vc.next_token[b] = -1;   // a target row without any weight
+  if (rank != owner) return;
+  // the segment, then the position in it: the first whose running sum exceeds the threshold, else the last with weight
+  int seg = -1;
+  run = before;
+  for (int s0 = 0; s0 < n_segs; s0 += 32) {
+    const double v = s0 + lane < n_segs ? sm.seg_sum[s0 + lane] : 0.0;
+    const double upto = run + running_sum(v, lane);
+    const unsigned over = __ballot_sync(0xffffffffu, v > 0.0 && upto > threshold), with = __ballot_sync(0xffffffffu, v > 0.0);
+    const int pick = over ? __ffs(over) - 1 : with ? 31 - __clz(with) : -1;
+    if (pick >= 0) {
+      seg = s0 + pick;
+      before = __shfl_sync(0xffffffffu, upto - v, pick);
+    }
+    if (over) break;
+    run = __shfl_sync(0xffffffffu, upto, 31);
+  }
+  const double a = sm.minus;
+  const T* p_row = target + (size_t)sm.row * vc.target_stride_row;
+  const T* q_row = a != 0.0 ? draft + (size_t)sm.row * vc.draft_stride_row : nullptr;
+  const int lo = (seg0 + seg) * seg_len, hi = min(V, lo + seg_len);
+  int token = -1;
+  run = before;
+  for (int i0 = lo; i0 < hi; i0 += 32) {
+    const double w = i0 + lane < hi ? weight_at(sm, p_row, q_row, a, i0 + lane) : 0.0;
+    const double upto = run + running_sum(w, lane);
+    const unsigned over = __ballot_sync(0xffffffffu, w > 0.0 && upto > threshold), with = __ballot_sync(0xffffffffu, w > 0.0);
+    if (over || with) token = i0 + (over ? __ffs(over) - 1 : 31 - __clz(with));
+    if (over) break;
+    run = __shfl_sync(0xffffffffu, upto, 31);
+  }
+  if (lane == 0) vc.next_token[b] = token;
+}
+
+}  // namespace
+
+cudaError_t launch_verify(const VerifyCall& call, int dtype, cudaStream_t stream) {
+  VerifyCall vc = call;
+  // segments: at most kMaxSegs to a CTA
+  const long long units = ((long long)vc.vocab + kSegUnit - 1) / kSegUnit;
+  vc.seg_len = (int)(kSegUnit * ((units + (long long)kVerifyCluster * kMaxSegs - 1) / ((long long)kVerifyCluster * kMaxSegs)));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)vc.batch * kVerifyCluster);
+  cfg.blockDim = dim3(kVerifyThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = kVerifyCluster;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return dtype == RAZOR_BF16 ? cudaLaunchKernelEx(&cfg, verify_kernel<__nv_bfloat16>, vc)
+                             : cudaLaunchKernelEx(&cfg, verify_kernel<float>, vc);
+}
+
+}  // namespace razor
