@@ -32,7 +32,7 @@ inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 inline int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 struct Layout {
-  size_t state, comp_sum, comp_mean, ring_sum, ring_valid, page_table, items, jobs, multi, rec_ml, rec_o, queue, tickets, scratch, plan, slopes, round_items, round_units, total;
+  size_t state, comp_sum, comp_mean, ring_sum, ring_valid, page_table, items, jobs, multi, rec_ml, rec_o, queue, tickets, scratch, plan, slopes, round_items, round_units, tree_units, total;
   int max_pages, max_items;
 };
 
@@ -84,6 +84,7 @@ Layout make_layout(const razor_config_t& c) {
   l.slopes = take(L * (size_t)c.n_q_heads * sizeof(float));
   l.round_items = take((size_t)kRoundMaxItems * sizeof(RoundItem));
   l.round_units = take((size_t)kRoundMaxUnits * sizeof(RoundUnit));
+  l.tree_units = take((size_t)kTreeMaxSpans * sizeof(TreeUnit));
   l.total = off;
   return l;
 }
@@ -259,6 +260,7 @@ int razor_cache_create(razor_cache_t** out, const razor_config_t* cfg, void* poo
   dv.alibi_slopes = (float*)(ws + lay.slopes);
   dv.round_items = (RoundItem*)(ws + lay.round_items);
   dv.round_units = (RoundUnit*)(ws + lay.round_units);
+  dv.tree_units = (TreeUnit*)(ws + lay.tree_units);
   dv.alibi = 0;
   dv.n_heads = cfg->batch * cfg->n_kv_heads;
   dv.n_kv_heads = cfg->n_kv_heads;
@@ -765,8 +767,11 @@ int razor_decode_attention_tree(razor_cache_t* c, int32_t layer, const void* q, 
   tc.q = q; tc.k = k_draft; tc.v = v_draft; tc.parent = parent; tc.out = out;
   tc.q_stride_b = q_stride_b; tc.q_stride_t = q_stride_t; tc.kv_stride_b = kv_stride_b; tc.kv_stride_t = kv_stride_t;
   tc.n_nodes = n_nodes;
-  RZ_CUDA(launch_tree(c->dv, cfg.dtype, layer, tc, longest, (long long)c->lay.max_items * kMaxGroup, c->n_sms,
-                      (cudaStream_t)stream));
+  const long long rec_rows = (long long)c->lay.max_items * kMaxGroup;
+  if (cfg.dtype == RAZOR_BF16)
+    RZ_CUDA(launch_tree_mma(c->dv, c->pool_pages, layer, tc, rec_rows, c->n_sms, (cudaStream_t)stream));
+  else
+    RZ_CUDA(launch_tree_rows(c->dv, cfg.dtype, layer, tc, longest, rec_rows, c->n_sms, (cudaStream_t)stream));
   c->last_writer_layer = -1;
   c->writes_since_decode.clear();   // an ordinary launch: everything before it has completed when it starts
   c->writes_overflow = false;

@@ -192,7 +192,7 @@ cudaError_t rows_launch(const DeviceView& dv, int layer, const TreeCall& tc, cud
 
 }  // namespace
 
-cudaError_t launch_tree(const DeviceView& dv, int dtype, int layer, const TreeCall& call, int longest, long long rec_rows,
+cudaError_t launch_tree_rows(const DeviceView& dv, int dtype, int layer, const TreeCall& call, int longest, long long rec_rows,
                         int n_sms, cudaStream_t s) {
   TreeCall tc = call;
   // Parts: about four CTAs per SM in all, at least 256 tokens to a part, no more than the records have rows for.
