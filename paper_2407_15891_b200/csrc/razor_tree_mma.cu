@@ -45,7 +45,8 @@ namespace {
 constexpr int kTok = 128;                       // tokens of a step = tensor-memory lanes
 constexpr int kStepPages = kTok / kPageTokens;
 constexpr int kSoftWarps = 8;
-constexpr int kMmaThreads = (kSoftWarps + 2) * 32;
+constexpr int kMmaThreads = (kSoftWarps + 4) * 32;   // (two of the last four warps have no part)
+constexpr int kFlush = 16;                      // steps whose products add up in tensor memory
 constexpr int kItemSlots = 4;
 constexpr int kMaxStages = 4;                   // of K and of V
 constexpr float kLag = 20.f;                    // log2 of how far a weight may outgrow the reference maximum
@@ -89,8 +90,8 @@ struct TreeSmem {
   static constexpr int kP = kTok * 2 * R * 2;
   static constexpr int kMax = 232448;
   static constexpr int kRoom = kMax - kQ - kP - (int)sizeof(TreeCtl<R>);
-  static constexpr int kV = kRoom / (2 * kKv) < kMaxStages ? kRoom / (2 * kKv) : kMaxStages;   // stages
-  static constexpr int kK = kRoom / kKv - kV < kMaxStages ? kRoom / kKv - kV : kMaxStages;     // (a stage left over goes to K)
+  static constexpr int kK = kRoom / (2 * kKv) < kMaxStages ? kRoom / (2 * kKv) : kMaxStages;   // stages
+  static constexpr int kV = kRoom / kKv - kK < kMaxStages ? kRoom / kKv - kK : kMaxStages;     // (one left over goes to V: it is held a step longer)
   static constexpr int kBytes = (kK + kV) * kKv + kQ + kP + (int)sizeof(TreeCtl<R>);
   static_assert(kV >= 2 && kK >= 2 && kBytes <= kMax, "shared memory");
 };
@@ -197,7 +198,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   Ctl* ctl = (Ctl*)(q_tile + Smem::kQ);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   volatile int* abort_flag = &ctl->abort_flag;
-  const int G = dv.group, n_nodes = tc.n_nodes;
+  const int G = dv.group, lg = __ffs(G) - 1, n_nodes = tc.n_nodes;   // (the group is a power of two)
   const int tile = blockIdx.x % tc.n_tiles, span = blockIdx.x / tc.n_tiles;
   const HeadState* states = dv.state + (size_t)layer * dv.n_heads;
   if (smem_u32(tree_smem) & 1023u) {   // (the operand layouts need it; the first byte of a CTA's dynamic shared memory is)
@@ -290,6 +291,10 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const long long span_len = first_head >= 0 ? bounds[0] : 0;
   __syncthreads();   // (the scratch becomes the tile of P)
 
+  // Registers: 168 a thread at launch; the softmax warps (two warpgroups) take what the third does not need.
+  // (3 x 128 x 168 at launch; 2 x 128 x 224 + 128 x 56 = as many after the split)
+  if (warp >= kSoftWarps) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
   if (warp == kSoftWarps) {
     // ================================================================ producer: items and TMA copies
     unsigned gk = 0, gi = 0, gq = 0;   // steps issued, items published, query tiles issued
@@ -387,7 +392,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     if (lane == 0) {
       bool ok = true, pending = false, pend_first = false;
       unsigned g = 0;                  // steps whose scores have been issued
-      unsigned pend_item = 0;
+      unsigned pend_flush = 0, n_flush = 0;   // accumulators begun before the pending one; begun so far
       int pend_kk = 0;
       const uint32_t q0 = smem_u32(q_tile), p0 = smem_u32(p_tile);
       // O^T of step g - 1
@@ -395,8 +400,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         const int s = step % NV;
         if (!mbar_wait(&ctl->p_full, step & 1, abort_flag)) return false;
         if (!mbar_wait(&ctl->v_full[s], (step / NV) & 1, abort_flag)) return false;
-        // the first product of an item overwrites the accumulator: the item before must have been read out
-        if (pend_first && pend_item >= 1 && !mbar_wait(&ctl->o_read, (pend_item - 1) & 1, abort_flag)) return false;
+        // the first product of an accumulator overwrites the one before, which must have been read out
+        if (pend_first && pend_flush >= 1 && !mbar_wait(&ctl->o_read, (pend_flush - 1) & 1, abort_flag)) return false;
         tc_fence_after();
         const uint32_t v0 = smem_u32(v_ring + s * KV);
         for (int kk = 0; kk < pend_kk; ++kk)   // 16 tokens per instruction
@@ -441,8 +446,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           const bool draft = it.draft && i == n - 1;
           const int left = draft ? n_nodes : it.st.len - (it.begin + i) * kTok;
           pending = true;
-          pend_first = i == 0;
-          pend_item = gi;
+          pend_first = i % kFlush == 0;
+          pend_flush = pend_first ? n_flush++ : n_flush;
           pend_kk = min(kTok / 16, (left + 15) / 16);
         }
       }
@@ -454,12 +459,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       }
     }
     __syncwarp();
+  }
   } else {
     // ================================================================ softmax and epilogue: a thread per token
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
     const int half = warp >> 2, quarter = warp & 3;         // column half; tensor-memory lane quarter
     const int tk = quarter * 32 + lane;                     // token of the step; in the epilogue, dimension of the output
     const int c0 = half * NC;                               // first column
-    constexpr int LC = NC > 32 ? 2 : 1;                     // columns whose bookkeeping a lane carries
+    constexpr int LC = NC > 32 ? 2 : 1, W = NC / LC;        // columns whose bookkeeping a lane carries; run of columns in registers
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
     const float scale_log2 = dv.scale_log2;
     const uint64_t scale2 = f2_pack(scale_log2, scale_log2);
@@ -488,7 +495,14 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       const int b = it.head / dv.n_kv_heads, g_kv = it.head % dv.n_kv_heads;
       const int total = it.st.len + it.st.n_drop;
       const int32_t* parent = tc.parent + (size_t)b * n_nodes;
-      auto node_of = [&](int c) { return min(row0 + c0 + c, rows - 1) / G; };
+      // node and query head of this lane's columns, and where the row stands in the output (from the item's first row on)
+      int node[LC], place[LC];
+#pragma unroll
+      for (int k = 0; k < LC; ++k) {
+        const int r = min(row0 + c0 + (NC < 32 ? lane % NC : lane + 32 * k), rows - 1);
+        node[k] = r >> lg;
+        place[k] = ((r >> lg) * dv.n_kv_heads * G + (r & (G - 1))) * D;
+      }
 
       // ---- the tree (items that hold its tokens; with ALiBi, all: a row's position is its node's depth)
       uint32_t vis[LC] = {}, live[LC] = {};   // columns that see this thread's draft; columns that are a node of the tree
@@ -502,11 +516,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         tree_mask_walk(*mask, n_nodes, tid, kSoftWarps * 32);
         if (!(ok = all_sync())) break;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          if (row0 + c0 + c < rows) {
-            const int t = node_of(c);
-            if (tree_sees(*mask, t, t)) live[LC == 2 ? c >> 5 : 0] |= 1u << (c & 31);
-            if (tk < n_nodes && tree_sees(*mask, t, tk)) vis[LC == 2 ? c >> 5 : 0] |= 1u << (c & 31);
+        for (int k = 0; k < LC; ++k) {
+          live[k] = __ballot_sync(0xffffffffu, lane + 32 * k < NC && row0 + c0 + lane + 32 * k < rows && tree_sees(*mask, node[k], node[k]));
+#pragma unroll 4
+          for (int c = 0; c < W; ++c) {   // (tokens are nodes here: this warp's are bits of one word)
+            const int t = __shfl_sync(0xffffffffu, node[k], c);
+            vis[k] |= (mask->see[t][quarter] >> lane & live[k] >> c & 1u) << c;
           }
         }
         if constexpr (kAlibi) {
@@ -516,8 +531,8 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
             for (int i = 0; i < LC; ++i) {
               const int c = lane + 32 * i;
               if (c < NC) {
-                ctl->depth[c0 + c] = (float)mask->depth[node_of(c)];
-                ctl->slope[c0 + c] = dv.alibi_slopes[((size_t)layer * dv.n_kv_heads + g_kv) * G + min(row0 + c0 + c, rows - 1) % G];
+                ctl->depth[c0 + c] = (float)mask->depth[node[i]];
+                ctl->slope[c0 + c] = dv.alibi_slopes[((size_t)layer * dv.n_kv_heads + g_kv) * G + (min(row0 + c0 + c, rows - 1) & (G - 1))];
               }
             }
           }
@@ -535,7 +550,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 #pragma unroll
         for (int e = 0; e < EPL; ++e) kh[e] = k_hat[lane * EPL + e];
         for (int c = quarter; c < NC; c += 4) {
-          const int r = min(row0 + c0 + c, rows - 1), t = r / G, j = r % G;
+          const int r = min(row0 + c0 + c, rows - 1), t = r >> lg, j = r & (G - 1);
           const __nv_bfloat16* src = (const __nv_bfloat16*)tc.q + (size_t)b * tc.q_stride_b + (size_t)t * tc.q_stride_t + ((size_t)g_kv * G + j) * D + lane * EPL;
           float s = 0.f;
 #pragma unroll
@@ -552,9 +567,32 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         m_lane[i] = it.seed ? -ctl->neg_m[c0 + (NC < 32 ? lane % NC : lane + 32 * i)] : -CUDART_INF_F;
         w_seed[i] = it.seed ? 1.f : 0.f;
       }
-      float l[NC];
+      // Sums of the weights of this thread's tokens, and this thread's dimension of the rows' outputs: the accumulator in
+      // tensor memory is added on every kFlush steps.  (The matrix unit truncates when it adds to the accumulator; over
+      // the thousand products of a long span that bias reached 1.6e-5 of the result, 4e-6 with sixteen steps.)
+      // (With 64 columns to a thread the sum lives in local memory - its loops are not unrolled -, which costs less than
+      // spilling what the steps use.)
+      constexpr int kUnroll = LC == 2 ? 1 : NC / 16;
+      float l[NC], acc[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) l[c] = 0.f;
+#pragma unroll kUnroll
+      for (int c = 0; c < NC; c += 16)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[c + e] = 0.f;
+      auto flush = [&]() {
+        tc_fence_after();
+#pragma unroll kUnroll
+        for (int c = 0; c < NC; c += 16) {
+          uint32_t oh[16], ol[16];
+          tmem_load<16>(lane_addr + kOCol + (uint32_t)(c0 + c), oh);
+          tmem_load<16>(lane_addr + kOCol + (uint32_t)(R + c0 + c), ol);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[c + e] += __uint_as_float(oh[e]) + __uint_as_float(ol[e]);
+        }
+        tc_fence_before();
+        warp_arrive(&ctl->o_read, lane);
+      };
 
       const int n = it.end - it.begin + it.draft;
       for (int i = 0; i < n && ok; ++i, ++g) {
@@ -567,19 +605,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         ok = warp_wait(&ctl->s_full[g & 1], (g / 2) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        uint32_t v[NC];
-        // scores to log2 domain, minus the reference; returns whether one outran it
-        auto scores = [&]() -> bool {
-          tmem_load<NC>(lane_addr + (g & 1) * R + c0, v);
+        uint32_t v[W];
+        // scores of a run of W columns to the log2 domain, minus the reference; returns whether one outran it
+        auto scores = [&](const int run) -> bool {
+          const int cr = c0 + run * W;
+          tmem_load<W>(lane_addr + (g & 1) * R + cr, v);
           float mx = -CUDART_INF_F;
 #pragma unroll
-          for (int c = 0; c < NC; c += 4) {
-            const float4 nm = *(const float4*)&ctl->neg_m[c0 + c];
+          for (int c = 0; c < W; c += 4) {
+            const float4 nm = *(const float4*)&ctl->neg_m[cr + c];
             float t[4];
             f2_unpack(f2_fma(f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, f2_pack(nm.x, nm.y)), t[0], t[1]);
             f2_unpack(f2_fma(f2_pack(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), scale2, f2_pack(nm.z, nm.w)), t[2], t[3]);
             if constexpr (kAlibi) {
-              const float4 sl = *(const float4*)&ctl->slope[c0 + c], de = *(const float4*)&ctl->depth[c0 + c];
+              const float4 sl = *(const float4*)&ctl->slope[cr + c], de = *(const float4*)&ctl->depth[cr + c];
               t[0] = fmaf(sl.x, rel - de.x, t[0]);
               t[1] = fmaf(sl.y, rel - de.y, t[1]);
               t[2] = fmaf(sl.z, rel - de.z, t[2]);
@@ -591,45 +630,53 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           }
           if (draft) {
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              if (!(vis[LC == 2 ? c >> 5 : 0] >> (c & 31) & 1)) v[c] = 0xff800000u;
+            for (int c = 0; c < W; ++c) {
+              if (!(vis[run] >> c & 1)) v[c] = 0xff800000u;
               mx = fmaxf(mx, __uint_as_float(v[c]));
             }
           } else if (!valid) {
             mx = -CUDART_INF_F;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) v[c] = 0xff800000u;
+            for (int c = 0; c < W; ++c) v[c] = 0xff800000u;
           }
           return mx > kLag;
         };
         auto weights = [&]() {
 #pragma unroll
-          for (int c = 0; c < NC; ++c) v[c] = __float_as_uint(fast_exp2(__uint_as_float(v[c])));
+          for (int c = 0; c < W; ++c) v[c] = __float_as_uint(fast_exp2(__uint_as_float(v[c])));
         };
-        const bool outran = scores();
+        // (with two runs of columns the second stays in registers and the first is computed again: fewer registers)
+        bool outran = false;
+#pragma unroll
+        for (int run = 0; run < LC; ++run) outran |= scores(run);
         if (__any_sync(0xffffffffu, outran) && lane == 0) *(volatile uint32_t*)&ctl->need[half][g & 1] = g + 1;
         warp_arrive(&ctl->agree[half], lane);
         weights();
         ok = warp_wait(&ctl->agree[half], n_agree++ & 1, abort_flag);
         if (!ok) break;
-        bool p_free = g == 0;
-        if (*(volatile uint32_t*)&ctl->need[half][g & 1] == g + 1) {
+        bool flush_now = i > 0 && i % kFlush == 0;
+        const bool move = *(volatile uint32_t*)&ctl->need[half][g & 1] == g + 1;
+        if (move) {
           // ---- move the references that were outrun to the maximum of what has been seen
-          if (!p_free) {
+          if (g > 0) {
             ok = warp_wait(&ctl->p_done, (g - 1) & 1, abort_flag);
             if (!ok) break;
-            p_free = true;
           }
+          if (flush_now) flush();
+          flush_now = false;
           int32_t* top = ctl->top[n_top & 1];
-          uint32_t s[NC];
-          tmem_load<NC>(lane_addr + (g & 1) * R + c0, s);
+#pragma unroll 1
+          for (int c = 0; c < NC; c += 16) {
+            uint32_t s[16];
+            tmem_load<16>(lane_addr + (g & 1) * R + c0 + c, s);
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            float t = __uint_as_float(s[c]) * scale_log2;
-            if constexpr (kAlibi) t = fmaf(ctl->slope[c0 + c], rel - ctl->depth[c0 + c], t);
-            if (draft ? !(vis[LC == 2 ? c >> 5 : 0] >> (c & 31) & 1) : !valid) t = -CUDART_INF_F;
-            t = warp_max(t);
-            if (lane == (c & 31)) atomicMax(&top[c0 + c], ordered(t));
+            for (int e = 0; e < 16; ++e) {
+              float t = __uint_as_float(s[e]) * scale_log2;
+              if constexpr (kAlibi) t = fmaf(ctl->slope[c0 + c + e], rel - ctl->depth[c0 + c + e], t);
+              if (draft ? !(vis[LC == 2 ? c >> 5 : 0] >> ((c + e) & 31) & 1) : !valid) t = -CUDART_INF_F;
+              t = warp_max(t);
+              if (lane == e) atomicMax(&top[c0 + c + e], ordered(t));
+            }
           }
           if (!(ok = group_sync())) break;
           float f[LC];
@@ -651,50 +698,66 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           if (!(ok = group_sync())) break;
 #pragma unroll
           for (int c = 0; c < NC; ++c) l[c] *= pick(f, c);
-          if (i >= 1) {   // the accumulator holds products of this item
-            tc_fence_after();
+          tc_fence_after();
+#pragma unroll kUnroll
+          for (int c = 0; c < NC; c += 16) {
+            float fc[16];
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
+            for (int e = 0; e < 16; ++e) {
+              fc[e] = __shfl_sync(0xffffffffu, LC == 2 && c >= 32 ? f[LC - 1] : f[0], (c + e) & 31);
+              acc[c + e] *= fc[e];
+            }
+            if (i % kFlush != 0) {   // the accumulator holds products of this item
 #pragma unroll
-              for (int c = 0; c < NC; c += 16) {
+              for (int part = 0; part < 2; ++part) {
                 const uint32_t addr = lane_addr + kOCol + (uint32_t)(part * R + c0 + c);
                 uint32_t o[16];
                 tmem_load<16>(addr, o);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * pick(f, c + e));
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fc[e]);
                 tmem_st16(addr, o);
               }
             }
-            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           }
-          (void)scores();
-          weights();
-        }
-        tc_fence_before();
-        warp_arrive(&ctl->s_empty[g & 1], lane);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) l[c] += __uint_as_float(v[c]);
-        // ---- the weights, as a bf16 head (their upper 16 bits) plus a bf16 remainder, once the product of the step before
-        // has read its own
-        if (!p_free) {
+          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        } else if (g > 0) {   // the product of the step before must have read its weights
           ok = warp_wait(&ctl->p_done, (g - 1) & 1, abort_flag);
           if (!ok) break;
         }
+        if (flush_now) flush();
         uint8_t* p_row = p_tile + tk * 128;
 #pragma unroll
-        for (int c = 0; c < NC; c += 8) {
-          uint32_t hi[4], lo[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t b0 = v[c + 2 * k], b1 = v[c + 2 * k + 1];
-            hi[k] = __byte_perm(b0, b1, 0x7632);
-            const __nv_bfloat162 r = __floats2bfloat162_rn(__uint_as_float(b0) - __uint_as_float(b0 & 0xffff0000u),
-                                                           __uint_as_float(b1) - __uint_as_float(b1 & 0xffff0000u));
-            lo[k] = *(const uint32_t*)&r;
+        for (int run = LC - 1; run >= 0; --run) {
+          if (move || run < LC - 1) {
+            (void)scores(run);
+            weights();
           }
-          const int ch = c0 + c, cl = R + ch;   // columns of heads and remainders in the 2R-column operand
-          *(uint4*)(p_row + (ch >> 6) * (128 * kTok) + ((((ch & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *(uint4*)(p_row + (cl >> 6) * (128 * kTok) + ((((cl & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          if (run == 0) {   // S is read out
+            tc_fence_before();
+            warp_arrive(&ctl->s_empty[g & 1], lane);
+          }
+#pragma unroll
+          for (int c = 0; c < W; c += 2)
+            f2_unpack(f2_add(f2_pack(l[run * W + c], l[run * W + c + 1]), f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1]))),
+                      l[run * W + c], l[run * W + c + 1]);
+          // ---- a weight is written as a bf16 head (its upper 16 bits) plus a bf16 remainder
+#pragma unroll
+          for (int c = 0; c < W; c += 8) {
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t b0 = v[c + 2 * k], b1 = v[c + 2 * k + 1];
+              hi[k] = __byte_perm(b0, b1, 0x7632);
+              float r0, r1;
+              f2_unpack(f2_sub(f2_pack(__uint_as_float(b0), __uint_as_float(b1)),
+                               f2_pack(__uint_as_float(b0 & 0xffff0000u), __uint_as_float(b1 & 0xffff0000u))), r0, r1);
+              const __nv_bfloat162 r = __floats2bfloat162_rn(r0, r1);
+              lo[k] = *(const uint32_t*)&r;
+            }
+            const int ch = c0 + run * W + c, cl = R + ch;   // columns of heads and remainders in the 2R-column operand
+            *(uint4*)(p_row + (ch >> 6) * (128 * kTok) + ((((ch & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *(uint4*)(p_row + (cl >> 6) * (128 * kTok) + ((((cl & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          }
         }
         // ---- V rows that no weight may meet: a zero weight times a NaN is a NaN.  Behind the head's last token the pool
         // may hold anything; a draft is hidden from the nodes of other branches.
@@ -737,13 +800,12 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       // ---- the rows' results
       ok = warp_wait(&ctl->p_done, (g - 1) & 1, abort_flag);
       if (!ok) break;
-      tc_fence_after();
+      flush();
       float* l_part = (float*)(p_tile + 8192) + half * 4 * NC;   // [quarter][NC]
       static_assert(8192 + 8 * NC * 4 <= Smem::kP, "scratch");
       float l_lane[LC];
 #pragma unroll
       for (int k = 0; k < LC; ++k) {
-        constexpr int W = NC < 32 ? NC : 32;
         const float x = column_sum<W>(l + 32 * k, lane);
         if (lane + 32 * k < NC) l_part[quarter * NC + lane + 32 * k] = x;
       }
@@ -759,42 +821,39 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           dv.rec_ml[(size_t)it.rec * R + c0 + c] = make_float2(m_lane[k], it.draft && !(live[k] >> (c & 31) & 1) ? -1.f : l_lane[k]);
       }
       const bool poisoned = it.draft && (ctl->bad_v[0] | ctl->bad_v[1] | ctl->bad_v[2] | ctl->bad_v[3]) != 0;
+      // The NaN and infinities that were taken out of the drafts' V reach the rows that see them.
+      auto add_poison = [&](float x, int r) -> float {
+#pragma unroll 1
+        for (int nd = 0; nd <= r >> lg; ++nd) {
+          if (!(ctl->bad_v[nd >> 5] >> (nd & 31) & 1) || !walk_sees(parent, r >> lg, nd)) continue;
+          const float bad = __bfloat162float(((const __nv_bfloat16*)tc.v)[(size_t)b * tc.kv_stride_b + (size_t)nd * tc.kv_stride_t + (size_t)g_kv * D + tk]);
+          if (!(fabsf(bad) < CUDART_INF_F)) x += bad;
+        }
+        return x;
+      };
       if (quarter * 32 < D) {
         const float v_hat = it.seed ? dv.comp_mean[hs * 2 * D + D + tk] : 0.f;
-#pragma unroll 1
+        float* dst = direct ? tc.out + ((size_t)b * n_nodes * dv.n_kv_heads + g_kv) * G * D + tk : dv.rec_o + ((size_t)it.rec * R + c0) * D + tk;
+        const int n_cols = min(NC, rows - (row0 + c0));   // (rows behind the last are nobody's)
+#pragma unroll kUnroll
         for (int cb = 0; cb < NC; cb += 16) {
-          if (row0 + c0 + cb >= rows) break;
-          uint32_t oh[16], ol[16];
-          tmem_load<16>(lane_addr + kOCol + (uint32_t)(c0 + cb), oh);
-          tmem_load<16>(lane_addr + kOCol + (uint32_t)(R + c0 + cb), ol);
+          const bool up = LC == 2 && cb >= 32;
+          const float w16 = up ? w_seed[LC - 1] : w_seed[0], i16 = up ? inv[LC - 1] : inv[0];
+          const int p16 = up ? place[LC - 1] : place[0];
+          const uint32_t live16 = up ? live[LC - 1] : live[0];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int c = cb + e, r = row0 + c0 + c;
-            float x = __uint_as_float(oh[e]) + __uint_as_float(ol[e]);
-            const int src = c & 31;
-            const float ws = __shfl_sync(0xffffffffu, LC == 2 && c >= 32 ? w_seed[LC - 1] : w_seed[0], src);
-            const float iv = __shfl_sync(0xffffffffu, LC == 2 && c >= 32 ? inv[LC - 1] : inv[0], src);
-            if (it.seed) x = fmaf(ws, v_hat, x);
-            if (r >= rows) continue;
-            const int t = r / G, j = r % G;
-            if (poisoned) {
-              for (int nd = 0; nd <= t; ++nd) {
-                if (!(ctl->bad_v[nd >> 5] >> (nd & 31) & 1) || !walk_sees(parent, t, nd)) continue;
-                const float bad = __bfloat162float(((const __nv_bfloat16*)tc.v)[(size_t)b * tc.kv_stride_b + (size_t)nd * tc.kv_stride_t + (size_t)g_kv * D + tk]);
-                if (!(fabsf(bad) < CUDART_INF_F)) x += bad;
-              }
-            }
-            if (direct) {
-              if ((c < 32 ? live[0] : live[LC - 1]) >> (c & 31) & 1)
-                tc.out[(((size_t)b * n_nodes + t) * dv.n_kv_heads * G + (size_t)g_kv * G + j) * D + tk] = x * iv;
-            } else {
-              dv.rec_o[((size_t)it.rec * R + c0 + c) * D + tk] = x;
-            }
+            const int c = cb + e;
+            float x = fmaf(__shfl_sync(0xffffffffu, w16, c & 31), v_hat, acc[c]);
+            const float iv = __shfl_sync(0xffffffffu, i16, c & 31);
+            const int at = __shfl_sync(0xffffffffu, p16, c & 31);
+            if (c >= n_cols) continue;
+            if (poisoned) x = add_poison(x, row0 + c0 + c);
+            if (!direct) dst[c * D] = x;
+            else if (live16 >> (c & 31) & 1) dst[at] = x * iv;
           }
         }
       }
-      tc_fence_before();
-      warp_arrive(&ctl->o_read, lane);
       if (!(ok = all_sync())) break;   // (the scratch in P's tile, and bad_v, are done with)
     }
     if (!ok && lane == 0) atomicOr(dv.status, kStatusReducerTimeout);
