@@ -19,13 +19,13 @@
 // call costs the host nothing but the launch, and a captured graph follows the cache as it grows.  A head that a cut runs
 // through leaves one partial record per span; tree_combine_kernel folds them.
 //
-// A CTA (one per SM): eight softmax warps (two per tensor-memory lane quarter, each with half of the columns), a producer
+// A CTA (one per SM): softmax warps (one per tensor-memory lane quarter and group of columns), a producer
 // warp (TMA: pages of the pool, whose rows are stored in the swizzle of the operand layout; drafts and queries through
 // maps of their own) and a warp that issues the matrix instructions.  S is double-buffered, so the scores of the next
 // step are computed during the softmax of this one.
 //
 // The running maximum of a row is a reference that may lag: weights are 2^(s - m), floats, as exact at 2^20 as at one.  It
-// is moved (and the accumulator rescaled) only when a score outruns it by 2^kLag; the four warps of a column half agree on
+// is moved (and the accumulator rescaled) only when a score outruns it by 2^kLag; the four warps of a column group agree on
 // that once per step, and compute their weights while the agreement is on its way.
 //
 // Every wait is bounded in time; a wait that runs out sets the CTA's abort flag and a bit of the device status word,
@@ -44,10 +44,12 @@ namespace {
 
 constexpr int kTok = 128;                       // tokens of a step = tensor-memory lanes
 constexpr int kStepPages = kTok / kPageTokens;
-constexpr int kSoftWarps = 8;
-constexpr int kMmaThreads = (kSoftWarps + 4) * 32;   // (two of the last four warps have no part)
+// Eight softmax warps: two groups of columns, four warps each (one per tensor-memory lane quarter).  (Sixteen warps with
+// half as many columns each had 104 registers apiece and spilled, and next to 227 KB of shared memory there is no L1 to
+// spill to: slower for 64 rows and for 128.)  Two further warps feed them, and two have no part.
+constexpr int kGroups = 2, kSoftWarps = 4 * kGroups, kTreeThreads = (kSoftWarps + 4) * 32;
 constexpr int kFlush = 16;                      // steps whose products add up in tensor memory
-constexpr int kItemSlots = 4;
+constexpr int kItemSlots = 3;
 constexpr int kMaxStages = 4;                   // of K and of V
 constexpr float kLag = 20.f;                    // log2 of how far a weight may outgrow the reference maximum
 constexpr float kLow = -3.0e38f;                // stands for a reference maximum of minus infinity in the arithmetic
@@ -66,16 +68,16 @@ struct TreeCtl {
   uint64_t q_full, q_empty;
   uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
   uint64_t s_full[2], s_empty[2];     // per S buffer
-  uint64_t p_full, p_done;            // the weights are in shared memory; the product that read them has run
-  uint64_t o_read;                    // the accumulator has been read out
+  // per unit of columns: the weights are in shared memory; the product that read them has run; the accumulator has been read out
+  uint64_t p_full[2], p_done[2], o_read[2];
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
-  uint64_t agree[2];                  // the four warps of a column half among themselves
-  uint64_t all_sync;                  // the eight softmax warps among themselves
+  uint64_t agree[kGroups];   // the four warps of a column group among themselves
+  uint64_t all_sync;                  // the softmax warps among themselves
   uint64_t drain;
   uint32_t tmem_base;
   int abort_flag;
-  uint32_t need[2][2];                // [column half][step parity]: step + 1 when a score outran the reference
-  uint32_t bad_v[kTreeMaxNodes / 32]; // drafts whose V holds a NaN or an infinity
+  uint32_t need[kGroups][2]; // [column group][step parity]: step + 1 when a score outran the reference
+  uint32_t bad_v[2][kTreeMaxNodes / 32];   // [item parity]: drafts whose V holds a NaN or an infinity
   TreeItem item[kItemSlots];
   alignas(16) float neg_m[R];                     // minus the reference maximum of each row (log2 domain)
   int32_t top[2][R];                  // column maxima while the reference moves, as ordered integers
@@ -127,21 +129,17 @@ __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&v)[NC]) {
 #pragma unroll
   for (int c = 0; c < NC; ++c) asm volatile("" : "+r"(v[c]));
 }
-__device__ __forceinline__ float warp_max(float x) {
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
-  return r;
-}
 // Floats as integers of the same order.
 __device__ __forceinline__ int ordered(float x) { const int i = __float_as_int(x); return i < 0 ? i ^ 0x7fffffff : i; }
 __device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i < 0 ? i ^ 0x7fffffff : i); }
 
-// Sums over the warp of NC (16 or 32) values per lane: lane c (mod NC) gets the sum of x[c].  Destroys x.
-template <int NC>
-__device__ __forceinline__ float column_sum(float* x, int lane) {
+// Sums (or maxima) over the warp of NC (16 or 32) values per lane: lane c (mod NC) gets that of x[c].  Destroys x.
+template <int NC, bool kMax>
+__device__ __forceinline__ float across_warp(float* x, int lane) {
+  auto join = [](float a, float b) { return kMax ? fmaxf(a, b) : a + b; };
   if constexpr (NC == 16) {
 #pragma unroll
-    for (int c = 0; c < 16; ++c) x[c] += __shfl_xor_sync(0xffffffffu, x[c], 16);
+    for (int c = 0; c < 16; ++c) x[c] = join(x[c], __shfl_xor_sync(0xffffffffu, x[c], 16));
   }
 #pragma unroll
   for (int half = NC / 2; half > 0; half >>= 1) {
@@ -149,7 +147,7 @@ __device__ __forceinline__ float column_sum(float* x, int lane) {
 #pragma unroll
     for (int c = 0; c < half; ++c) {
       const float send = up ? x[c] : x[c + half], keep = up ? x[c + half] : x[c];
-      x[c] = keep + __shfl_xor_sync(0xffffffffu, send, half);
+      x[c] = join(keep, __shfl_xor_sync(0xffffffffu, send, half));
     }
   }
   return x[0];
@@ -178,17 +176,23 @@ __device__ __noinline__ bool walk_sees(const int32_t* parent, int t, int n) {
 }
 
 template <int D, int R, bool kAlibi>
-__global__ void __launch_bounds__(kMmaThreads, 1)
+__global__ void __launch_bounds__(kTreeThreads, 1)
     tree_mma_kernel(DeviceView dv, const __grid_constant__ CUtensorMap map_pool, const __grid_constant__ CUtensorMap map_q,
                     const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, int layer, TreeCall tc) {
   using Smem = TreeSmem<D, R>;
   using Ctl = TreeCtl<R>;
   constexpr int HALVES = D / 64, KV = Smem::kKv, NK = Smem::kK, NV = Smem::kV;
-  constexpr int NC = R / 2;                             // columns of a softmax warp
+  constexpr int SW = kSoftWarps, NT = kTreeThreads;
+  constexpr int NC = R / kGroups;                       // columns of a softmax warp: 16, 32, 64
+  constexpr int LC = NC > 32 ? 2 : 1, LW = NC / LC;     // columns whose bookkeeping a lane carries, LW apart
   constexpr uint32_t kOctet = 8 * D * 2;                // bytes of eight tokens in a stage: [octet][64-element half][8][128 B]
-  constexpr uint32_t kTmemCols = 4 * R, kOCol = 2 * R;  // S, S, O (heads), O (remainders)
+  // A unit of columns has its own weights, accumulator and product.  With 128 rows each column group is a unit, so that one
+  // group's exponentials run beside the other's stores and products (V is read out of shared memory twice for it); with
+  // fewer rows there is one.
+  constexpr int NU = R == 128 ? 2 : 1, RU = R / NU, PU = Smem::kP / NU;
+  constexpr uint32_t kTmemCols = 4 * R, kOCol = 2 * R;  // S, S, then per unit O (heads), O (remainders)
   constexpr uint32_t kIdescS = instr_desc_bf16(kTok, R, false);
-  constexpr uint32_t kIdescO = instr_desc_bf16(kTok, 2 * R, true) | (1u << 15);   // (bit 15: A is MN-major too)
+  constexpr uint32_t kIdescO = instr_desc_bf16(kTok, 2 * RU, true) | (1u << 15);   // (bit 15: A is MN-major too)
 
   extern __shared__ __align__(1024) uint8_t tree_smem[];
   uint8_t* k_ring = tree_smem;
@@ -213,33 +217,38 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     for (int s = 0; s < NV; ++s) { mbar_init(&ctl->v_full[s], 1); mbar_init(&ctl->v_empty[s], 1); }
     for (int s = 0; s < 2; ++s) {
       mbar_init(&ctl->s_full[s], 1);
-      mbar_init(&ctl->s_empty[s], kSoftWarps);
-      mbar_init(&ctl->agree[s], kSoftWarps / 2);
+      mbar_init(&ctl->s_empty[s], SW);
+    }
+    for (int s = 0; s < kGroups; ++s) {
+      mbar_init(&ctl->agree[s], 4);
       ctl->need[s][0] = ctl->need[s][1] = 0;
     }
-    mbar_init(&ctl->p_full, kSoftWarps);
-    mbar_init(&ctl->p_done, 1);
-    mbar_init(&ctl->o_read, kSoftWarps);
-    for (int s = 0; s < kItemSlots; ++s) { mbar_init(&ctl->item_full[s], 1); mbar_init(&ctl->item_empty[s], kSoftWarps + 1); }
-    mbar_init(&ctl->all_sync, kSoftWarps);
+    for (int u = 0; u < NU; ++u) {
+      mbar_init(&ctl->p_full[u], SW / NU);
+      mbar_init(&ctl->p_done[u], 1);
+      mbar_init(&ctl->o_read[u], SW / NU);
+    }
+    for (int s = 0; s < kItemSlots; ++s) { mbar_init(&ctl->item_full[s], 1); mbar_init(&ctl->item_empty[s], SW + 1); }
+    mbar_init(&ctl->all_sync, SW);
     mbar_init(&ctl->drain, 1);
     ctl->abort_flag = 0;
+    for (int k = 0; k < 2 * kTreeMaxNodes / 32; ++k) ctl->bad_v[0][k] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kSoftWarps + 1) {
+  if (warp == SW + 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
                  "r"(kTmemCols)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  for (int c = tid; c < 2 * R; c += kMmaThreads) ctl->top[0][c] = ordered(-CUDART_INF_F);
+  for (int c = tid; c < 2 * R; c += NT) ctl->top[0][c] = ordered(-CUDART_INF_F);
 
   // ---- this CTA's span: a scan over the heads' steps (scratch: the tile of P)
   long long* warp_tot = (long long*)p_tile;
-  int* found = (int*)(p_tile + 256);   // head and step the span begins with
+  int* found = (int*)(p_tile + 256);   // head and step the span begins with, and the head's state
   long long* bounds = (long long*)(p_tile + 512);
   {
-    const int per = (dv.n_heads + kMmaThreads - 1) / kMmaThreads;
+    const int per = (dv.n_heads + NT - 1) / NT;
     const int h0 = min(dv.n_heads, tid * per), h1 = min(dv.n_heads, h0 + per);
     long long mine = 0;
     for (int h = h0; h < h1; ++h) mine += head_steps(states[h].len) + 1;
@@ -253,7 +262,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
     if (tid == 0) found[0] = -1;
     __syncthreads();
     long long before = 0, total = 0;
-    for (int w = 0; w < kMmaThreads / 32; ++w) {
+    for (int w = 0; w < NT / 32; ++w) {
       if (w < warp) before += warp_tot[w];
       total += warp_tot[w];
     }
@@ -271,6 +280,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       }
       found[0] = h;
       found[1] = (int)(x0 - u0);
+      *(HeadState*)(found + 4) = states[h];
       bounds[0] = x1 - x0;
       // the span in which a head is cut for the first time lists it for the combine kernel
       TreeUnit u{h, span - 1, 0, 0};
@@ -289,19 +299,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   const uint32_t tmem = ctl->tmem_base;
   const int first_head = found[0], first_step = found[1];
   const long long span_len = first_head >= 0 ? bounds[0] : 0;
+  const HeadState first_state = first_head >= 0 ? *(const HeadState*)(found + 4) : HeadState{0, 0, 0, 0};
   __syncthreads();   // (the scratch becomes the tile of P)
 
-  // Registers: 168 a thread at launch; the softmax warps (two warpgroups) take what the third does not need.
-  // (3 x 128 x 168 at launch; 2 x 128 x 224 + 128 x 56 = as many after the split)
-  if (warp >= kSoftWarps) {
+  // Registers: the last warpgroup hands over what it does not need (3 x 128 x 168 at launch = 2 x 128 x 224 + 128 x 56).
+  if (warp >= SW) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-  if (warp == kSoftWarps) {
+  if (warp == SW) {
     // ================================================================ producer: items and TMA copies
     unsigned gk = 0, gi = 0, gq = 0;   // steps issued, items published, query tiles issued
     int head = first_head, y = first_step;
     long long todo = span_len;
     bool ok = true;
-    HeadState st = todo > 0 ? states[head] : HeadState{0, 0, 0, 0};
+    HeadState st = first_state;
     for (;; ++gi) {
       TreeItem it;
       it.head = todo > 0 ? head : -1;
@@ -387,7 +397,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       }
     }
     __syncwarp();
-  } else if (warp == kSoftWarps + 1) {
+  } else if (warp == SW + 1) {
     // ================================================================ matrix instructions: one thread
     if (lane == 0) {
       bool ok = true, pending = false, pend_first = false;
@@ -398,17 +408,20 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       // O^T of step g - 1
       auto issue_o = [&](unsigned step) -> bool {
         const int s = step % NV;
-        if (!mbar_wait(&ctl->p_full, step & 1, abort_flag)) return false;
-        if (!mbar_wait(&ctl->v_full[s], (step / NV) & 1, abort_flag)) return false;
-        // the first product of an accumulator overwrites the one before, which must have been read out
-        if (pend_first && pend_flush >= 1 && !mbar_wait(&ctl->o_read, (pend_flush - 1) & 1, abort_flag)) return false;
-        tc_fence_after();
         const uint32_t v0 = smem_u32(v_ring + s * KV);
-        for (int kk = 0; kk < pend_kk; ++kk)   // 16 tokens per instruction
-          umma_bf16_desc(tmem + kOCol, operand_desc_mn(v0 + (uint32_t)kk * 2 * kOctet, 1024, kOctet),
-                         operand_desc_mn(p0 + (uint32_t)kk * 2048, 128 * kTok, 1024), kIdescO, (kk > 0 || !pend_first) ? 1u : 0u);
-        umma_commit(&ctl->v_empty[s]);
-        umma_commit(&ctl->p_done);
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          if (!mbar_wait(&ctl->p_full[u], step & 1, abort_flag)) return false;
+          if (u == 0 && !mbar_wait(&ctl->v_full[s], (step / NV) & 1, abort_flag)) return false;
+          // the first product of an accumulator overwrites the one before, which must have been read out
+          if (pend_first && pend_flush >= 1 && !mbar_wait(&ctl->o_read[u], (pend_flush - 1) & 1, abort_flag)) return false;
+          tc_fence_after();
+          for (int kk = 0; kk < pend_kk; ++kk)   // 16 tokens per instruction
+            umma_bf16_desc(tmem + kOCol + u * 2 * RU, operand_desc_mn(v0 + (uint32_t)kk * 2 * kOctet, 1024, kOctet),
+                           operand_desc_mn(p0 + (uint32_t)(u * PU + kk * 2048), 128 * kTok, 1024), kIdescO, (kk > 0 || !pend_first) ? 1u : 0u);
+          if (u == NU - 1) umma_commit(&ctl->v_empty[s]);
+          umma_commit(&ctl->p_done[u]);
+        }
         return true;
       };
       for (unsigned gi = 0; ok; ++gi) {
@@ -463,27 +476,30 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   } else {
     // ================================================================ softmax and epilogue: a thread per token
     asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
-    const int half = warp >> 2, quarter = warp & 3;         // column half; tensor-memory lane quarter
+    const int grp = warp >> 2, quarter = warp & 3;          // column group; tensor-memory lane quarter
     const int tk = quarter * 32 + lane;                     // token of the step; in the epilogue, dimension of the output
-    const int c0 = half * NC;                               // first column
-    constexpr int LC = NC > 32 ? 2 : 1, W = NC / LC;        // columns whose bookkeeping a lane carries; run of columns in registers
+    const int c0 = grp * NC;                                // first column
+    const int unit = NU == 2 ? grp : 0, u0 = c0 - unit * RU; // unit of columns, first column in it
+    const uint32_t o_cols = kOCol + unit * 2 * RU + u0;      // accumulator of the first column (heads; remainders RU further)
+    const int my_c = c0 + lane % LW;                         // the column(s) whose bookkeeping this lane carries: my_c + k LW
+    const bool keeper = lane < LW;
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
     const float scale_log2 = dv.scale_log2;
     const uint64_t scale2 = f2_pack(scale_log2, scale_log2);
     const int rows = n_nodes * G, row0 = tile * R;
     unsigned g = 0, n_agree = 0, n_all = 0, n_top = 0;
+    int mask_b = -1;              // the sequence whose tree the next three belong to
+    uint32_t vis[LC] = {}, live[LC] = {};   // columns that see this thread's draft; columns that are a node of the tree
+    float my_depth = 0.f;         // this thread's draft's
     bool ok = true;
-    auto group_sync = [&]() -> bool {   // the four warps of this column half
-      warp_arrive(&ctl->agree[half], lane);
-      return warp_wait(&ctl->agree[half], n_agree++ & 1, abort_flag);
+    auto group_sync = [&]() -> bool {   // the four warps of this column group
+      warp_arrive(&ctl->agree[grp], lane);
+      return warp_wait(&ctl->agree[grp], n_agree++ & 1, abort_flag);
     };
     auto all_sync = [&]() -> bool {
       warp_arrive(&ctl->all_sync, lane);
       return warp_wait(&ctl->all_sync, n_all++ & 1, abort_flag);
     };
-    // bookkeeping of column c (0 <= c < NC) sits in lane c % 32 (NC = 16: in lanes c and c + 16)
-    auto pick = [&](const float (&x)[LC], int c) { return __shfl_sync(0xffffffffu, x[LC == 2 ? c >> 5 : 0], c & 31); };
-
     for (unsigned gi = 0; ok; ++gi) {
       const int slot = gi % kItemSlots;
       ok = warp_wait(&ctl->item_full[slot], (gi / kItemSlots) & 1, abort_flag);
@@ -495,53 +511,53 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
       const int b = it.head / dv.n_kv_heads, g_kv = it.head % dv.n_kv_heads;
       const int total = it.st.len + it.st.n_drop;
       const int32_t* parent = tc.parent + (size_t)b * n_nodes;
-      // node and query head of this lane's columns, and where the row stands in the output (from the item's first row on)
-      int node[LC], place[LC];
+      // this lane's columns: their nodes, and where their rows stand in the output (from the KV head's first row on)
+      int my_node[LC], place[LC];
 #pragma unroll
       for (int k = 0; k < LC; ++k) {
-        const int r = min(row0 + c0 + (NC < 32 ? lane % NC : lane + 32 * k), rows - 1);
-        node[k] = r >> lg;
-        place[k] = ((r >> lg) * dv.n_kv_heads * G + (r & (G - 1))) * D;
+        const int r = min(row0 + my_c + k * LW, rows - 1);
+        my_node[k] = r >> lg;
+        place[k] = (my_node[k] * dv.n_kv_heads * G + (r & (G - 1))) * D;
       }
 
       // ---- the tree (items that hold its tokens; with ALiBi, all: a row's position is its node's depth)
-      uint32_t vis[LC] = {}, live[LC] = {};   // columns that see this thread's draft; columns that are a node of the tree
-      float my_depth = 0.f;
-      if (it.draft || kAlibi) {
+      // (the heads of a sequence follow one another: its tree is worked out once)
+      if ((it.draft || kAlibi) && b != mask_b) {
+        mask_b = b;
         TreeMask* mask = (TreeMask*)p_tile;   // (no weights are in there between items)
         static_assert(sizeof(TreeMask) <= (size_t)Smem::kP, "scratch");
-        tree_mask_load(*mask, parent, n_nodes, tid, kSoftWarps * 32);
-        if (tid < kTreeMaxNodes / 32) ctl->bad_v[tid] = 0;
+        tree_mask_load(*mask, parent, n_nodes, tid, SW * 32);
         if (!(ok = all_sync())) break;
-        tree_mask_walk(*mask, n_nodes, tid, kSoftWarps * 32);
+        tree_mask_walk(*mask, n_nodes, tid, SW * 32);
         if (!(ok = all_sync())) break;
 #pragma unroll
         for (int k = 0; k < LC; ++k) {
-          live[k] = __ballot_sync(0xffffffffu, lane + 32 * k < NC && row0 + c0 + lane + 32 * k < rows && tree_sees(*mask, node[k], node[k]));
-#pragma unroll 4
-          for (int c = 0; c < W; ++c) {   // (tokens are nodes here: this warp's are bits of one word)
-            const int t = __shfl_sync(0xffffffffu, node[k], c);
+          live[k] = __ballot_sync(0xffffffffu, keeper && row0 + my_c + k * LW < rows && tree_sees(*mask, my_node[k], my_node[k]));
+          vis[k] = 0;
+#pragma unroll 8
+          for (int c = 0; c < LW; ++c) {   // (tokens are nodes here: this warp's are bits of one word)
+            const int t = __shfl_sync(0xffffffffu, my_node[k], c);
             vis[k] |= (mask->see[t][quarter] >> lane & live[k] >> c & 1u) << c;
           }
         }
         if constexpr (kAlibi) {
           my_depth = (float)mask->depth[min(tk, n_nodes - 1)];
-          if (quarter == 0) {
 #pragma unroll
-            for (int i = 0; i < LC; ++i) {
-              const int c = lane + 32 * i;
-              if (c < NC) {
-                ctl->depth[c0 + c] = (float)mask->depth[node[i]];
-                ctl->slope[c0 + c] = dv.alibi_slopes[((size_t)layer * dv.n_kv_heads + g_kv) * G + (min(row0 + c0 + c, rows - 1) & (G - 1))];
-              }
-            }
-          }
+          for (int k = 0; k < LC; ++k)
+            if (quarter == 0 && keeper) ctl->depth[my_c + k * LW] = (float)mask->depth[my_node[k]];
         }
         if (!(ok = all_sync())) break;
       }
+      if constexpr (kAlibi) {
+#pragma unroll
+        for (int k = 0; k < LC; ++k)
+          if (quarter == 0 && keeper)
+            ctl->slope[my_c + k * LW] = dv.alibi_slopes[((size_t)layer * dv.n_kv_heads + g_kv) * G + (min(row0 + my_c + k * LW, rows - 1) & (G - 1))];
+      }
+      if (tid < kTreeMaxNodes / 32) ctl->bad_v[(gi + 1) & 1][tid] = 0;   // (last read before the barrier that ended the item before, next written behind this item's)
+      uint32_t* bad_v = ctl->bad_v[gi & 1];
       // ---- reference maxima: minus infinity, or the compensation token's logit (Eq. 5: weight N_d exp(s_c), value v_hat),
       // whose weight is carried apart and added at the end
-      float m_lane[LC], w_seed[LC];
       if (it.seed) {
         const float* k_hat = dv.comp_mean + hs * 2 * D;
         const float count_log2 = log2f((float)it.st.n_drop);
@@ -549,23 +565,28 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         float kh[EPL];
 #pragma unroll
         for (int e = 0; e < EPL; ++e) kh[e] = k_hat[lane * EPL + e];
-        for (int c = quarter; c < NC; c += 4) {
-          const int r = min(row0 + c0 + c, rows - 1), t = r >> lg, j = r & (G - 1);
-          const __nv_bfloat16* src = (const __nv_bfloat16*)tc.q + (size_t)b * tc.q_stride_b + (size_t)t * tc.q_stride_t + ((size_t)g_kv * G + j) * D + lane * EPL;
+#pragma unroll 4
+        for (int k = 0; k < NC / 4; ++k) {
+          const int c = c0 + quarter * (NC / 4) + k, r = min(row0 + c, rows - 1);
+          const __nv_bfloat16* src = (const __nv_bfloat16*)tc.q + (size_t)b * tc.q_stride_b + (size_t)(r >> lg) * tc.q_stride_t + ((size_t)g_kv * G + (r & (G - 1))) * D + lane * EPL;
+          uint32_t x[EPL / 2];
+#pragma unroll
+          for (int e = 0; e < EPL / 2; ++e) x[e] = __ldg((const uint32_t*)src + e);
           float s = 0.f;
 #pragma unroll
-          for (int e = 0; e < EPL; ++e) s = fmaf(__bfloat162float(src[e]), kh[e], s);
+          for (int e = 0; e < EPL; ++e) s = fmaf(__uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16), kh[e], s);
           s = row_sum<32>(s);
-          if (lane == 0) ctl->neg_m[c0 + c] = -fmaf(s, scale_log2, count_log2);
+          if (lane == 0) ctl->neg_m[c] = -fmaf(s, scale_log2, count_log2);
         }
       } else {
-        for (int c = tk; c < NC; c += kTok) ctl->neg_m[c0 + c] = -kLow;
+        if (tk < NC) ctl->neg_m[c0 + tk] = -kLow;
       }
       if (!(ok = group_sync())) break;
+      float m_lane[LC], w_seed[LC];
 #pragma unroll
-      for (int i = 0; i < LC; ++i) {
-        m_lane[i] = it.seed ? -ctl->neg_m[c0 + (NC < 32 ? lane % NC : lane + 32 * i)] : -CUDART_INF_F;
-        w_seed[i] = it.seed ? 1.f : 0.f;
+      for (int k = 0; k < LC; ++k) {
+        m_lane[k] = it.seed ? -ctl->neg_m[my_c + k * LW] : -CUDART_INF_F;
+        w_seed[k] = it.seed ? 1.f : 0.f;
       }
       // Sums of the weights of this thread's tokens, and this thread's dimension of the rows' outputs: the accumulator in
       // tensor memory is added on every kFlush steps.  (The matrix unit truncates when it adds to the accumulator; over
@@ -585,13 +606,13 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
 #pragma unroll kUnroll
         for (int c = 0; c < NC; c += 16) {
           uint32_t oh[16], ol[16];
-          tmem_load<16>(lane_addr + kOCol + (uint32_t)(c0 + c), oh);
-          tmem_load<16>(lane_addr + kOCol + (uint32_t)(R + c0 + c), ol);
+          tmem_load<16>(lane_addr + o_cols + (uint32_t)c, oh);
+          tmem_load<16>(lane_addr + o_cols + (uint32_t)(RU + c), ol);
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[c + e] += __uint_as_float(oh[e]) + __uint_as_float(ol[e]);
         }
         tc_fence_before();
-        warp_arrive(&ctl->o_read, lane);
+        warp_arrive(&ctl->o_read[unit], lane);
       };
 
       const int n = it.end - it.begin + it.draft;
@@ -605,20 +626,19 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
         ok = warp_wait(&ctl->s_full[g & 1], (g / 2) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
-        uint32_t v[W];
-        // scores of a run of W columns to the log2 domain, minus the reference; returns whether one outran it
-        auto scores = [&](const int run) -> bool {
-          const int cr = c0 + run * W;
-          tmem_load<W>(lane_addr + (g & 1) * R + cr, v);
+        uint32_t v[NC];
+        // scores to the log2 domain, minus the reference; returns whether one outran it
+        auto scores = [&]() -> bool {
+          tmem_load<NC>(lane_addr + (g & 1) * R + c0, v);
           float mx = -CUDART_INF_F;
 #pragma unroll
-          for (int c = 0; c < W; c += 4) {
-            const float4 nm = *(const float4*)&ctl->neg_m[cr + c];
+          for (int c = 0; c < NC; c += 4) {
+            const float4 nm = *(const float4*)&ctl->neg_m[c0 + c];
             float t[4];
             f2_unpack(f2_fma(f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), scale2, f2_pack(nm.x, nm.y)), t[0], t[1]);
             f2_unpack(f2_fma(f2_pack(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), scale2, f2_pack(nm.z, nm.w)), t[2], t[3]);
             if constexpr (kAlibi) {
-              const float4 sl = *(const float4*)&ctl->slope[cr + c], de = *(const float4*)&ctl->depth[cr + c];
+              const float4 sl = *(const float4*)&ctl->slope[c0 + c], de = *(const float4*)&ctl->depth[c0 + c];
               t[0] = fmaf(sl.x, rel - de.x, t[0]);
               t[1] = fmaf(sl.y, rel - de.y, t[1]);
               t[2] = fmaf(sl.z, rel - de.z, t[2]);
@@ -630,145 +650,138 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
           }
           if (draft) {
 #pragma unroll
-            for (int c = 0; c < W; ++c) {
-              if (!(vis[run] >> c & 1)) v[c] = 0xff800000u;
+            for (int c = 0; c < NC; ++c) {
+              if (!(vis[c / LW] >> (c % LW) & 1)) v[c] = 0xff800000u;
               mx = fmaxf(mx, __uint_as_float(v[c]));
             }
           } else if (!valid) {
             mx = -CUDART_INF_F;
 #pragma unroll
-            for (int c = 0; c < W; ++c) v[c] = 0xff800000u;
+            for (int c = 0; c < NC; ++c) v[c] = 0xff800000u;
           }
           return mx > kLag;
         };
         auto weights = [&]() {
 #pragma unroll
-          for (int c = 0; c < W; ++c) v[c] = __float_as_uint(fast_exp2(__uint_as_float(v[c])));
+          for (int c = 0; c < NC; ++c) v[c] = __float_as_uint(fast_exp2(__uint_as_float(v[c])));
         };
-        // (with two runs of columns the second stays in registers and the first is computed again: fewer registers)
-        bool outran = false;
-#pragma unroll
-        for (int run = 0; run < LC; ++run) outran |= scores(run);
-        if (__any_sync(0xffffffffu, outran) && lane == 0) *(volatile uint32_t*)&ctl->need[half][g & 1] = g + 1;
-        warp_arrive(&ctl->agree[half], lane);
+        const bool outran = scores();
+        if (__any_sync(0xffffffffu, outran) && lane == 0) *(volatile uint32_t*)&ctl->need[grp][g & 1] = g + 1;
+        warp_arrive(&ctl->agree[grp], lane);
         weights();
-        ok = warp_wait(&ctl->agree[half], n_agree++ & 1, abort_flag);
+        ok = warp_wait(&ctl->agree[grp], n_agree++ & 1, abort_flag);
         if (!ok) break;
         bool flush_now = i > 0 && i % kFlush == 0;
-        const bool move = *(volatile uint32_t*)&ctl->need[half][g & 1] == g + 1;
-        if (move) {
+        if (*(volatile uint32_t*)&ctl->need[grp][g & 1] == g + 1) {
           // ---- move the references that were outrun to the maximum of what has been seen
           if (g > 0) {
-            ok = warp_wait(&ctl->p_done, (g - 1) & 1, abort_flag);
+            ok = warp_wait(&ctl->p_done[unit], (g - 1) & 1, abort_flag);
             if (!ok) break;
           }
           if (flush_now) flush();
           flush_now = false;
           int32_t* top = ctl->top[n_top & 1];
-#pragma unroll 1
-          for (int c = 0; c < NC; c += 16) {
-            uint32_t s[16];
-            tmem_load<16>(lane_addr + (g & 1) * R + c0 + c, s);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float t = __uint_as_float(s[e]) * scale_log2;
-              if constexpr (kAlibi) t = fmaf(ctl->slope[c0 + c + e], rel - ctl->depth[c0 + c + e], t);
-              if (draft ? !(vis[LC == 2 ? c >> 5 : 0] >> ((c + e) & 31) & 1) : !valid) t = -CUDART_INF_F;
-              t = warp_max(t);
-              if (lane == e) atomicMax(&top[c0 + c + e], ordered(t));
+          for (int k = 0; k < LC; ++k) {
+            uint32_t s[LW];
+            float t[LW];
+            tmem_load<LW>(lane_addr + (g & 1) * R + c0 + k * LW, s);
+#pragma unroll
+            for (int c = 0; c < LW; ++c) {
+              t[c] = __uint_as_float(s[c]) * scale_log2;
+              if constexpr (kAlibi) t[c] = fmaf(ctl->slope[c0 + k * LW + c], rel - ctl->depth[c0 + k * LW + c], t[c]);
+              if (draft ? !(vis[k] >> c & 1) : !valid) t[c] = -CUDART_INF_F;
             }
+            const float mx = across_warp<LW, true>(t, lane);
+            if (keeper) atomicMax(&top[my_c + k * LW], ordered(mx));
           }
           if (!(ok = group_sync())) break;
           float f[LC];
 #pragma unroll
           for (int k = 0; k < LC; ++k) {
-            const int c = NC < 32 ? lane % NC : lane + 32 * k;
             // (a row moves only when it has been outrun itself: what it computes does not depend on the rows beside it)
-            const float seen = from_ordered(top[c0 + c]);
+            const float seen = from_ordered(top[my_c + k * LW]);
             const float m_new = m_lane[k] == -CUDART_INF_F || seen > m_lane[k] + kLag ? fmaxf(m_lane[k], seen) : m_lane[k];
             f[k] = m_lane[k] == -CUDART_INF_F ? 0.f : fast_exp2(m_lane[k] - m_new);
             m_lane[k] = m_new;
             w_seed[k] *= f[k];
-            if (quarter == 0 && lane + 32 * k < NC) {
-              ctl->neg_m[c0 + c] = m_new == -CUDART_INF_F ? -kLow : -m_new;
-              ctl->top[(n_top + 1) & 1][c0 + c] = ordered(-CUDART_INF_F);   // (its last readers are two moves back)
+            if (quarter == 0 && keeper) {
+              ctl->neg_m[my_c + k * LW] = m_new == -CUDART_INF_F ? -kLow : -m_new;
+              ctl->top[(n_top + 1) & 1][my_c + k * LW] = ordered(-CUDART_INF_F);   // (its last readers are two moves back)
             }
           }
           n_top += 1;
           if (!(ok = group_sync())) break;
+          if (i > 0) {   // (an item's first step finds nothing to rescale)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) l[c] *= pick(f, c);
-          tc_fence_after();
+            for (int c = 0; c < NC; ++c) l[c] *= __shfl_sync(0xffffffffu, f[c / LW], c % LW);
+            tc_fence_after();
 #pragma unroll kUnroll
-          for (int c = 0; c < NC; c += 16) {
-            float fc[16];
+            for (int c = 0; c < NC; c += 16) {
+              const float f16 = LC == 2 && c >= 32 ? f[LC - 1] : f[0];
+              float fc[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              fc[e] = __shfl_sync(0xffffffffu, LC == 2 && c >= 32 ? f[LC - 1] : f[0], (c + e) & 31);
-              acc[c + e] *= fc[e];
-            }
-            if (i % kFlush != 0) {   // the accumulator holds products of this item
+              for (int e = 0; e < 16; ++e) {
+                fc[e] = __shfl_sync(0xffffffffu, f16, (c + e) % LW);
+                acc[c + e] *= fc[e];
+              }
+              if (i % kFlush != 0) {   // the accumulator holds products of this item
 #pragma unroll
-              for (int part = 0; part < 2; ++part) {
-                const uint32_t addr = lane_addr + kOCol + (uint32_t)(part * R + c0 + c);
-                uint32_t o[16];
-                tmem_load<16>(addr, o);
+                for (int part = 0; part < 2; ++part) {
+                  const uint32_t addr = lane_addr + o_cols + (uint32_t)(part * RU + c);
+                  uint32_t o[16];
+                  tmem_load<16>(addr, o);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fc[e]);
-                tmem_st16(addr, o);
+                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * fc[e]);
+                  tmem_st16(addr, o);
+                }
               }
             }
+            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
           }
-          asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+          (void)scores();
+          weights();
         } else if (g > 0) {   // the product of the step before must have read its weights
-          ok = warp_wait(&ctl->p_done, (g - 1) & 1, abort_flag);
+          ok = warp_wait(&ctl->p_done[unit], (g - 1) & 1, abort_flag);
           if (!ok) break;
         }
+        // S is read out
+        tc_fence_before();
+        warp_arrive(&ctl->s_empty[g & 1], lane);
         if (flush_now) flush();
-        uint8_t* p_row = p_tile + tk * 128;
+        // ---- sums; a weight is written as a bf16 head (its upper 16 bits) plus a bf16 remainder
+        uint8_t* p_row = p_tile + unit * PU + tk * 128;
 #pragma unroll
-        for (int run = LC - 1; run >= 0; --run) {
-          if (move || run < LC - 1) {
-            (void)scores(run);
-            weights();
+        for (int c = 0; c < NC; c += 8) {
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int e = c + 2 * k;
+            const uint32_t b0 = v[e], b1 = v[e + 1];
+            const uint64_t w2 = f2_pack(__uint_as_float(b0), __uint_as_float(b1));
+            f2_unpack(f2_add(f2_pack(l[e], l[e + 1]), w2), l[e], l[e + 1]);
+            hi[k] = __byte_perm(b0, b1, 0x7632);
+            float r0, r1;
+            f2_unpack(f2_sub(w2, f2_pack(__uint_as_float(b0 & 0xffff0000u), __uint_as_float(b1 & 0xffff0000u))), r0, r1);
+            const __nv_bfloat162 r = __floats2bfloat162_rn(r0, r1);
+            lo[k] = *(const uint32_t*)&r;
           }
-          if (run == 0) {   // S is read out
-            tc_fence_before();
-            warp_arrive(&ctl->s_empty[g & 1], lane);
-          }
-#pragma unroll
-          for (int c = 0; c < W; c += 2)
-            f2_unpack(f2_add(f2_pack(l[run * W + c], l[run * W + c + 1]), f2_pack(__uint_as_float(v[c]), __uint_as_float(v[c + 1]))),
-                      l[run * W + c], l[run * W + c + 1]);
-          // ---- a weight is written as a bf16 head (its upper 16 bits) plus a bf16 remainder
-#pragma unroll
-          for (int c = 0; c < W; c += 8) {
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t b0 = v[c + 2 * k], b1 = v[c + 2 * k + 1];
-              hi[k] = __byte_perm(b0, b1, 0x7632);
-              float r0, r1;
-              f2_unpack(f2_sub(f2_pack(__uint_as_float(b0), __uint_as_float(b1)),
-                               f2_pack(__uint_as_float(b0 & 0xffff0000u), __uint_as_float(b1 & 0xffff0000u))), r0, r1);
-              const __nv_bfloat162 r = __floats2bfloat162_rn(r0, r1);
-              lo[k] = *(const uint32_t*)&r;
-            }
-            const int ch = c0 + run * W + c, cl = R + ch;   // columns of heads and remainders in the 2R-column operand
-            *(uint4*)(p_row + (ch >> 6) * (128 * kTok) + ((((ch & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *(uint4*)(p_row + (cl >> 6) * (128 * kTok) + ((((cl & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          }
+          const int ch = u0 + c, cl = RU + ch;   // columns of heads and remainders in the unit's operand
+          *(uint4*)(p_row + (ch >> 6) * (128 * kTok) + ((((ch & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *(uint4*)(p_row + (cl >> 6) * (128 * kTok) + ((((cl & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
         // ---- V rows that no weight may meet: a zero weight times a NaN is a NaN.  Behind the head's last token the pool
         // may hold anything; a draft is hidden from the nodes of other branches.
         const int sv = g % NV;
+        bool fixed = draft;
         if (draft) {
           ok = warp_wait(&ctl->v_full[sv], (g / NV) & 1, abort_flag);
           if (!ok) break;
           if (tk < n_nodes) {
+            constexpr int kChunks = D / 8 / kGroups;
             bool bad = false;
 #pragma unroll 4
-            for (int c = half * (D / 16); c < (half + 1) * (D / 16); ++c) {   // 16-byte chunks, this half of the row
+            for (int c = grp * kChunks; c < (grp + 1) * kChunks; ++c) {   // 16-byte chunks: this group's share of the row
               uint4* at = (uint4*)(v_ring + sv * KV + (tk >> 3) * kOctet + (c >> 3) * 1024 + (tk & 7) * 128 + (((c & 7) ^ (tk & 7)) << 4));
               uint4 x = *at;
               uint32_t* w = (uint32_t*)&x;
@@ -781,76 +794,78 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
               if (hit) *at = x;
               bad |= hit;
             }
-            if (bad) atomicOr(&ctl->bad_v[tk >> 5], 1u << (tk & 31));
+            if (bad) atomicOr(&bad_v[tk >> 5], 1u << (tk & 31));
           }
         } else if (slot0 + kTok > it.st.len) {
           ok = warp_wait(&ctl->v_full[sv], (g / NV) & 1, abort_flag);
           if (!ok) break;
+          fixed = true;
           const int first = it.st.len - slot0, last = (first + 15) / 16 * 16;
-          for (int idx = tid; idx < (last - first) * (D / 8); idx += kSoftWarps * 32) {
+          for (int idx = tid; idx < (last - first) * (D / 8); idx += SW * 32) {
             const int t = first + idx / (D / 8), c = idx % (D / 8);
             *(uint4*)(v_ring + sv * KV + (t >> 3) * kOctet + (c >> 3) * 1024 + (t & 7) * 128 + ((c & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if (NU > 1 && fixed && !(ok = all_sync())) break;   // (a unit's product reads rows that the other group has put right)
         tc_fence_before();
-        warp_arrive(&ctl->p_full, lane);
+        warp_arrive(&ctl->p_full[unit], lane);
       }
       if (!ok) break;
       // ---- the rows' results
-      ok = warp_wait(&ctl->p_done, (g - 1) & 1, abort_flag);
+      ok = warp_wait(&ctl->p_done[unit], (g - 1) & 1, abort_flag);
       if (!ok) break;
       flush();
-      float* l_part = (float*)(p_tile + 8192) + half * 4 * NC;   // [quarter][NC]
-      static_assert(8192 + 8 * NC * 4 <= Smem::kP, "scratch");
-      float l_lane[LC];
+      float* l_part = (float*)(p_tile + 8192) + grp * 4 * NC;   // [quarter][NC]
+      static_assert(8192 + 16 * R <= Smem::kP, "scratch");
 #pragma unroll
       for (int k = 0; k < LC; ++k) {
-        const float x = column_sum<W>(l + 32 * k, lane);
-        if (lane + 32 * k < NC) l_part[quarter * NC + lane + 32 * k] = x;
+        const float x = across_warp<LW, false>(l + k * LW, lane);
+        if (keeper) l_part[quarter * NC + lane + k * LW] = x;
       }
       if (!(ok = group_sync())) break;
       const bool direct = it.rec < 0;
-      float inv[LC];
+      // what a column's results need, for every lane to read: factor, the compensation token's share, place, liveness
+      float4* table = (float4*)(p_tile + 10240 + warp * NC * 16);
+      static_assert(10240 + SW * NC * 16 <= Smem::kP, "scratch");
 #pragma unroll
       for (int k = 0; k < LC; ++k) {
-        const int c = NC < 32 ? lane % NC : lane + 32 * k;
-        l_lane[k] = ((l_part[c] + l_part[NC + c]) + (l_part[2 * NC + c] + l_part[3 * NC + c])) + w_seed[k];
-        inv[k] = direct ? 1.f / l_lane[k] : 1.f;
-        if (!direct && quarter == 0 && lane + 32 * k < NC)   // (a negative sum marks an absent node's row for the combine kernel)
-          dv.rec_ml[(size_t)it.rec * R + c0 + c] = make_float2(m_lane[k], it.draft && !(live[k] >> (c & 31) & 1) ? -1.f : l_lane[k]);
+        if (!keeper) continue;
+        const int c = lane + k * LW;
+        const float* lp = l_part + c;
+        const float l_all = ((lp[0] + lp[NC]) + (lp[2 * NC] + lp[3 * NC])) + w_seed[k];
+        const float inv = direct ? 1.f / l_all : 1.f;
+        const bool is_node = (live[k] >> lane & 1) != 0;
+        table[c] = make_float4(inv, w_seed[k] * inv, __int_as_float(direct ? place[k] : c * D), __int_as_float(row0 + c0 + c < rows && (!direct || is_node)));
+        if (!direct && quarter == 0)   // (a negative sum marks an absent node's row for the combine kernel)
+          dv.rec_ml[(size_t)it.rec * R + c0 + c] = make_float2(m_lane[k], it.draft && !is_node ? -1.f : l_all);
       }
-      const bool poisoned = it.draft && (ctl->bad_v[0] | ctl->bad_v[1] | ctl->bad_v[2] | ctl->bad_v[3]) != 0;
-      // The NaN and infinities that were taken out of the drafts' V reach the rows that see them.
-      auto add_poison = [&](float x, int r) -> float {
-#pragma unroll 1
-        for (int nd = 0; nd <= r >> lg; ++nd) {
-          if (!(ctl->bad_v[nd >> 5] >> (nd & 31) & 1) || !walk_sees(parent, r >> lg, nd)) continue;
-          const float bad = __bfloat162float(((const __nv_bfloat16*)tc.v)[(size_t)b * tc.kv_stride_b + (size_t)nd * tc.kv_stride_t + (size_t)g_kv * D + tk]);
-          if (!(fabsf(bad) < CUDART_INF_F)) x += bad;
-        }
-        return x;
-      };
+      __syncwarp();
       if (quarter * 32 < D) {
         const float v_hat = it.seed ? dv.comp_mean[hs * 2 * D + D + tk] : 0.f;
         float* dst = direct ? tc.out + ((size_t)b * n_nodes * dv.n_kv_heads + g_kv) * G * D + tk : dv.rec_o + ((size_t)it.rec * R + c0) * D + tk;
         const int n_cols = min(NC, rows - (row0 + c0));   // (rows behind the last are nobody's)
 #pragma unroll kUnroll
         for (int cb = 0; cb < NC; cb += 16) {
-          const bool up = LC == 2 && cb >= 32;
-          const float w16 = up ? w_seed[LC - 1] : w_seed[0], i16 = up ? inv[LC - 1] : inv[0];
-          const int p16 = up ? place[LC - 1] : place[0];
-          const uint32_t live16 = up ? live[LC - 1] : live[0];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int c = cb + e;
-            float x = fmaf(__shfl_sync(0xffffffffu, w16, c & 31), v_hat, acc[c]);
-            const float iv = __shfl_sync(0xffffffffu, i16, c & 31);
-            const int at = __shfl_sync(0xffffffffu, p16, c & 31);
-            if (c >= n_cols) continue;
-            if (poisoned) x = add_poison(x, row0 + c0 + c);
-            if (!direct) dst[c * D] = x;
-            else if (live16 >> (c & 31) & 1) dst[at] = x * iv;
+            const float4 w = table[cb + e];
+            if (__float_as_int(w.w)) dst[__float_as_int(w.z)] = fmaf(w.y, v_hat, w.x * acc[cb + e]);
+          }
+        }
+        // The NaN and infinities that were taken out of the drafts' V reach the rows that see them.
+        if (it.draft && (bad_v[0] | bad_v[1] | bad_v[2] | bad_v[3]) != 0) {
+#pragma unroll 1
+          for (int c = 0; c < n_cols; ++c) {
+            const int t = (row0 + c0 + c) >> lg;
+            float bad = 0.f;
+#pragma unroll 1
+            for (int nd = 0; nd <= t; ++nd) {
+              if (!(bad_v[nd >> 5] >> (nd & 31) & 1) || !walk_sees(parent, t, nd)) continue;
+              const float y = __bfloat162float(((const __nv_bfloat16*)tc.v)[(size_t)b * tc.kv_stride_b + (size_t)nd * tc.kv_stride_t + (size_t)g_kv * D + tk]);
+              if (!(fabsf(y) < CUDART_INF_F)) bad += y;
+            }
+            if (bad != 0.f && __float_as_int(table[c].w)) dst[__float_as_int(table[c].z)] += bad;   // (this thread's own store)
           }
         }
       }
@@ -860,7 +875,7 @@ __global__ void __launch_bounds__(kMmaThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kSoftWarps + 1) {
+  if (warp == SW + 1) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   }
@@ -952,7 +967,7 @@ cudaError_t mma_launch(const DeviceView& dv, long long pool_pages, int layer, co
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) opted_in[dev] = true;
   }
-  tree_mma_kernel<D, R, kAlibi><<<tc.n_spans * tc.n_tiles, kMmaThreads, kBytes, s>>>(dv, pool, q, k, v, layer, tc);
+  tree_mma_kernel<D, R, kAlibi><<<tc.n_spans * tc.n_tiles, kTreeThreads, kBytes, s>>>(dv, pool, q, k, v, layer, tc);
   e = cudaGetLastError();
   if (e != cudaSuccess || tc.n_spans == 1) return e;
   cudaLaunchConfig_t cfg = {};
