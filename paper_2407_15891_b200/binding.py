@@ -222,6 +222,27 @@ def razor_decode_attention_multi(cache: int, layer: int, q, out, n_tokens: int, 
 
 
 TREE_MAX_NODES = 128
+_VERIFY_DTYPES = {torch.float32: RAZOR_F32, torch.bfloat16: RAZOR_BF16}
+
+
+class _on:
+    """The given CUDA device as the current one: streams and launches follow the tensors, not the caller's device."""
+    __slots__ = ("index", "before")
+
+    def __init__(self, device: torch.device):
+        self.index = device.index
+
+    def __enter__(self):
+        self.before = None
+        if self.index is not None:
+            before = torch.cuda.current_device()
+            if before != self.index:
+                self.before = before
+                torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.before is not None:
+            torch.cuda.set_device(self.before)
 
 
 def razor_decode_attention_tree(cache: int, layer: int, q, q_stride_b: int, q_stride_t: int, k_draft, v_draft,
@@ -244,23 +265,27 @@ def razor_verify_tree(target: torch.Tensor, draft: Optional[torch.Tensor], token
     tokens, parent int32 and u_accept fp32 [B, n_nodes], u_sample fp32 [B], contiguous.
     -> dict(accepted int32 [B], path int32 [B, n_nodes] (-1 behind the accepted nodes), token int32 [B])."""
     B, T = tokens.shape
-    V = target.shape[2]
-    dt = {torch.float32: RAZOR_F32, torch.bfloat16: RAZOR_BF16}[target.dtype]
-    assert target.shape[0] == B and target.shape[1] >= T + 1 and (V == 1 or target.stride(2) == 1)
+    shape, dev, dtype = target.shape, target.device, target.dtype
+    V = shape[2]
+    dt = _VERIFY_DTYPES[dtype]
+    assert shape[0] == B and shape[1] > T and (V == 1 or target.stride(2) == 1)
     # (the rows of a tree's leaves are not read: a chain's draft rows may be T of them)
-    assert draft is None or (draft.dtype == target.dtype and draft.shape[0] == B and draft.shape[1] >= T
-                             and draft.shape[2] == V and (V == 1 or draft.stride(2) == 1))
-    for x, shape, dtype in ((tokens, (B, T), torch.int32), (parent, (B, T), torch.int32),
-                            (u_accept, (B, T), torch.float32), (u_sample, (B,), torch.float32)):
-        assert x.shape == shape and x.dtype == dtype and x.is_contiguous()
-    assert all(x is None or x.device == target.device for x in (draft, tokens, parent, u_accept, u_sample))
-    res = torch.empty((B, T + 2), dtype=torch.int32, device=target.device)   # one allocation for the three results
-    flat = res.view(-1)
-    accepted, token, path = flat[:B], flat[B:2 * B], flat[2 * B:].view(B, T)
-    d_strides = (draft.stride(0), draft.stride(1)) if draft is not None else (0, 0)
-    _check(load().razor_verify_tree(_ptr(target), target.stride(0), target.stride(1), _ptr(draft), *d_strides, dt,
-                                    _ptr(tokens), _ptr(parent), _ptr(u_accept), _ptr(u_sample), B, T, V, _ptr(accepted),
-                                    _ptr(path), _ptr(token), _stream(stream)), "razor_verify_tree")
+    assert draft is None or (draft.dtype is dtype and draft.shape[0] == B and draft.shape[1] >= T and draft.shape[2] == V
+                             and (V == 1 or draft.stride(2) == 1) and draft.device == dev)
+    assert tokens.dtype is torch.int32 and parent.dtype is torch.int32 and parent.shape == tokens.shape
+    assert u_accept.dtype is torch.float32 and u_sample.dtype is torch.float32
+    assert u_accept.shape == tokens.shape and u_sample.shape == (B,)
+    assert tokens.is_contiguous() and parent.is_contiguous() and u_accept.is_contiguous() and u_sample.is_contiguous()
+    assert tokens.device == dev and parent.device == dev and u_accept.device == dev and u_sample.device == dev
+    accepted = torch.empty((B,), dtype=torch.int32, device=dev)
+    path = torch.empty((B, T), dtype=torch.int32, device=dev)
+    token = torch.empty((B,), dtype=torch.int32, device=dev)
+    with _on(dev):
+        q_ptr, q_b, q_row = (draft.data_ptr(), draft.stride(0), draft.stride(1)) if draft is not None else (None, 0, 0)
+        _check(load().razor_verify_tree(target.data_ptr(), target.stride(0), target.stride(1), q_ptr, q_b, q_row, dt,
+                                        tokens.data_ptr(), parent.data_ptr(), u_accept.data_ptr(), u_sample.data_ptr(),
+                                        B, T, V, accepted.data_ptr(), path.data_ptr(), token.data_ptr(),
+                                        _stream(stream)), "razor_verify_tree")
     return dict(accepted=accepted, path=path, token=token)
 
 
@@ -468,36 +493,40 @@ class RazorCache:
                     parent: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """q [B, T, Hq, D], k_draft, v_draft [B, T, Hkv, D] (strided over b and t), parent int32 [B, T] -> out fp32
         [B, T, Hq, D].  Rows of absent nodes are left as they are (zeros when `out` is not given)."""
-        self._check_draft(k_draft, v_draft)
-        T = k_draft.shape[1]
+        T, dev = self._check_draft(k_draft, v_draft)
         shape = (self.cfg.batch, T, self.cfg.n_q_heads, self.cfg.head_dim)
-        assert q.shape == shape and q.dtype == self.tdtype and self._heads_contiguous(q)
-        assert parent.shape == (self.cfg.batch, T) and parent.dtype == torch.int32 and parent.is_contiguous()
+        assert q.shape == shape and q.dtype is self.tdtype and q.device == dev and self._heads_contiguous(q)
+        assert parent.shape == shape[:2] and parent.dtype is torch.int32 and parent.is_contiguous() and parent.device == dev
         if out is None:
-            out = torch.zeros(shape, dtype=torch.float32, device=q.device)
-        assert out.shape == shape and out.dtype == torch.float32 and out.is_contiguous()
-        razor_decode_attention_tree(self.handle, layer, q, q.stride(0), q.stride(1), k_draft, v_draft,
-                                    k_draft.stride(0), k_draft.stride(1), parent, T, out)
+            out = torch.zeros(shape, dtype=torch.float32, device=dev)
+        assert out.shape == shape and out.dtype is torch.float32 and out.is_contiguous() and out.device == dev
+        with _on(dev):
+            razor_decode_attention_tree(self.handle, layer, q, q.stride(0), q.stride(1), k_draft, v_draft,
+                                        k_draft.stride(0), k_draft.stride(1), parent, T, out)
         return out
 
     def append_tree(self, layer: int, k_draft: torch.Tensor, v_draft: torch.Tensor, path: Optional[torch.Tensor],
                     n_accept) -> None:
         """Append the accepted path: rows path[b, :n_accept[b]] of k_draft, v_draft [B, T, Hkv, D].  path int32 [B, T]
         (or None: the first rows), n_accept [B] on the host."""
-        self._check_draft(k_draft, v_draft)
-        T = k_draft.shape[1]
-        assert path is None or (path.shape == (self.cfg.batch, T) and path.dtype == torch.int32 and path.is_contiguous())
+        T, dev = self._check_draft(k_draft, v_draft)
+        assert path is None or (path.shape == (self.cfg.batch, T) and path.dtype is torch.int32 and path.is_contiguous()
+                                and path.device == dev)
         assert len(n_accept) == self.cfg.batch
-        razor_append_tree(self.handle, layer, k_draft, v_draft, k_draft.stride(0), k_draft.stride(1), path, T, n_accept)
+        with _on(dev):
+            razor_append_tree(self.handle, layer, k_draft, v_draft, k_draft.stride(0), k_draft.stride(1), path, T, n_accept)
 
     @staticmethod
     def _heads_contiguous(x: torch.Tensor) -> bool:
-        return (x.shape[3] == 1 or x.stride(3) == 1) and (x.shape[2] == 1 or x.stride(2) == x.shape[3])
+        _, _, heads, dim = x.shape
+        return (dim == 1 or x.stride(3) == 1) and (heads == 1 or x.stride(2) == dim)
 
-    def _check_draft(self, k: torch.Tensor, v: torch.Tensor) -> None:
-        assert k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and self._heads_contiguous(k)
-        assert k.shape[0] == self.cfg.batch and k.shape[2:] == (self.cfg.n_kv_heads, self.cfg.head_dim)
-        assert k.dtype == self.tdtype and v.dtype == self.tdtype
+    def _check_draft(self, k: torch.Tensor, v: torch.Tensor):
+        cfg, dev, shape = self.cfg, self.pool.device, k.shape
+        assert len(shape) == 4 and shape == v.shape and k.stride() == v.stride() and self._heads_contiguous(k)
+        assert shape[0] == cfg.batch and shape[2] == cfg.n_kv_heads and shape[3] == cfg.head_dim
+        assert k.dtype is self.tdtype and v.dtype is self.tdtype and k.device == dev and v.device == dev
+        return shape[1], dev
 
     def export(self, layer: int, b: int, kv_head: int):
         """-> dict(kept_pos, K, V, mean_k, mean_v, sum_k, sum_v, n_drop) in logical order (device tensors)."""

@@ -800,7 +800,10 @@ int razor_verify_tree(const void* target, int64_t target_stride_b, int64_t targe
   vc.target_stride_b = target_stride_b; vc.target_stride_row = target_stride_row;
   vc.draft_stride_b = draft_stride_b; vc.draft_stride_row = draft_stride_row;
   vc.batch = batch; vc.n_nodes = n_nodes; vc.vocab = vocab;
-  RZ_CUDA(launch_verify(vc, dtype, (cudaStream_t)stream));
+  int dev = 0, sms = 0;
+  RZ_CUDA(cudaGetDevice(&dev));
+  RZ_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  RZ_CUDA(launch_verify(vc, dtype, sms, (cudaStream_t)stream));
   return RAZOR_OK;
 }
 

@@ -299,7 +299,7 @@ struct VerifyCall {
   int32_t batch, n_nodes, vocab;
   int32_t seg_len;         // set by the launcher
 };
-cudaError_t launch_verify(const VerifyCall& call, int dtype, cudaStream_t stream);
+cudaError_t launch_verify(const VerifyCall& call, int dtype, int n_sms, cudaStream_t stream);
 cudaError_t launch_wait_selftest(const DeviceView& dv, unsigned long long limit_ns, cudaStream_t stream);
 cudaError_t launch_export(const DeviceView& dv, int dtype, int layer, int head, int32_t* kept_pos, void* K, void* V,
                           float* mean_k, float* mean_v, float* sum_k, float* sum_v, cudaStream_t stream);

@@ -68,8 +68,8 @@ struct TreeCtl {
   uint64_t q_full, q_empty;
   uint64_t k_full[kMaxStages], k_empty[kMaxStages], v_full[kMaxStages], v_empty[kMaxStages];
   uint64_t s_full[2], s_empty[2];     // per S buffer
-  // per unit of columns: the weights are in shared memory; the product that read them has run; the accumulator has been read out
-  uint64_t p_full[2], p_done[2], o_read[2];
+  uint64_t p_full, p_done;            // the weights are in shared memory; the product that read them has run
+  uint64_t o_read;                    // the accumulator has been read out
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   uint64_t agree[kGroups];   // the four warps of a column group among themselves
   uint64_t all_sync;                  // the softmax warps among themselves
@@ -118,6 +118,20 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* v) {
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
       "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
       "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+// One matrix instruction with the operand descriptors given as (low word, high word).  The start address is in the low
+// word, in 16-byte units, so a walk along an operand is one 32-bit addition.
+__device__ __forceinline__ void umma_words(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                           uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "mov.b64 da, {%1, %2};\n\t"
+      "mov.b64 db, {%3, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %5, p;\n\t}"
+      :
+      : "r"(tmem_d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 // NC consecutive columns of this thread's lane, in registers when the function returns.
@@ -186,13 +200,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   constexpr int NC = R / kGroups;                       // columns of a softmax warp: 16, 32, 64
   constexpr int LC = NC > 32 ? 2 : 1, LW = NC / LC;     // columns whose bookkeeping a lane carries, LW apart
   constexpr uint32_t kOctet = 8 * D * 2;                // bytes of eight tokens in a stage: [octet][64-element half][8][128 B]
-  // A unit of columns has its own weights, accumulator and product.  With 128 rows each column group is a unit, so that one
-  // group's exponentials run beside the other's stores and products (V is read out of shared memory twice for it); with
-  // fewer rows there is one.
-  constexpr int NU = R == 128 ? 2 : 1, RU = R / NU, PU = Smem::kP / NU;
-  constexpr uint32_t kTmemCols = 4 * R, kOCol = 2 * R;  // S, S, then per unit O (heads), O (remainders)
+  constexpr uint32_t kTmemCols = 4 * R, kOCol = 2 * R;  // S, S, O (heads), O (remainders)
   constexpr uint32_t kIdescS = instr_desc_bf16(kTok, R, false);
-  constexpr uint32_t kIdescO = instr_desc_bf16(kTok, 2 * RU, true) | (1u << 15);   // (bit 15: A is MN-major too)
+  constexpr uint32_t kIdescO = instr_desc_bf16(kTok, 2 * R, true) | (1u << 15);   // (bit 15: A is MN-major too)
 
   extern __shared__ __align__(1024) uint8_t tree_smem[];
   uint8_t* k_ring = tree_smem;
@@ -223,11 +233,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       mbar_init(&ctl->agree[s], 4);
       ctl->need[s][0] = ctl->need[s][1] = 0;
     }
-    for (int u = 0; u < NU; ++u) {
-      mbar_init(&ctl->p_full[u], SW / NU);
-      mbar_init(&ctl->p_done[u], 1);
-      mbar_init(&ctl->o_read[u], SW / NU);
-    }
+    mbar_init(&ctl->p_full, SW);
+    mbar_init(&ctl->p_done, 1);
+    mbar_init(&ctl->o_read, SW);
     for (int s = 0; s < kItemSlots; ++s) { mbar_init(&ctl->item_full[s], 1); mbar_init(&ctl->item_empty[s], SW + 1); }
     mbar_init(&ctl->all_sync, SW);
     mbar_init(&ctl->drain, 1);
@@ -404,24 +412,30 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       unsigned g = 0;                  // steps whose scores have been issued
       unsigned pend_flush = 0, n_flush = 0;   // accumulators begun before the pending one; begun so far
       int pend_kk = 0;
-      const uint32_t q0 = smem_u32(q_tile), p0 = smem_u32(p_tile);
+      // descriptors of the operands' first rows
+      const uint64_t v_desc = operand_desc_mn(smem_u32(v_ring), 1024, kOctet), p_desc = operand_desc_mn(smem_u32(p_tile), 128 * kTok, 1024);
+      const uint64_t k_desc = operand_desc_mn(smem_u32(k_ring), 16, kOctet), q_desc = operand_desc(smem_u32(q_tile));
+      const uint32_t v_lo = (uint32_t)v_desc, v_hi = (uint32_t)(v_desc >> 32), p_lo = (uint32_t)p_desc, p_hi = (uint32_t)(p_desc >> 32);
+      const uint32_t k_lo = (uint32_t)k_desc, k_hi = (uint32_t)(k_desc >> 32), q_lo = (uint32_t)q_desc, q_hi = (uint32_t)(q_desc >> 32);
       // O^T of step g - 1
       auto issue_o = [&](unsigned step) -> bool {
         const int s = step % NV;
-        const uint32_t v0 = smem_u32(v_ring + s * KV);
+        if (!mbar_wait(&ctl->p_full, step & 1, abort_flag)) return false;
+        if (!mbar_wait(&ctl->v_full[s], (step / NV) & 1, abort_flag)) return false;
+        // the first product of an accumulator overwrites the one before, which must have been read out
+        if (pend_first && pend_flush >= 1 && !mbar_wait(&ctl->o_read, (pend_flush - 1) & 1, abort_flag)) return false;
+        tc_fence_after();
+        const uint32_t a_lo = v_lo + (uint32_t)s * (KV >> 4), d = tmem + kOCol;
+        if (pend_kk == kTok / 16) {
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-          if (!mbar_wait(&ctl->p_full[u], step & 1, abort_flag)) return false;
-          if (u == 0 && !mbar_wait(&ctl->v_full[s], (step / NV) & 1, abort_flag)) return false;
-          // the first product of an accumulator overwrites the one before, which must have been read out
-          if (pend_first && pend_flush >= 1 && !mbar_wait(&ctl->o_read[u], (pend_flush - 1) & 1, abort_flag)) return false;
-          tc_fence_after();
-          for (int kk = 0; kk < pend_kk; ++kk)   // 16 tokens per instruction
-            umma_bf16_desc(tmem + kOCol + u * 2 * RU, operand_desc_mn(v0 + (uint32_t)kk * 2 * kOctet, 1024, kOctet),
-                           operand_desc_mn(p0 + (uint32_t)(u * PU + kk * 2048), 128 * kTok, 1024), kIdescO, (kk > 0 || !pend_first) ? 1u : 0u);
-          if (u == NU - 1) umma_commit(&ctl->v_empty[s]);
-          umma_commit(&ctl->p_done[u]);
+          for (int kk = 0; kk < kTok / 16; ++kk)   // 16 tokens per instruction
+            umma_words(d, a_lo + kk * (2 * kOctet >> 4), v_hi, p_lo + kk * (2048 >> 4), p_hi, kIdescO, kk > 0 ? 1u : (pend_first ? 0u : 1u));
+        } else {
+          for (int kk = 0; kk < pend_kk; ++kk)
+            umma_words(d, a_lo + kk * (2 * kOctet >> 4), v_hi, p_lo + kk * (2048 >> 4), p_hi, kIdescO, (kk > 0 || !pend_first) ? 1u : 0u);
         }
+        umma_commit(&ctl->v_empty[s]);
+        umma_commit(&ctl->p_done);
         return true;
       };
       for (unsigned gi = 0; ok; ++gi) {
@@ -445,13 +459,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           if (ok && g >= 2) ok = mbar_wait(&ctl->s_empty[g & 1], (g / 2 - 1) & 1, abort_flag);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t k0 = smem_u32(k_ring + s * KV);
+          const uint32_t a_lo = k_lo + (uint32_t)s * (KV >> 4), d = tmem + (g & 1) * R;
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {   // 16 elements = 32 bytes along the swizzled half row
-            const uint64_t dk = operand_desc_mn(k0 + (uint32_t)((kk >> 2) * 1024 + (kk & 3) * 32), 16, kOctet);
-            const uint64_t dq = operand_desc(q0 + (uint32_t)((kk >> 2) * R * 128 + (kk & 3) * 32));
-            umma_bf16_desc(tmem + (g & 1) * R, dk, dq, kIdescS, kk > 0);
-          }
+          for (int kk = 0; kk < D / 16; ++kk)   // 16 elements = 32 bytes along the swizzled half row
+            umma_words(d, a_lo + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), k_hi, q_lo + (((kk >> 2) * R * 128 + (kk & 3) * 32) >> 4), q_hi, kIdescS, kk > 0);
           umma_commit(&ctl->k_empty[s]);
           umma_commit(&ctl->s_full[g & 1]);
           if (i == n - 1) umma_commit(&ctl->q_empty);
@@ -479,8 +490,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     const int grp = warp >> 2, quarter = warp & 3;          // column group; tensor-memory lane quarter
     const int tk = quarter * 32 + lane;                     // token of the step; in the epilogue, dimension of the output
     const int c0 = grp * NC;                                // first column
-    const int unit = NU == 2 ? grp : 0, u0 = c0 - unit * RU; // unit of columns, first column in it
-    const uint32_t o_cols = kOCol + unit * 2 * RU + u0;      // accumulator of the first column (heads; remainders RU further)
+    const uint32_t o_cols = kOCol + c0;                      // accumulator of the first column (heads; remainders R further)
     const int my_c = c0 + lane % LW;                         // the column(s) whose bookkeeping this lane carries: my_c + k LW
     const bool keeper = lane < LW;
     const uint32_t lane_addr = tmem + ((uint32_t)(quarter * 32) << 16);
@@ -607,12 +617,12 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         for (int c = 0; c < NC; c += 16) {
           uint32_t oh[16], ol[16];
           tmem_load<16>(lane_addr + o_cols + (uint32_t)c, oh);
-          tmem_load<16>(lane_addr + o_cols + (uint32_t)(RU + c), ol);
+          tmem_load<16>(lane_addr + o_cols + (uint32_t)(R + c), ol);
 #pragma unroll
           for (int e = 0; e < 16; ++e) acc[c + e] += __uint_as_float(oh[e]) + __uint_as_float(ol[e]);
         }
         tc_fence_before();
-        warp_arrive(&ctl->o_read[unit], lane);
+        warp_arrive(&ctl->o_read, lane);
       };
 
       const int n = it.end - it.begin + it.draft;
@@ -675,7 +685,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         if (*(volatile uint32_t*)&ctl->need[grp][g & 1] == g + 1) {
           // ---- move the references that were outrun to the maximum of what has been seen
           if (g > 0) {
-            ok = warp_wait(&ctl->p_done[unit], (g - 1) & 1, abort_flag);
+            ok = warp_wait(&ctl->p_done, (g - 1) & 1, abort_flag);
             if (!ok) break;
           }
           if (flush_now) flush();
@@ -728,7 +738,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               if (i % kFlush != 0) {   // the accumulator holds products of this item
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
-                  const uint32_t addr = lane_addr + o_cols + (uint32_t)(part * RU + c);
+                  const uint32_t addr = lane_addr + o_cols + (uint32_t)(part * R + c);
                   uint32_t o[16];
                   tmem_load<16>(addr, o);
 #pragma unroll
@@ -742,7 +752,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           (void)scores();
           weights();
         } else if (g > 0) {   // the product of the step before must have read its weights
-          ok = warp_wait(&ctl->p_done[unit], (g - 1) & 1, abort_flag);
+          ok = warp_wait(&ctl->p_done, (g - 1) & 1, abort_flag);
           if (!ok) break;
         }
         // S is read out
@@ -750,7 +760,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         warp_arrive(&ctl->s_empty[g & 1], lane);
         if (flush_now) flush();
         // ---- sums; a weight is written as a bf16 head (its upper 16 bits) plus a bf16 remainder
-        uint8_t* p_row = p_tile + unit * PU + tk * 128;
+        uint8_t* p_row = p_tile + tk * 128;
 #pragma unroll
         for (int c = 0; c < NC; c += 8) {
           uint32_t hi[4], lo[4];
@@ -766,14 +776,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             const __nv_bfloat162 r = __floats2bfloat162_rn(r0, r1);
             lo[k] = *(const uint32_t*)&r;
           }
-          const int ch = u0 + c, cl = RU + ch;   // columns of heads and remainders in the unit's operand
+          const int ch = c0 + c, cl = R + ch;   // columns of heads and remainders in the 2R-column operand
           *(uint4*)(p_row + (ch >> 6) * (128 * kTok) + ((((ch & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
           *(uint4*)(p_row + (cl >> 6) * (128 * kTok) + ((((cl & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
         // ---- V rows that no weight may meet: a zero weight times a NaN is a NaN.  Behind the head's last token the pool
         // may hold anything; a draft is hidden from the nodes of other branches.
         const int sv = g % NV;
-        bool fixed = draft;
         if (draft) {
           ok = warp_wait(&ctl->v_full[sv], (g / NV) & 1, abort_flag);
           if (!ok) break;
@@ -799,7 +808,6 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         } else if (slot0 + kTok > it.st.len) {
           ok = warp_wait(&ctl->v_full[sv], (g / NV) & 1, abort_flag);
           if (!ok) break;
-          fixed = true;
           const int first = it.st.len - slot0, last = (first + 15) / 16 * 16;
           for (int idx = tid; idx < (last - first) * (D / 8); idx += SW * 32) {
             const int t = first + idx / (D / 8), c = idx % (D / 8);
@@ -807,13 +815,12 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        if (NU > 1 && fixed && !(ok = all_sync())) break;   // (a unit's product reads rows that the other group has put right)
         tc_fence_before();
-        warp_arrive(&ctl->p_full[unit], lane);
+        warp_arrive(&ctl->p_full, lane);
       }
       if (!ok) break;
       // ---- the rows' results
-      ok = warp_wait(&ctl->p_done[unit], (g - 1) & 1, abort_flag);
+      ok = warp_wait(&ctl->p_done, (g - 1) & 1, abort_flag);
       if (!ok) break;
       flush();
       float* l_part = (float*)(p_tile + 8192) + grp * 4 * NC;   // [quarter][NC]

@@ -36,6 +36,7 @@ constexpr int kVerifyCluster = 8;       // CTAs that share a sequence (the porta
 constexpr int kMaxSegs = 1024;          // segments of a CTA's share of a row
 constexpr int kUnroll = 8;              // values of a row in flight per lane
 constexpr int kSegUnit = 32 * kUnroll;  // a segment is a multiple of this
+constexpr int kKeepSegs = 4;            // segments of one unit each that a warp can keep in registers
 
 __device__ __forceinline__ float raw_prob(const float* x) { return __ldg(x); }
 __device__ __forceinline__ float raw_prob(const __nv_bfloat16* x) {
@@ -77,8 +78,10 @@ __device__ __forceinline__ double running_sum(double x, int lane) {
   return x;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyCall vc) {
+// kKeep: a row's values stay in registers while its node is the current one, so that every rejected child after the
+// first costs no memory access (needs rows of at most kVerifyCluster * kVerifyWarps * kKeepSegs units, 131072 values).
+template <typename T, bool kKeep>
+__global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(VerifyCall vc) {
   __shared__ VerifySmem sm;
   cg::cluster_group cluster = cg::this_cluster();
   const int rank = (int)cluster.block_rank(), n_ranks = (int)cluster.num_blocks();
@@ -109,6 +112,8 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyCall vc) {
   double minus = 0.0, left = 1.0, total = 1.0;
   bool fresh = false, whole = false;   // the segment sums belong to the current W; the residual was empty
   unsigned pass = 0;
+  float p_kept[kKeep ? kKeepSegs : 1][kUnroll], q_kept[kKeep ? kKeepSegs : 1][kUnroll];
+  int p_row_kept = -1, q_row_kept = -1;
   for (;; ++pass) {
     if (warp == 0) {
       bool draw = false;
@@ -181,34 +186,62 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyCall vc) {
     const T* p_row = target + (size_t)sm.row * vc.target_stride_row;
     const T* q_row = a != 0.0 ? draft + (size_t)sm.row * vc.draft_stride_row : nullptr;
     double mine = 0.0;
-    for (int s = warp; s < n_segs; s += kVerifyWarps) {
+    // kUnroll values of a row, 32 apart, from position i0 on
+    auto load = [&](const T* row, int i0, int hi, float (&x)[kUnroll]) {
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) x[k] = i0 + 32 * k < hi ? raw_prob(row + i0 + 32 * k) : 0.f;
+    };
+    // the sum of W over them
+    auto weigh = [&](const float (&pv)[kUnroll], const float (&qv)[kUnroll], int i0, bool has_gone) -> double {
+      double sum = 0.0;
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        double w = prob(pv[k]);
+        if (q_row) w = fmax(w - a * prob(qv[k]), 0.0);
+        if (has_gone)
+          for (int j = 0; j < gone; ++j)
+            if (sm.gone[j] == i0 + 32 * k) w = 0.0;
+        sum += w;
+      }
+      return sum;
+    };
+    auto segment = [&](int s, const float (*pk)[kUnroll], const float (*qk)[kUnroll]) {
       const int lo = (seg0 + s) * seg_len, hi = min(V, lo + seg_len);
       bool has_gone = false;
       for (int i = lane; i < gone; i += 32) has_gone |= sm.gone[i] >= lo && sm.gone[i] < hi;
       has_gone = __any_sync(0xffffffffu, has_gone);
       double sum = 0.0;
-      for (int i0 = lo + lane; i0 < hi; i0 += kSegUnit) {
-        float pv[kUnroll], qv[kUnroll];
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-          const int i = i0 + 32 * k;
-          pv[k] = i < hi ? raw_prob(p_row + i) : 0.f;
-          qv[k] = q_row && i < hi ? raw_prob(q_row + i) : 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-          double w = prob(pv[k]);
-          if (q_row) w = fmax(w - a * prob(qv[k]), 0.0);
-          if (has_gone)
-            for (int j = 0; j < gone; ++j)
-              if (sm.gone[j] == i0 + 32 * k) w = 0.0;
-          sum += w;
+      if (pk) {
+        sum = weigh(*pk, *qk, lo + lane, has_gone);
+      } else {
+        for (int i0 = lo + lane; i0 < hi; i0 += kSegUnit) {
+          float pv[kUnroll], qv[kUnroll] = {};
+          load(p_row, i0, hi, pv);
+          if (q_row) load(q_row, i0, hi, qv);
+          sum += weigh(pv, qv, i0, has_gone);
         }
       }
 #pragma unroll
       for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
       if (lane == 0) sm.seg_sum[s] = sum;
       mine += sum;
+    };
+    if constexpr (kKeep) {   // (a segment is one unit here)
+      if (p_row_kept != sm.row) {
+        p_row_kept = sm.row;
+#pragma unroll
+        for (int k = 0; k < kKeepSegs; ++k) load(p_row, (seg0 + warp + k * kVerifyWarps) * kSegUnit + lane, warp + k * kVerifyWarps < n_segs ? V : 0, p_kept[k]);
+      }
+      if (q_row && q_row_kept != sm.row) {
+        q_row_kept = sm.row;
+#pragma unroll
+        for (int k = 0; k < kKeepSegs; ++k) load(q_row, (seg0 + warp + k * kVerifyWarps) * kSegUnit + lane, warp + k * kVerifyWarps < n_segs ? V : 0, q_kept[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kKeepSegs; ++k)
+        if (warp + k * kVerifyWarps < n_segs) segment(warp + k * kVerifyWarps, &p_kept[k], &q_kept[k]);
+    } else {
+      for (int s = warp; s < n_segs; s += kVerifyWarps) segment(s, nullptr, nullptr);
     }
     if (lane == 0) sm.warp_sum[warp] = mine;
     __syncthreads();
@@ -266,11 +299,27 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyCall vc) {
   const int lo = (seg0 + seg) * seg_len, hi = min(V, lo + seg_len);
   int token = -1;
   run = before;
-  for (int i0 = lo; i0 < hi; i0 += 32) {
-    const double w = i0 + lane < hi ? weight_at(sm, p_row, q_row, a, i0 + lane) : 0.0;
-    const double upto = run + running_sum(w, lane);
-    const unsigned over = __ballot_sync(0xffffffffu, w > 0.0 && upto > threshold), with = __ballot_sync(0xffffffffu, w > 0.0);
-    if (over || with) token = i0 + (over ? __ffs(over) - 1 : 31 - __clz(with));
+  for (int i0 = lo; i0 < hi; i0 += kSegUnit) {   // kUnroll neighbours to a lane
+    double w[kUnroll], mine = 0.0;
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+      const int i = i0 + lane * kUnroll + k;
+      w[k] = i < hi ? weight_at(sm, p_row, q_row, a, i) : 0.0;
+      mine += w[k];
+    }
+    const double upto = run + running_sum(mine, lane);
+    const unsigned over = __ballot_sync(0xffffffffu, mine > 0.0 && upto > threshold), with = __ballot_sync(0xffffffffu, mine > 0.0);
+    if (over || with) {
+      const int pick = over ? __ffs(over) - 1 : 31 - __clz(with);
+      double r = upto - mine;
+      int at = -1;
+#pragma unroll
+      for (int k = 0; k < kUnroll; ++k) {
+        if (w[k] > 0.0 && (at < 0 || !(over && r > threshold))) at = k;   // the first whose sum is beyond the threshold, or the last
+        r += w[k];
+      }
+      token = i0 + pick * kUnroll + __shfl_sync(0xffffffffu, at, pick);
+    }
     if (over) break;
     run = __shfl_sync(0xffffffffu, upto, 31);
   }
@@ -279,7 +328,7 @@ __global__ void __launch_bounds__(kVerifyThreads) verify_kernel(VerifyCall vc) {
 
 }  // namespace
 
-cudaError_t launch_verify(const VerifyCall& call, int dtype, cudaStream_t stream) {
+cudaError_t launch_verify(const VerifyCall& call, int dtype, int n_sms, cudaStream_t stream) {
   VerifyCall vc = call;
   // segments: at most kMaxSegs to a CTA
   const long long units = ((long long)vc.vocab + kSegUnit - 1) / kSegUnit;
@@ -294,8 +343,13 @@ cudaError_t launch_verify(const VerifyCall& call, int dtype, cudaStream_t stream
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return dtype == RAZOR_BF16 ? cudaLaunchKernelEx(&cfg, verify_kernel<__nv_bfloat16>, vc)
-                             : cudaLaunchKernelEx(&cfg, verify_kernel<float>, vc);
+  // Rows in registers: when the clusters have an SM to each CTA anyway (the registers of a CTA fill most of an SM; with
+  // more sequences the SMs are kept busy by CTAs waiting side by side).
+  const bool keep = vc.seg_len == kSegUnit && units <= (long long)kVerifyCluster * kVerifyWarps * kKeepSegs &&
+                    (long long)vc.batch * kVerifyCluster <= n_sms;
+  if (dtype == RAZOR_BF16)
+    return keep ? cudaLaunchKernelEx(&cfg, verify_kernel<__nv_bfloat16, true>, vc) : cudaLaunchKernelEx(&cfg, verify_kernel<__nv_bfloat16, false>, vc);
+  return keep ? cudaLaunchKernelEx(&cfg, verify_kernel<float, true>, vc) : cudaLaunchKernelEx(&cfg, verify_kernel<float, false>, vc);
 }
 
 }  // namespace razor
