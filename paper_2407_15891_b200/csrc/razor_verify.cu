@@ -34,7 +34,7 @@ constexpr int kVerifyThreads = 512;
 constexpr int kVerifyWarps = kVerifyThreads / 32;
 constexpr int kVerifyCluster = 8;       // CTAs that share a sequence (the portable cluster size)
 constexpr int kMaxSegs = 1024;          // segments of a CTA's share of a row
-constexpr int kUnroll = 8;              // values of a row in flight per lane
+constexpr int kUnroll = 8;              // neighbouring values of a row that a lane takes at a time
 constexpr int kSegUnit = 32 * kUnroll;  // a segment is a multiple of this
 constexpr int kKeepSegs = 4;            // segments of one unit each that a warp can keep in registers
 
@@ -43,18 +43,42 @@ __device__ __forceinline__ float raw_prob(const __nv_bfloat16* x) {
   return __uint_as_float((uint32_t)__ldg((const unsigned short*)x) << 16);
 }
 // What is not a positive finite number counts as zero.
-__device__ __forceinline__ double prob(float x) { return x > 0.f && x < CUDART_INF_F ? (double)x : 0.0; }
+__device__ __forceinline__ float clean(float x) { return x < CUDART_INF_F ? fmaxf(x, 0.f) : 0.f; }
+__device__ __forceinline__ double prob(float x) { return (double)clean(x); }
+// kUnroll values of a row from position i on (none at or beyond hi), cleaned; wide: 16-byte loads will do.
+__device__ __forceinline__ void load_row(const float* row, int i, int hi, bool wide, float (&x)[kUnroll]) {
+  if (wide && i + kUnroll <= hi) {
+    const float4 a = __ldg((const float4*)(row + i)), b = __ldg((const float4*)(row + i) + 1);
+    x[0] = clean(a.x); x[1] = clean(a.y); x[2] = clean(a.z); x[3] = clean(a.w);
+    x[4] = clean(b.x); x[5] = clean(b.y); x[6] = clean(b.z); x[7] = clean(b.w);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) x[k] = i + k < hi ? clean(raw_prob(row + i + k)) : 0.f;
+  }
+}
+__device__ __forceinline__ void load_row(const __nv_bfloat16* row, int i, int hi, bool wide, float (&x)[kUnroll]) {
+  if (wide && i + kUnroll <= hi) {
+    Elem<__nv_bfloat16>::unpack(__ldg((const uint4*)(row + i)), x);
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) x[k] = clean(x[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) x[k] = i + k < hi ? clean(raw_prob(row + i + k)) : 0.f;
+  }
+}
+// max(x, 0) by the sign bit: the library's maximum of two doubles runs at a quarter of an addition's rate.  (x is no NaN.)
+__device__ __forceinline__ double at_least_0(double x) { return __double2hiint(x) < 0 ? 0.0 : x; }
 
 struct VerifySmem {
   double seg_sum[kMaxSegs];
-  double warp_sum[kVerifyWarps];
-  double part[2][kVerifyCluster];   // sum of every CTA's share, written by its owner; passes take turns
+  double part[2][kVerifyCluster][kVerifyWarps];   // every warp's sum of every CTA's share, written by its owner; passes take turns
   float p_child[kTreeMaxNodes], q_child[kTreeMaxNodes], u[kTreeMaxNodes];
   int32_t parent[kTreeMaxNodes], token[kTreeMaxNodes];
   int32_t gone[kTreeMaxNodes];      // rejected children of the current node
   int32_t path[kTreeMaxNodes];
   int32_t n_gone, row;              // row: the current node + 1
   int32_t draw;                     // 1: the walk has ended and the segment sums are those of its last W
+  int32_t again;                    // 1: the pass is over the target's own row, rejected children among it
   double minus;                     // A
 };
 
@@ -62,7 +86,7 @@ struct VerifySmem {
 template <typename T>
 __device__ __forceinline__ double weight_at(const VerifySmem& sm, const T* p_row, const T* q_row, double a, int i) {
   double w = prob(raw_prob(p_row + i));
-  if (q_row) w = fmax(w - a * prob(raw_prob(q_row + i)), 0.0);
+  if (q_row) w = at_least_0(fma(-a, prob(raw_prob(q_row + i)), w));
   for (int j = 0; j < sm.n_gone; ++j)
     if (sm.gone[j] == i) w = 0.0;
   return w;
@@ -80,6 +104,24 @@ __device__ __forceinline__ double running_sum(double x, int lane) {
 
 // kKeep: a row's values stay in registers while its node is the current one, so that every rejected child after the
 // first costs no memory access (needs rows of at most kVerifyCluster * kVerifyWarps * kKeepSegs units, 131072 values).
+constexpr int kParts = kVerifyCluster * kVerifyWarps;
+static_assert(kParts == 128 && kUnroll == 8, "four sums to a lane; eight values to a tree of sums");
+// The CTAs' sums from their warps': lane r < kVerifyCluster gets CTA r's, and all lanes the whole (in the same order in
+// every CTA of the cluster).
+__device__ __forceinline__ double cta_part(const double (*part)[kVerifyWarps], int lane) {
+  const double* p = &part[0][0] + lane * 4;   // a CTA's sixteen sums lie in four neighbouring lanes
+  double x = (p[0] + p[1]) + (p[2] + p[3]);
+  x += __shfl_xor_sync(0xffffffffu, x, 1);
+  x += __shfl_xor_sync(0xffffffffu, x, 2);
+  return __shfl_sync(0xffffffffu, x, (lane & 7) * 4);
+}
+__device__ __forceinline__ double all_parts(const double (*part)[kVerifyWarps], int lane) {
+  double x = cta_part(part, lane);
+#pragma unroll
+  for (int off = 1; off < kVerifyCluster; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+  return x;
+}
+
 template <typename T, bool kKeep>
 __global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(VerifyCall vc) {
   __shared__ VerifySmem sm;
@@ -118,8 +160,7 @@ __global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(V
     if (warp == 0) {
       bool draw = false;
       double sum = 0.0;   // of the last pass
-      if (pass > 0)
-        for (int r = 0; r < n_ranks; ++r) sum += sm.part[(pass - 1) & 1][r];
+      if (pass > 0) sum = all_parts(sm.part[(pass - 1) & 1], lane);
       if (fresh && draft && !whole) total = sum;
       for (;;) {
         int t = -1;       // the next child of `cur` behind `last`
@@ -173,6 +214,7 @@ __global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(V
       }
       if (lane == 0) {
         sm.draw = draw;
+        sm.again = whole;
         sm.row = cur + 1;
         sm.minus = minus;
         sm.n_gone = n_gone;
@@ -183,73 +225,80 @@ __global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(V
     // ---- one pass over this CTA's share of the row: segment sums of W
     const double a = sm.minus;
     const int gone = sm.n_gone;
+    if (kKeep && sm.again) p_row_kept = -1;   // (the kept row has lost its rejected children)
     const T* p_row = target + (size_t)sm.row * vc.target_stride_row;
     const T* q_row = a != 0.0 ? draft + (size_t)sm.row * vc.draft_stride_row : nullptr;
     double mine = 0.0;
-    // kUnroll values of a row, 32 apart, from position i0 on
-    auto load = [&](const T* row, int i0, int hi, float (&x)[kUnroll]) {
-#pragma unroll
-      for (int k = 0; k < kUnroll; ++k) x[k] = i0 + 32 * k < hi ? raw_prob(row + i0 + 32 * k) : 0.f;
+    const bool wide = (((uintptr_t)p_row | (uintptr_t)q_row) & 15) == 0;
+    // does a rejected child lie in [lo, hi)?
+    auto any_gone = [&](int lo, int hi) -> bool {
+      bool hit = false;
+      for (int i = lane; i < gone; i += 32) hit |= sm.gone[i] >= lo && sm.gone[i] < hi;
+      return __any_sync(0xffffffffu, hit);
     };
-    // the sum of W over them
-    auto weigh = [&](const float (&pv)[kUnroll], const float (&qv)[kUnroll], int i0, bool has_gone) -> double {
-      double sum = 0.0;
+    // the sum of W over kUnroll values from position i on
+    auto weigh = [&](float (&pv)[kUnroll], const float (&qv)[kUnroll], int i, bool has_gone) -> double {
+      if (has_gone) {
+#pragma unroll 1
+        for (int j = 0; j < gone; ++j)
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        double w = prob(pv[k]);
-        if (q_row) w = fmax(w - a * prob(qv[k]), 0.0);
-        if (has_gone)
-          for (int j = 0; j < gone; ++j)
-            if (sm.gone[j] == i0 + 32 * k) w = 0.0;
-        sum += w;
+          for (int k = 0; k < kUnroll; ++k)
+            if (sm.gone[j] == i + k) pv[k] = 0.f;
       }
-      return sum;
-    };
-    auto segment = [&](int s, const float (*pk)[kUnroll], const float (*qk)[kUnroll]) {
-      const int lo = (seg0 + s) * seg_len, hi = min(V, lo + seg_len);
-      bool has_gone = false;
-      for (int i = lane; i < gone; i += 32) has_gone |= sm.gone[i] >= lo && sm.gone[i] < hi;
-      has_gone = __any_sync(0xffffffffu, has_gone);
-      double sum = 0.0;
-      if (pk) {
-        sum = weigh(*pk, *qk, lo + lane, has_gone);
-      } else {
-        for (int i0 = lo + lane; i0 < hi; i0 += kSegUnit) {
-          float pv[kUnroll], qv[kUnroll] = {};
-          load(p_row, i0, hi, pv);
-          if (q_row) load(q_row, i0, hi, qv);
-          sum += weigh(pv, qv, i0, has_gone);
-        }
-      }
+      double s0 = 0.0, s1 = 0.0;
 #pragma unroll
-      for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-      if (lane == 0) sm.seg_sum[s] = sum;
-      mine += sum;
+      for (int k = 0; k < kUnroll; k += 2) {
+        const double x = (double)pv[k], y = (double)pv[k + 1];
+        s0 += q_row ? at_least_0(fma(-a, (double)qv[k], x)) : x;
+        s1 += q_row ? at_least_0(fma(-a, (double)qv[k + 1], y)) : y;
+      }
+      return s0 + s1;
     };
     if constexpr (kKeep) {   // (a segment is one unit here)
-      if (p_row_kept != sm.row) {
-        p_row_kept = sm.row;
+      const bool fresh_p = p_row_kept != sm.row, fresh_q = q_row && q_row_kept != sm.row;
 #pragma unroll
-        for (int k = 0; k < kKeepSegs; ++k) load(p_row, (seg0 + warp + k * kVerifyWarps) * kSegUnit + lane, warp + k * kVerifyWarps < n_segs ? V : 0, p_kept[k]);
+      for (int k = 0; k < kKeepSegs; ++k) {
+        const int i = (seg0 + warp + k * kVerifyWarps) * kSegUnit + lane * kUnroll, hi = warp + k * kVerifyWarps < n_segs ? V : 0;
+        if (fresh_p) load_row(p_row, i, hi, wide, p_kept[k]);
+        if (fresh_q) load_row(q_row, i, hi, wide, q_kept[k]);
       }
-      if (q_row && q_row_kept != sm.row) {
-        q_row_kept = sm.row;
+      if (fresh_p) p_row_kept = sm.row;
+      if (fresh_q) q_row_kept = sm.row;
+      double sum[kKeepSegs];
 #pragma unroll
-        for (int k = 0; k < kKeepSegs; ++k) load(q_row, (seg0 + warp + k * kVerifyWarps) * kSegUnit + lane, warp + k * kVerifyWarps < n_segs ? V : 0, q_kept[k]);
+      for (int k = 0; k < kKeepSegs; ++k) {
+        const int lo = (seg0 + warp + k * kVerifyWarps) * kSegUnit;
+        sum[k] = weigh(p_kept[k], q_kept[k], lo + lane * kUnroll, any_gone(lo, lo + kSegUnit));
       }
 #pragma unroll
-      for (int k = 0; k < kKeepSegs; ++k)
-        if (warp + k * kVerifyWarps < n_segs) segment(warp + k * kVerifyWarps, &p_kept[k], &q_kept[k]);
+      for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+        for (int k = 0; k < kKeepSegs; ++k) sum[k] += __shfl_xor_sync(0xffffffffu, sum[k], off);
+#pragma unroll
+      for (int k = 0; k < kKeepSegs; ++k) {
+        if (lane == 0 && warp + k * kVerifyWarps < n_segs) sm.seg_sum[warp + k * kVerifyWarps] = sum[k];
+        mine += sum[k];
+      }
     } else {
-      for (int s = warp; s < n_segs; s += kVerifyWarps) segment(s, nullptr, nullptr);
+      for (int s = warp; s < n_segs; s += kVerifyWarps) {
+        const int lo = (seg0 + s) * seg_len, hi = min(V, lo + seg_len);
+        const bool has_gone = any_gone(lo, hi);
+        double sum = 0.0;
+#pragma unroll 1
+        for (int i = lo + lane * kUnroll; i < hi; i += kSegUnit) {
+          float pv[kUnroll], qv[kUnroll] = {};
+          load_row(p_row, i, hi, wide, pv);
+          if (q_row) load_row(q_row, i, hi, wide, qv);
+          sum += weigh(pv, qv, i, has_gone);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        if (lane == 0) sm.seg_sum[s] = sum;
+        mine += sum;
+      }
     }
-    if (lane == 0) sm.warp_sum[warp] = mine;
-    __syncthreads();
-    if (tid < n_ranks) {   // this CTA's sum to every CTA of the cluster
-      double sum = 0.0;
-      for (int w = 0; w < kVerifyWarps; ++w) sum += sm.warp_sum[w];
-      *cluster.map_shared_rank(&sm.part[pass & 1][rank], tid) = sum;
-    }
+    if (lane < n_ranks) *cluster.map_shared_rank(&sm.part[pass & 1][rank][warp], lane) = mine;   // to every CTA of the cluster
     cluster.sync();   // (no CTA writes the same half of part[] again before all have come through the next pass's)
   }
 
@@ -261,21 +310,14 @@ __global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(V
   // The draw: the token is in the share of the first CTA whose running sum exceeds the threshold.  (Sums taken in
   // another order may differ in the last bit, so the last one with any weight stands in where none does.)
   if (warp != 0) return;
-  const double* part = sm.part[(pass - 1) & 1];   // (the walk draws after at least one pass)
-  double sum = 0.0;
-  for (int r = 0; r < n_ranks; ++r) sum += part[r];
-  const double threshold = (double)vc.u_sample[b] * sum;
-  double run = 0.0, before = 0.0, before_last = 0.0;
-  int owner = -1, last_with = -1;
-  for (int r = 0; r < n_ranks && owner < 0; ++r) {
-    if (part[r] > 0.0) {
-      last_with = r;
-      before_last = run;
-      if (run + part[r] > threshold) { owner = r; before = run; }
-    }
-    run += part[r];
-  }
-  if (owner < 0) { owner = last_with; before = before_last; }
+  const double (*part)[kVerifyWarps] = sm.part[(pass - 1) & 1];   // (the walk draws after at least one pass)
+  const double threshold = (double)vc.u_sample[b] * all_parts(part, lane);
+  const double cta_sum = cta_part(part, lane), mine = lane < n_ranks ? cta_sum : 0.0;
+  const double upto_cta = running_sum(mine, lane);
+  const unsigned cta_over = __ballot_sync(0xffffffffu, lane < n_ranks && mine > 0.0 && upto_cta > threshold);
+  const unsigned cta_with = __ballot_sync(0xffffffffu, lane < n_ranks && mine > 0.0);
+  const int owner = cta_over ? __ffs(cta_over) - 1 : cta_with ? 31 - __clz(cta_with) : -1;
+  double run, before = owner >= 0 ? __shfl_sync(0xffffffffu, upto_cta - mine, owner) : 0.0;
   if (owner < 0 && rank == 0 && lane == 0) vc.next_token[b] = -1;   // a target row without any weight
   if (rank != owner) return;
   // the segment, then the position in it: the first whose running sum exceeds the threshold, else the last with weight
