@@ -276,6 +276,8 @@ constexpr int kTreeMaxSpans = 1024;
 struct TreeUnit {
   int32_t head, first_span, n_parts, pad;
 };
+cudaError_t launch_tree_wide(const DeviceView& dv, long long pool_pages, int layer, const TreeCall& call, long long rec_rows,
+                             int n_sms, cudaStream_t stream);   // more than 64 query rows per KV head, no ALiBi
 cudaError_t launch_tree_mma(const DeviceView& dv, long long pool_pages, int layer, const TreeCall& call, long long rec_rows,
                             int n_sms, cudaStream_t stream);
 // longest: tokens of the longest head (sizes the parts); rec_rows: rows the record area of the workspace has.

@@ -179,17 +179,19 @@ def test_a_late_maximum_far_above_the_first():
     cache.close()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_what_a_node_does_not_see_cannot_reach_it(dtype):
+@pytest.mark.parametrize("dtype,group,D,more", [("bf16", 4, 128, 0), ("f32", 4, 128, 0), ("bf16", 1, 128, 0),
+                                                  ("bf16", 8, 128, 0), ("bf16", 8, 64, 20), ("bf16", 1, 128, 119)])
+def test_what_a_node_does_not_see_cannot_reach_it(dtype, group, D, more):
     """NaN and infinities in the K and V of nodes on other branches, in absent nodes and in the pool beyond a head's last
     token leave a node's output as it is, bit for bit; nodes that see them get what the arithmetic gives."""
-    w = synth.Workload("poison", 2, 1, 8, 2, 128, dtype, [130, 37], [60, 30], 4, 1, 0, 15)
+    w = synth.Workload("poison", 2, 1, 2 * group, 2, D, dtype, [130, 37], [60, 30], 4, 1, 0, 15)
     cache = make_cache(w)
     cache.pool.fill_(0xFF)             # every 16- and 32-bit pattern of it is a NaN
     K, V = synth.make_dense_kv(w, 0, DEV)
     cache.compress(0, K, V, w.ctx_len, w.retrieval(0), w.window)
-    q, k, v = _drafts(w, 9, 9)
-    parent = np.array([[-1, 0, 0, 1, 2, -2, 5, -1, 7]] * 2, dtype=np.int32)   # 2, 4: the clean line; 5, 6 absent
+    q, k, v = _drafts(w, 9 + more, 9)
+    # 2, 4: the clean line; 5, 6 absent; `more` nodes behind them that follow node 4
+    parent = np.array([[-1, 0, 0, 1, 2, -2, 5, -1, 7] + [4] * more] * 2, dtype=np.int32)
     pd = torch.from_numpy(parent).to(DEV)
     clean = cache.decode_tree(0, q, k, v, pd).clone()
     assert torch.isfinite(clean).all()
@@ -199,7 +201,7 @@ def test_what_a_node_does_not_see_cannot_reach_it(dtype):
             v2[:, n, :, ::3] = bad
             k2[:, n, :, 5] = bad
         got = cache.decode_tree(0, q, k2, v2, pd)
-        for t in (0, 2, 4):
+        for t in (0, 2, 4, *range(9, 9 + more)):
             assert torch.equal(got[:, t], clean[:, t]), (bad, t)
         assert (got[:, 5:7] == 0).all()
         # V alone: the nodes that see it get non-finite values there and the clean ones elsewhere
@@ -210,7 +212,7 @@ def test_what_a_node_does_not_see_cannot_reach_it(dtype):
             assert not torch.isfinite(got[:, t, :, 10]).any()
             if not math.isnan(bad):
                 assert (got[:, t, :, 10] == bad).all()
-            keep = [d for d in range(128) if d != 10]
+            keep = [d for d in range(D) if d != 10]
             assert torch.equal(got[:, t][..., keep], clean[:, t][..., keep])
         assert torch.equal(got[:, 0], clean[:, 0]) and torch.equal(got[:, 4], clean[:, 4])
     assert cache.device_status() == 0
