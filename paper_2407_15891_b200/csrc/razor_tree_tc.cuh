@@ -306,7 +306,7 @@ __device__ __forceinline__ void tree_produce(const DeviceView& dv, const CUtenso
 }
 
 // Folds the partial records of the heads that a cut ran through, parts in order: a warp per query row.
-// grid = (spans, tiles, R / 32), eight warps of four rows each.
+// grid = (spans, tiles, R / 8).
 template <int D, int R>
 __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCall tc) {
   cudaGridDependencySynchronize();
@@ -316,10 +316,10 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCa
   const int b = u.head / dv.n_kv_heads, g = u.head % dv.n_kv_heads;
   // the first part is the last item of its span, the others are the first of theirs
   auto record = [&](int p) { return ((size_t)((u.first_span + p) * tc.n_tiles + tile) * 2 + (p == 0 ? 1 : 0)) * R; };
-  for (int k = 0; k < 4; ++k) {
-    const int c = blockIdx.z * 32 + k * 8 + warp, r = tile * R + c;
+  {
+    const int c = blockIdx.z * 8 + warp, r = tile * R + c;
     if (r >= tc.n_nodes * G) return;
-    if (dv.rec_ml[record(u.n_parts - 1) + c].y < 0.f) continue;   // an absent node (the last part holds the tree)
+    if (dv.rec_ml[record(u.n_parts - 1) + c].y < 0.f) return;   // an absent node (the last part holds the tree)
     float m = -CUDART_INF_F, l = 0.f;
     LaneVec<D> acc;
     acc.zero();
@@ -394,7 +394,7 @@ cudaError_t tree_launch(Kernel kernel, int smem_bytes, const DeviceView& dv, lon
   e = cudaGetLastError();
   if (e != cudaSuccess || tc.n_spans == 1) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(tc.n_spans, tc.n_tiles, R / 32);
+  cfg.gridDim = dim3(tc.n_spans, tc.n_tiles, R / 8);
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute at[1];

@@ -298,9 +298,28 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             }
             return fmaxf(m0, m1) > kLag;
           };
+          // Weights, their sum, and their two halves for the product: a bf16 head (the upper 16 bits) plus a bf16 remainder,
+          // column c of either holding the pair of tokens 2 c and 2 c + 1 (remainders replace the scores).  One loop: the
+          // exponentials of a pair go to the special-function unit while the pair before is split.
+          uint32_t hi[HT / 2];
+          float step_sum;
           auto weights = [&]() {
+            uint64_t sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
 #pragma unroll
-            for (int c = 0; c < HT; ++c) v[c] = __float_as_uint(fast_exp2(__uint_as_float(v[c])));
+            for (int c = 0; c < HT / 2; ++c) {
+              const float w0 = fast_exp2(__uint_as_float(v[2 * c])), w1 = fast_exp2(__uint_as_float(v[2 * c + 1]));
+              const uint32_t b0 = __float_as_uint(w0), b1 = __float_as_uint(w1);
+              const uint64_t w2 = f2_pack(w0, w1);
+              sum2[c & 1] = f2_add(sum2[c & 1], w2);
+              hi[c] = __byte_perm(b0, b1, 0x7632);
+              float r0, r1;
+              f2_unpack(f2_sub(w2, f2_pack(__uint_as_float(b0 & 0xffff0000u), __uint_as_float(b1 & 0xffff0000u))), r0, r1);
+              const __nv_bfloat162 lo = __floats2bfloat162_rn(r0, r1);
+              v[c] = *(const uint32_t*)&lo;
+            }
+            float a0, a1;
+            f2_unpack(f2_add(sum2[0], sum2[1]), a0, a1);
+            step_sum = a0 + a1;
           };
           const bool outran = scores();
           if (__any_sync(0xffffffffu, outran) && lane == 0) *(volatile uint32_t*)&ctl->need[quarter][g & 1] = g + 1;
@@ -363,26 +382,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           tc_fence_before();
           warp_arrive(&p->s_empty[g & 1], lane);
           if (flush_now) flush();
-          // ---- sums; a weight goes into the product as a bf16 head (its upper 16 bits) plus a bf16 remainder: column c of
-          // either part holds the pair of tokens 2 c and 2 c + 1
-          uint64_t sum2[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
-          uint32_t hi[HT / 2];
-#pragma unroll
-          for (int c = 0; c < HT / 2; ++c) {
-            const uint32_t b0 = v[2 * c], b1 = v[2 * c + 1];
-            const uint64_t w2 = f2_pack(__uint_as_float(b0), __uint_as_float(b1));
-            sum2[c & 1] = f2_add(sum2[c & 1], w2);
-            hi[c] = __byte_perm(b0, b1, 0x7632);
-            float r0, r1;
-            f2_unpack(f2_sub(w2, f2_pack(__uint_as_float(b0 & 0xffff0000u), __uint_as_float(b1 & 0xffff0000u))), r0, r1);
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(r0, r1);
-            v[c] = *(const uint32_t*)&lo;
-          }
           tmem_st32(lane_addr + p_cols, hi);
           tmem_st32(lane_addr + p_cols + kPLo, v);
-          float a0, a1;
-          f2_unpack(f2_add(sum2[0], sum2[1]), a0, a1);
-          l += a0 + a1;
+          l += step_sum;
         } else {
           tc_fence_before();
           warp_arrive(&p->s_empty[g & 1], lane);
