@@ -163,10 +163,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       // O^T of step g - 1
       auto issue_o = [&](unsigned step) -> bool {
         const int s = step % NV;
-        if (!mbar_wait(&p->p_full, step & 1, abort_flag)) return false;
         if (!mbar_wait(&p->v_full[s], (step / NV) & 1, abort_flag)) return false;
         // the first product of an accumulator overwrites the one before, which must have been read out
         if (pend_first && pend_flush >= 1 && !mbar_wait(&p->o_read, (pend_flush - 1) & 1, abort_flag)) return false;
+        if (!mbar_wait(&p->p_full, step & 1, abort_flag)) return false;
         tc_fence_after();
         const uint32_t a_lo = v_lo + (uint32_t)s * (KV >> 4), d = tmem + kOCol;
         if (pend_kk == kTok / 16) {

@@ -101,6 +101,18 @@ __device__ __forceinline__ void umma_words(uint32_t tmem_d, uint32_t a_lo, uint3
       : "r"(tmem_d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// The same with operand A out of tensor memory.
+__device__ __forceinline__ void umma_words_tmem_a(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                                  uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 db, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}"
+      :
+      : "r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 // NC consecutive columns of this thread's lane, in registers when the function returns.
 template <int NC>
 __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&v)[NC]) {

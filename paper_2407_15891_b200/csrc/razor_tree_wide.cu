@@ -106,21 +106,28 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         // descriptors of the operands' first rows
         const uint64_t v_desc = operand_desc_mn(smem_u32(v_ring), 1024, kOctet);
         const uint64_t k_desc = operand_desc_mn(smem_u32(k_ring), 16, kOctet), q_desc = operand_desc(smem_u32(q_tile));
+        const uint32_t v_lo = (uint32_t)v_desc, v_hi = (uint32_t)(v_desc >> 32);
         const uint32_t k_lo = (uint32_t)k_desc, k_hi = (uint32_t)(k_desc >> 32), q_lo = (uint32_t)q_desc, q_hi = (uint32_t)(q_desc >> 32);
         // O of step g - 1
         auto issue_o = [&](unsigned step) -> bool {
           const int s = step % NV;
-          if (!mbar_wait(&p->p_full, step & 1, abort_flag)) return false;
           if (!mbar_wait(&p->v_full[s], (step / NV) & 1, abort_flag)) return false;
           // the first product of an accumulator overwrites the one before, which must have been read out
           if (pend_first && pend_flush >= 1 && !mbar_wait(&p->o_read, (pend_flush - 1) & 1, abort_flag)) return false;
+          if (!mbar_wait(&p->p_full, step & 1, abort_flag)) return false;
           tc_fence_after();
-          const uint64_t b = v_desc + (uint64_t)(s * (KV >> 4));
-          const uint32_t d = tmem + kOCol, a = tmem + kPCol;
-          for (int kk = 0; kk < pend_kk; ++kk) {   // 16 tokens per instruction: 8 columns of pairs
-            const uint64_t bk = b + (uint64_t)(kk * (2 * kOctet >> 4));
-            umma_bf16_tmem_a(d, a + kk * 8, bk, kIdescO, (kk > 0 || !pend_first) ? 1u : 0u);
-            umma_bf16_tmem_a(d, a + kPLo + kk * 8, bk, kIdescO, 1u);
+          const uint32_t b_lo = v_lo + (uint32_t)s * (KV >> 4), d = tmem + kOCol, a = tmem + kPCol;
+          if (pend_kk == kTok / 16) {
+#pragma unroll
+            for (int kk = 0; kk < kTok / 16; ++kk) {   // 16 tokens per instruction: 8 columns of pairs
+              umma_words_tmem_a(d, a + kk * 8, b_lo + kk * (2 * kOctet >> 4), v_hi, kIdescO, kk > 0 ? 1u : (pend_first ? 0u : 1u));
+              umma_words_tmem_a(d, a + kPLo + kk * 8, b_lo + kk * (2 * kOctet >> 4), v_hi, kIdescO, 1u);
+            }
+          } else {
+            for (int kk = 0; kk < pend_kk; ++kk) {
+              umma_words_tmem_a(d, a + kk * 8, b_lo + kk * (2 * kOctet >> 4), v_hi, kIdescO, (kk > 0 || !pend_first) ? 1u : 0u);
+              umma_words_tmem_a(d, a + kPLo + kk * 8, b_lo + kk * (2 * kOctet >> 4), v_hi, kIdescO, 1u);
+            }
           }
           umma_commit(&p->v_empty[s]);
           umma_commit(&p->p_done);
