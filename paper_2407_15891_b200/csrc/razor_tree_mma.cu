@@ -149,81 +149,57 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     tree_produce<D, R, NK, NV>(dv, map_pool, map_q, map_k, map_v, layer, tc, sp, tile, p, k_ring, v_ring, q_tile, lane);
     __syncwarp();
   } else if (warp == SW + 1) {
-    // ================================================================ matrix instructions: one thread
+    // ================================================================ S^T = K Q^T
     if (lane == 0) {
-      bool ok = true, pending = false, pend_first = false;
-      unsigned g = 0;                  // steps whose scores have been issued
-      unsigned pend_flush = 0, n_flush = 0;   // accumulators begun before the pending one; begun so far
-      int pend_kk = 0;
-      // descriptors of the operands' first rows
-      const uint64_t v_desc = operand_desc_mn(smem_u32(v_ring), 1024, kOctet), p_desc = operand_desc_mn(smem_u32(p_tile), 128 * kTok, 1024);
       const uint64_t k_desc = operand_desc_mn(smem_u32(k_ring), 16, kOctet), q_desc = operand_desc(smem_u32(q_tile));
-      const uint32_t v_lo = (uint32_t)v_desc, v_hi = (uint32_t)(v_desc >> 32), p_lo = (uint32_t)p_desc, p_hi = (uint32_t)(p_desc >> 32);
       const uint32_t k_lo = (uint32_t)k_desc, k_hi = (uint32_t)(k_desc >> 32), q_lo = (uint32_t)q_desc, q_hi = (uint32_t)(q_desc >> 32);
-      // O^T of step g - 1
-      auto issue_o = [&](unsigned step) -> bool {
-        const int s = step % NV;
-        if (!mbar_wait(&p->v_full[s], (step / NV) & 1, abort_flag)) return false;
-        // the first product of an accumulator overwrites the one before, which must have been read out
-        if (pend_first && pend_flush >= 1 && !mbar_wait(&p->o_read, (pend_flush - 1) & 1, abort_flag)) return false;
-        if (!mbar_wait(&p->p_full, step & 1, abort_flag)) return false;
+      tree_issue(p, dv, &p->drain[0], [&](unsigned gi) { return mbar_wait(&p->q_full, gi & 1, abort_flag); },
+                 [&](unsigned g, int i, int n, const TreeItem&) {
+        const int s = g % NK;
+        if (g >= 2 && !mbar_wait(&p->s_empty[g & 1], (g / 2 - 1) & 1, abort_flag)) return false;
+        if (!mbar_wait(&p->k_full[s], (g / NK) & 1, abort_flag)) return false;
         tc_fence_after();
-        const uint32_t a_lo = v_lo + (uint32_t)s * (KV >> 4), d = tmem + kOCol;
-        if (pend_kk == kTok / 16) {
+        const uint32_t a_lo = k_lo + (uint32_t)s * (KV >> 4), d = tmem + (g & 1) * R;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)   // 16 elements = 32 bytes along the swizzled half row
+          umma_words(d, a_lo + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), k_hi, q_lo + (((kk >> 2) * R * 128 + (kk & 3) * 32) >> 4), q_hi, kIdescS, kk > 0);
+        umma_commit(&p->s_full[g & 1]);
+        umma_commit(&p->k_empty[s]);
+        if (i == n - 1) umma_commit(&p->q_empty);
+        return true;
+      });
+    }
+    __syncwarp();
+  } else if (warp == SW + 2) {
+    // ================================================================ O^T = V^T P^T
+    if (lane == 0) {
+      const uint64_t v_desc = operand_desc_mn(smem_u32(v_ring), 1024, kOctet), p_desc = operand_desc_mn(smem_u32(p_tile), 128 * kTok, 1024);
+      const uint32_t v_lo = (uint32_t)v_desc, v_hi = (uint32_t)(v_desc >> 32), p_lo = (uint32_t)p_desc, p_hi = (uint32_t)(p_desc >> 32);
+      const uint32_t d = tmem + kOCol;
+      unsigned n_flush = 0;   // accumulators begun
+      tree_issue(p, dv, &p->drain[1], [](unsigned) { return true; }, [&](unsigned g, int i, int n, const TreeItem& it) {
+        const int s = g % NV;
+        const int left = it.draft && i == n - 1 ? n_nodes : it.st.len - (it.begin + i) * kTok;
+        const bool first = i % kFlush == 0;
+        // the first product of an accumulator overwrites the one before, which must have been read out
+        if (first && n_flush >= 1 && !mbar_wait(&p->o_read, (n_flush - 1) & 1, abort_flag)) return false;
+        if (first) n_flush += 1;
+        if (!mbar_wait(&p->v_full[s], (g / NV) & 1, abort_flag)) return false;
+        if (!mbar_wait(&p->p_full, g & 1, abort_flag)) return false;
+        tc_fence_after();
+        const uint32_t a_lo = v_lo + (uint32_t)s * (KV >> 4);
+        if (left > kTok - 16) {
 #pragma unroll
           for (int kk = 0; kk < kTok / 16; ++kk)   // 16 tokens per instruction
-            umma_words(d, a_lo + kk * (2 * kOctet >> 4), v_hi, p_lo + kk * (2048 >> 4), p_hi, kIdescO, kk > 0 ? 1u : (pend_first ? 0u : 1u));
+            umma_words(d, a_lo + kk * (2 * kOctet >> 4), v_hi, p_lo + kk * (2048 >> 4), p_hi, kIdescO, kk > 0 ? 1u : (first ? 0u : 1u));
         } else {
-          for (int kk = 0; kk < pend_kk; ++kk)
-            umma_words(d, a_lo + kk * (2 * kOctet >> 4), v_hi, p_lo + kk * (2048 >> 4), p_hi, kIdescO, (kk > 0 || !pend_first) ? 1u : 0u);
+          for (int kk = 0; kk * 16 < left; ++kk)
+            umma_words(d, a_lo + kk * (2 * kOctet >> 4), v_hi, p_lo + kk * (2048 >> 4), p_hi, kIdescO, (kk > 0 || !first) ? 1u : 0u);
         }
-        umma_commit(&p->v_empty[s]);
         umma_commit(&p->p_done);
+        umma_commit(&p->v_empty[s]);
         return true;
-      };
-      for (unsigned gi = 0; ok; ++gi) {
-        const int slot = gi % kItemSlots;
-        ok = mbar_wait(&p->item_full[slot], (gi / kItemSlots) & 1, abort_flag);
-        if (!ok) break;
-        const TreeItem it = p->item[slot];
-        mbar_arrive(&p->item_empty[slot]);
-        if (it.head < 0) break;
-        // the last product of the item before is not kept waiting for copies of this one
-        if (pending && !(mbar_try_wait(&p->q_full, gi & 1) && mbar_try_wait(&p->k_full[g % NK], (g / NK) & 1))) {
-          ok = issue_o(g - 1);
-          pending = false;
-          if (!ok) break;
-        }
-        ok = mbar_wait(&p->q_full, gi & 1, abort_flag);
-        const int n = it.end - it.begin + it.draft;
-        for (int i = 0; i < n && ok; ++i, ++g) {
-          const int s = g % NK;
-          ok = mbar_wait(&p->k_full[s], (g / NK) & 1, abort_flag);
-          if (ok && g >= 2) ok = mbar_wait(&p->s_empty[g & 1], (g / 2 - 1) & 1, abort_flag);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t a_lo = k_lo + (uint32_t)s * (KV >> 4), d = tmem + (g & 1) * R;
-#pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)   // 16 elements = 32 bytes along the swizzled half row
-            umma_words(d, a_lo + (((kk >> 2) * 1024 + (kk & 3) * 32) >> 4), k_hi, q_lo + (((kk >> 2) * R * 128 + (kk & 3) * 32) >> 4), q_hi, kIdescS, kk > 0);
-          umma_commit(&p->k_empty[s]);
-          umma_commit(&p->s_full[g & 1]);
-          if (i == n - 1) umma_commit(&p->q_empty);
-          if (pending) ok = issue_o(g - 1);   // behind the next step's scores, so that its softmax overlaps this product
-          const bool draft = it.draft && i == n - 1;
-          const int left = draft ? n_nodes : it.st.len - (it.begin + i) * kTok;
-          pending = true;
-          pend_first = i % kFlush == 0;
-          pend_flush = pend_first ? n_flush++ : n_flush;
-          pend_kk = min(kTok / 16, (left + 15) / 16);
-        }
-      }
-      if (ok && pending) ok = issue_o(g - 1);
-      if (!ok) {   // leaving early: let the instructions in flight finish before tensor memory is released
-        atomicOr(dv.status, kStatusConsumerTimeout);
-        umma_commit(&p->drain);
-        (void)mbar_wait_drain(&p->drain, 0);
-      }
+      });
     }
     __syncwarp();
   }

@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kTok = 128;                       // tokens of a step
 constexpr int kStepPages = kTok / kPageTokens;
-constexpr int kSoftWarps = 8, kTreeThreads = (kSoftWarps + 4) * 32;   // softmax warps; two more feed them, two have no part
+constexpr int kSoftWarps = 8, kTreeThreads = (kSoftWarps + 4) * 32;   // softmax warps; of four more, one copies, one issues the scores' products, one the outputs', and one has no part
 constexpr int kFlush = 16;                      // steps whose products add up in tensor memory
 constexpr int kItemSlots = 3;
 constexpr int kMaxStages = 4;                   // of K and of V
@@ -43,7 +43,7 @@ struct TreePipe {
   uint64_t o_read;                    // the accumulator has been read out
   uint64_t item_full[kItemSlots], item_empty[kItemSlots];
   uint64_t all_sync;                  // the softmax warps among themselves
-  uint64_t drain;
+  uint64_t drain[2];                  // of the two issuing warps
   uint32_t tmem_base;
   int abort_flag;
   uint32_t bad_v[2][kTreeMaxNodes / 32];   // [item parity]: drafts whose V holds a NaN or an infinity
@@ -58,9 +58,10 @@ __device__ __forceinline__ void tree_pipe_init(TreePipe* p, int nk, int nv) {
   mbar_init(&p->p_full, kSoftWarps);
   mbar_init(&p->p_done, 1);
   mbar_init(&p->o_read, kSoftWarps);
-  for (int s = 0; s < kItemSlots; ++s) { mbar_init(&p->item_full[s], 1); mbar_init(&p->item_empty[s], kSoftWarps + 1); }
+  for (int s = 0; s < kItemSlots; ++s) { mbar_init(&p->item_full[s], 1); mbar_init(&p->item_empty[s], kSoftWarps + 2); }
   mbar_init(&p->all_sync, kSoftWarps);
-  mbar_init(&p->drain, 1);
+  mbar_init(&p->drain[0], 1);
+  mbar_init(&p->drain[1], 1);
   p->abort_flag = 0;
   for (int k = 0; k < 2 * kTreeMaxNodes / 32; ++k) p->bad_v[0][k] = 0;
 }
@@ -133,6 +134,33 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar, int lane) {
 }
 
 __device__ __forceinline__ int head_steps(int len) { return (len + kTok - 1) / kTok; }
+
+// The warps that issue matrix instructions, one thread each: one the scores of a step, the other its output - two, because a
+// thread that did both had its waits and commits add up to more than the tensor cores' own time.  Each goes through the
+// items and their steps: step(g, i, it) issues global step g, the item's i-th, and returns false when a wait has run out; first(gi) comes
+// before an item's steps.
+template <typename First, typename Step>
+__device__ __forceinline__ void tree_issue(TreePipe* p, const DeviceView& dv, uint64_t* drain, First&& first, Step&& step) {
+  volatile int* abort_flag = &p->abort_flag;
+  bool ok = true;
+  unsigned g = 0;
+  for (unsigned gi = 0; ok; ++gi) {
+    const int slot = gi % kItemSlots;
+    ok = mbar_wait(&p->item_full[slot], (gi / kItemSlots) & 1, abort_flag);
+    if (!ok) break;
+    const TreeItem it = p->item[slot];
+    mbar_arrive(&p->item_empty[slot]);
+    if (it.head < 0) break;
+    ok = first(gi);
+    const int n = it.end - it.begin + it.draft;
+    for (int i = 0; i < n && ok; ++i, ++g) ok = step(g, i, n, it);
+  }
+  if (!ok) {   // leaving early: let the instructions in flight finish before tensor memory is released
+    atomicOr(dv.status, kStatusConsumerTimeout);
+    umma_commit(drain);
+    (void)mbar_wait_drain(drain, 0);
+  }
+}
 
 // Is node n node t or an ancestor of it?  (Straight from the parents: only where a draft holds a NaN or an infinity.)
 __device__ __noinline__ bool walk_sees(const int32_t* parent, int t, int n) {
