@@ -134,6 +134,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   }
   for (int c = tid; c < 2 * R; c += NT) ctl->top[0][c] = ordered(-CUDART_INF_F);
 
+  if (warp == SW && lane == 0) {
+    prefetch_map(&map_pool);
+    prefetch_map(&map_q);
+    prefetch_map(&map_k);
+    prefetch_map(&map_v);
+  }
+  cudaGridDependencySynchronize();   // (so far nothing in global memory has been touched)
   tree_find_span(dv, dv.state + (size_t)layer * dv.n_heads, tc, span, tile, p_tile);   // (scratch: the tile of P)
   tc_fence_before();
   __syncthreads();
@@ -318,8 +325,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         w_seed[k] = it.seed ? 1.f : 0.f;
       }
       // Sums of the weights of this thread's tokens, and this thread's dimension of the rows' outputs: the accumulator in
-      // tensor memory is added on every kFlush steps.  (The matrix unit truncates when it adds to the accumulator; over
-      // the thousand products of a long span that bias reached 1.6e-5 of the result, 4e-6 with sixteen steps.)
+      // tensor memory is added on every kFlush steps.
       // (With 64 columns to a thread the sum lives in local memory - its loops are not unrolled -, which costs less than
       // spilling what the steps use.)
       constexpr int kUnroll = LC == 2 ? 1 : NC / 16;
@@ -478,7 +484,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         tc_fence_before();
         warp_arrive(&p->s_empty[g & 1], lane);
         if (flush_now) flush();
-        // ---- sums; a weight is written as a bf16 head (its upper 16 bits) plus a bf16 remainder
+        // ---- sums; a weight is written as a bf16 head plus a bf16 remainder
         uint8_t* p_row = p_tile + tk * 128;
 #pragma unroll
         for (int c = 0; c < NC; c += 8) {
@@ -486,14 +492,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const int e = c + 2 * k;
-            const uint32_t b0 = v[e], b1 = v[e + 1];
-            const uint64_t w2 = f2_pack(__uint_as_float(b0), __uint_as_float(b1));
+            const float w0 = __uint_as_float(v[e]), w1 = __uint_as_float(v[e + 1]);
+            const uint64_t w2 = f2_pack(w0, w1);
             f2_unpack(f2_add(f2_pack(l[e], l[e + 1]), w2), l[e], l[e + 1]);
-            hi[k] = __byte_perm(b0, b1, 0x7632);
-            float r0, r1;
-            f2_unpack(f2_sub(w2, f2_pack(__uint_as_float(b0 & 0xffff0000u), __uint_as_float(b1 & 0xffff0000u))), r0, r1);
-            const __nv_bfloat162 r = __floats2bfloat162_rn(r0, r1);
-            lo[k] = *(const uint32_t*)&r;
+            split_weights(w2, w0, w1, hi[k], lo[k]);
           }
           const int ch = c0 + c, cl = R + ch;   // columns of heads and remainders in the 2R-column operand
           *(uint4*)(p_row + (ch >> 6) * (128 * kTok) + ((((ch & 63) >> 3) ^ (tk & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);

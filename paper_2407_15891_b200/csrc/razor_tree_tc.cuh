@@ -18,7 +18,10 @@ namespace {
 constexpr int kTok = 128;                       // tokens of a step
 constexpr int kStepPages = kTok / kPageTokens;
 constexpr int kSoftWarps = 8, kTreeThreads = (kSoftWarps + 4) * 32;   // softmax warps; of four more, one copies, one issues the scores' products, one the outputs', and one has no part
-constexpr int kFlush = 16;                      // steps whose products add up in tensor memory
+// Steps whose products add up in tensor memory before the softmax warps take the sum out.  The matrix unit truncates when it
+// adds to an accumulator: over a span of the 32K shape (147 steps, 1200 additions) that bias alone put 1.6e-5 of the
+// result's norm into it; every eight steps, with everything else, 3e-6.
+constexpr int kFlush = 8;
 constexpr int kItemSlots = 3;
 constexpr int kMaxStages = 4;                   // of K and of V
 constexpr int kSmemMax = 232448;
@@ -66,6 +69,9 @@ __device__ __forceinline__ void tree_pipe_init(TreePipe* p, int nk, int nv) {
   for (int k = 0; k < 2 * kTreeMaxNodes / 32; ++k) p->bad_v[0][k] = 0;
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
 __device__ __forceinline__ void tma5(void* dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, int c4, uint64_t* bar) {
   asm volatile(
       "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::
@@ -172,6 +178,16 @@ __device__ __noinline__ bool walk_sees(const int32_t* parent, int t, int n) {
   return t == n;
 }
 
+// A pair of weights as bf16 heads and bf16 remainders: together within 2^-18 of a weight (the head is off by at most 2^-9,
+// the remainder by 2^-9 of that); a head alone would put 2^-9 of a large weight's V row into the result.
+__device__ __forceinline__ void split_weights(uint64_t w2, float w0, float w1, uint32_t& heads, uint32_t& remainders) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(w0, w1);
+  heads = *(const uint32_t*)&h;
+  float r0, r1;
+  f2_unpack(f2_sub(w2, f2_pack(__uint_as_float(heads << 16), __uint_as_float(heads & 0xffff0000u))), r0, r1);
+  const __nv_bfloat162 r = __floats2bfloat162_rn(r0, r1);
+  remainders = *(const uint32_t*)&r;
+}
 // NaN and infinities in eight bf16 values to zero; returns whether there were any.
 __device__ __forceinline__ bool drop_non_finite(uint4& x) {
   uint32_t* w = (uint32_t*)&x;
@@ -430,18 +446,23 @@ cudaError_t tree_launch(Kernel kernel, int smem_bytes, const DeviceView& dv, lon
   // (set at every call: it costs less than a microsecond, and is kept per device)
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes);
   if (e != cudaSuccess) return e;
-  kernel<<<tc.n_spans * tc.n_tiles, kTreeThreads, smem_bytes, s>>>(dv, m.pool, m.q, m.k, m.v, layer, tc);
-  e = cudaGetLastError();
-  if (e != cudaSuccess || tc.n_spans == 1) return e;
+  // Both kernels are launched as programmatic dependents: barriers, tensor memory and descriptors are set up while the
+  // kernel before finishes, and everything else waits for it.
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(tc.n_spans, tc.n_tiles, R / 8);
-  cfg.blockDim = dim3(256);
-  cfg.stream = s;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(tc.n_spans * tc.n_tiles);
+  cfg.blockDim = dim3(kTreeThreads);
+  cfg.dynamicSmemBytes = smem_bytes;
+  cfg.stream = s;
   cfg.attrs = at;
   cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, kernel, dv, m.pool, m.q, m.k, m.v, layer, tc);
+  if (e != cudaSuccess || tc.n_spans == 1) return e;
+  cfg.gridDim = dim3(tc.n_spans, tc.n_tiles, R / 8);
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, tree_combine_kernel<D, R>, dv, tc);
 }
 

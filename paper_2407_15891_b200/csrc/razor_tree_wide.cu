@@ -17,7 +17,6 @@ namespace razor {
 namespace {
 
 constexpr int kRows = 128;
-constexpr int kWideFlush = 8;   // (two products of every weight go into one accumulator here: half as many steps for the same error)
 
 struct WideCtl {
   TreePipe pipe;
@@ -82,6 +81,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
+  if (warp == SW && lane == 0) {
+    prefetch_map(&map_pool);
+    prefetch_map(&map_q);
+    prefetch_map(&map_k);
+    prefetch_map(&map_v);
+  }
+  cudaGridDependencySynchronize();   // (so far nothing in global memory has been touched)
   tree_find_span(dv, dv.state + (size_t)layer * dv.n_heads, tc, span, tile, (uint8_t*)mask);   // (scratch: the mask)
   tc_fence_before();
   __syncthreads();
@@ -127,7 +133,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         tree_issue(p, dv, &p->drain[1], [](unsigned) { return true; }, [&](unsigned g, int i, int n, const TreeItem& it) {
           const int s = g % NV;
           const int left = it.draft && i == n - 1 ? n_nodes : it.st.len - (it.begin + i) * kTok;
-          const bool first = i % kWideFlush == 0;
+          const bool first = i % kFlush == 0;
           // the first product of an accumulator overwrites the one before, which must have been read out
           if (first && n_flush >= 1 && !mbar_wait(&p->o_read, (n_flush - 1) & 1, abort_flag)) return false;
           if (first) n_flush += 1;
@@ -220,8 +226,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         m_ref = fmaf(s, scale_log2, log2f((float)it.st.n_drop));
         w_seed = 1.f;
       }
-      // This thread's half of the row's output; the accumulator in tensor memory is added on every kWideFlush steps (the matrix
-      // unit truncates when it adds to the accumulator).
+      // This thread's half of the row's output; the accumulator in tensor memory is added on every kFlush steps.
       float acc[HD];
 #pragma unroll
       for (int c = 0; c < HD; ++c) acc[c] = 0.f;
@@ -245,7 +250,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         const bool draft = it.draft && i == n - 1;
         const int slot0 = (it.begin + i) * kTok;
         const int n_valid = (draft ? kTok : it.st.len - slot0) - half * HT;   // of this thread's tokens, from its first on
-        bool flush_now = i > 0 && i % kWideFlush == 0;
+        bool flush_now = i > 0 && i % kFlush == 0;
         ok = warp_wait(&p->s_full[g & 1], (g / 2) & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
@@ -280,7 +285,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             }
             return fmaxf(m0, m1) > kLag;
           };
-          // Weights, their sum, and their two halves for the product: a bf16 head (the upper 16 bits) plus a bf16 remainder,
+          // Weights, their sum, and their two halves for the product: a bf16 head plus a bf16 remainder,
           // column c of either holding the pair of tokens 2 c and 2 c + 1 (remainders replace the scores).  One loop: the
           // exponentials of a pair go to the special-function unit while the pair before is split.
           uint32_t hi[HT / 2];
@@ -290,14 +295,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
 #pragma unroll
             for (int c = 0; c < HT / 2; ++c) {
               const float w0 = fast_exp2(__uint_as_float(v[2 * c])), w1 = fast_exp2(__uint_as_float(v[2 * c + 1]));
-              const uint32_t b0 = __float_as_uint(w0), b1 = __float_as_uint(w1);
               const uint64_t w2 = f2_pack(w0, w1);
               sum2[c & 1] = f2_add(sum2[c & 1], w2);
-              hi[c] = __byte_perm(b0, b1, 0x7632);
-              float r0, r1;
-              f2_unpack(f2_sub(w2, f2_pack(__uint_as_float(b0 & 0xffff0000u), __uint_as_float(b1 & 0xffff0000u))), r0, r1);
-              const __nv_bfloat162 lo = __floats2bfloat162_rn(r0, r1);
-              v[c] = *(const uint32_t*)&lo;
+              split_weights(w2, w0, w1, hi[c], v[c]);
             }
             float a0, a1;
             f2_unpack(f2_add(sum2[0], sum2[1]), a0, a1);
@@ -340,7 +340,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               l *= f;
 #pragma unroll
               for (int c = 0; c < HD; ++c) acc[c] *= f;
-              if (i % kWideFlush != 0) {   // the accumulator holds products of this item
+              if (i % kFlush != 0) {   // the accumulator holds products of this item
                 tc_fence_after();
 #pragma unroll 1
                 for (int c = 0; c < HD; c += 16) {
