@@ -134,8 +134,14 @@ def _ptr(t) -> Optional[int]:
     return int(t)
 
 
+# (the current stream as a number, without the Python object around it where torch offers that: 3 us less a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device()) or None
         stream = torch.cuda.current_stream().cuda_stream
     return int(stream) or None
 
@@ -277,9 +283,8 @@ def razor_verify_tree(target: torch.Tensor, draft: Optional[torch.Tensor], token
     assert u_accept.shape == tokens.shape and u_sample.shape == (B,)
     assert tokens.is_contiguous() and parent.is_contiguous() and u_accept.is_contiguous() and u_sample.is_contiguous()
     assert tokens.device == dev and parent.device == dev and u_accept.device == dev and u_sample.device == dev
-    accepted = torch.empty((B,), dtype=torch.int32, device=dev)
-    path = torch.empty((B, T), dtype=torch.int32, device=dev)
-    token = torch.empty((B,), dtype=torch.int32, device=dev)
+    accepted, token, path = torch.empty(B * (T + 2), dtype=torch.int32, device=dev).split_with_sizes([B, B, B * T])
+    path = path.view(B, T)
     with _on(dev):
         q_ptr, q_b, q_row = (draft.data_ptr(), draft.stride(0), draft.stride(1)) if draft is not None else (None, 0, 0)
         _check(load().razor_verify_tree(target.data_ptr(), target.stride(0), target.stride(1), q_ptr, q_b, q_row, dt,
@@ -493,40 +498,44 @@ class RazorCache:
                     parent: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """q [B, T, Hq, D], k_draft, v_draft [B, T, Hkv, D] (strided over b and t), parent int32 [B, T] -> out fp32
         [B, T, Hq, D].  Rows of absent nodes are left as they are (zeros when `out` is not given)."""
-        T, dev = self._check_draft(k_draft, v_draft)
-        shape = (self.cfg.batch, T, self.cfg.n_q_heads, self.cfg.head_dim)
+        kv, dev = self._check_draft(k_draft, v_draft)
+        batch, T, cfg = kv[0], kv[1], self.cfg
+        shape = (batch, T, cfg.n_q_heads, kv[3])
         assert q.shape == shape and q.dtype is self.tdtype and q.device == dev and self._heads_contiguous(q)
-        assert parent.shape == shape[:2] and parent.dtype is torch.int32 and parent.is_contiguous() and parent.device == dev
+        assert parent.shape == (batch, T) and parent.dtype is torch.int32 and parent.is_contiguous() and parent.device == dev
         if out is None:
             out = torch.zeros(shape, dtype=torch.float32, device=dev)
-        assert out.shape == shape and out.dtype is torch.float32 and out.is_contiguous() and out.device == dev
+        else:
+            assert out.shape == shape and out.dtype is torch.float32 and out.is_contiguous() and out.device == dev
         with _on(dev):
-            razor_decode_attention_tree(self.handle, layer, q, q.stride(0), q.stride(1), k_draft, v_draft,
-                                        k_draft.stride(0), k_draft.stride(1), parent, T, out)
+            razor_decode_attention_tree(self.handle, layer, q, *q.stride()[:2], k_draft, v_draft, *k_draft.stride()[:2],
+                                        parent, T, out)
         return out
 
     def append_tree(self, layer: int, k_draft: torch.Tensor, v_draft: torch.Tensor, path: Optional[torch.Tensor],
                     n_accept) -> None:
         """Append the accepted path: rows path[b, :n_accept[b]] of k_draft, v_draft [B, T, Hkv, D].  path int32 [B, T]
         (or None: the first rows), n_accept [B] on the host."""
-        T, dev = self._check_draft(k_draft, v_draft)
-        assert path is None or (path.shape == (self.cfg.batch, T) and path.dtype is torch.int32 and path.is_contiguous()
+        (batch, T, _, _), dev = self._check_draft(k_draft, v_draft)
+        assert path is None or (path.shape == (batch, T) and path.dtype is torch.int32 and path.is_contiguous()
                                 and path.device == dev)
-        assert len(n_accept) == self.cfg.batch
+        assert len(n_accept) == batch
         with _on(dev):
-            razor_append_tree(self.handle, layer, k_draft, v_draft, k_draft.stride(0), k_draft.stride(1), path, T, n_accept)
+            razor_append_tree(self.handle, layer, k_draft, v_draft, *k_draft.stride()[:2], path, T, n_accept)
 
     @staticmethod
     def _heads_contiguous(x: torch.Tensor) -> bool:
         _, _, heads, dim = x.shape
-        return (dim == 1 or x.stride(3) == 1) and (heads == 1 or x.stride(2) == dim)
+        _, _, per_head, per_dim = x.stride()
+        return (dim == 1 or per_dim == 1) and (heads == 1 or per_head == dim)
 
     def _check_draft(self, k: torch.Tensor, v: torch.Tensor):
-        cfg, dev, shape = self.cfg, self.pool.device, k.shape
+        """-> (shape, device) of a round's K and V."""
+        cfg, dev, dtype, shape = self.cfg, self.pool.device, self.tdtype, k.shape
         assert len(shape) == 4 and shape == v.shape and k.stride() == v.stride() and self._heads_contiguous(k)
         assert shape[0] == cfg.batch and shape[2] == cfg.n_kv_heads and shape[3] == cfg.head_dim
-        assert k.dtype is self.tdtype and v.dtype is self.tdtype and k.device == dev and v.device == dev
-        return shape[1], dev
+        assert k.dtype is dtype and v.dtype is dtype and k.device == dev and v.device == dev
+        return shape, dev
 
     def export(self, layer: int, b: int, kv_head: int):
         """-> dict(kept_pos, K, V, mean_k, mean_v, sum_k, sum_v, n_drop) in logical order (device tensors)."""

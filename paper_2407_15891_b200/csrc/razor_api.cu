@@ -534,7 +534,10 @@ int compress_impl(razor_cache* c, int layer, const std::vector<SeqIn>& seqs, con
   // With the layer complete, its decode schedule is planned and sent to the device here, behind the compression
   // kernels, rather than in front of the layer's first decode launch, where the copies would sit between two
   // kernels that otherwise overlap.  (A failure here is not an error of the compression: the decode call plans again.)
-  if (L.n_done == cfg.batch) (void)ensure_schedule(c, layer, stream, true, cfg.n_q_heads / cfg.n_kv_heads);
+  // An empty layer (the start of a chunked prefill, or of ragged rounds) has nothing to plan yet.
+  bool any_token = false;
+  for (const HeadState& h : L.hs) any_token |= h.len > 0;
+  if (any_token && L.n_done == cfg.batch) (void)ensure_schedule(c, layer, stream, true, cfg.n_q_heads / cfg.n_kv_heads);
   return RAZOR_OK;
 }
 
