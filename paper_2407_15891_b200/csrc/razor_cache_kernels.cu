@@ -541,30 +541,57 @@ __global__ void __launch_bounds__(128) append_tree_kernel(DeviceView dv, int lay
   float accK[EPL], accV[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) accK[i] = accV[i] = 0.f;
-  for (int a = grp; a < n_tok; a += NGRP) {
-    // (an index that is no node of the tree reads the nearest node: never outside the buffers)
-    const int src = path ? min(max(path[(size_t)b * n_nodes + a], 0), n_nodes - 1) : a;
-    const size_t off = (size_t)b * stride_b + (size_t)src * stride_t + (size_t)g * D;
-    const uint4 kf = ((const uint4*)(k + off))[lir], vf = ((const uint4*)(v + off))[lir];
-    const AppendFate fate = append_fate(st, dv.n_sink, n_tok, a);
-    uint4 fk = kf, fv = vf;
-    bool fold = fate.slot < 0;
-    if (fate.slot >= 0) {
-      uint4* dst = (uint4*)(dv.pool + (size_t)pt[fate.slot >> 4] * dv.page_bytes + (size_t)(fate.slot & 15) * Geo::kRowBytes) + swz(fate.slot, lir);
-      if (fate.evicts_old) {
-        fold = true;
-        fk = dst[0];
-        fv = dst[kPageTokens * LPR];
-      }
-      dst[0] = kf;
-      dst[kPageTokens * LPR] = vf;
-    }
-    if (fold) {
-      float x[EPL], y[EPL];
-      Elem<T>::unpack(fk, x);
-      Elem<T>::unpack(fv, y);
+  constexpr int U = 4;   // rows of a thread group in flight
+  for (int a_first = grp; a_first < n_tok; a_first += NGRP * U) {
+    int src[U];
+    uint4 kf[U], vf[U], ok[U], ov[U];
+    uint4* dst[U];
+    bool fold[U];
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) { accK[i] += x[i]; accV[i] += y[i]; }
+    for (int u = 0; u < U; ++u) {
+      // (an index that is no node of the tree reads the nearest node: never outside the buffers)
+      const int a = min(a_first + u * NGRP, n_tok - 1);
+      src[u] = path ? min(max(path[(size_t)b * n_nodes + a], 0), n_nodes - 1) : a;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const size_t off = (size_t)b * stride_b + (size_t)src[u] * stride_t + (size_t)g * D;
+      kf[u] = ((const uint4*)(k + off))[lir];
+      vf[u] = ((const uint4*)(v + off))[lir];
+    }
+    // (no slot belongs to two tokens of a run, so a row that is evicted may be read before the others are written)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int a = a_first + u * NGRP;
+      dst[u] = nullptr;
+      fold[u] = false;
+      ok[u] = kf[u];
+      ov[u] = vf[u];
+      if (a < n_tok) {
+        const AppendFate fate = append_fate(st, dv.n_sink, n_tok, a);
+        fold[u] = fate.slot < 0 || fate.evicts_old;
+        if (fate.slot >= 0) {
+          dst[u] = (uint4*)(dv.pool + (size_t)pt[fate.slot >> 4] * dv.page_bytes + (size_t)(fate.slot & 15) * Geo::kRowBytes) + swz(fate.slot, lir);
+          if (fate.evicts_old) {
+            ok[u] = dst[u][0];
+            ov[u] = dst[u][kPageTokens * LPR];
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (dst[u]) {
+        dst[u][0] = kf[u];
+        dst[u][kPageTokens * LPR] = vf[u];
+      }
+      if (fold[u]) {
+        float x[EPL], y[EPL];
+        Elem<T>::unpack(ok[u], x);
+        Elem<T>::unpack(ov[u], y);
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) { accK[i] += x[i]; accV[i] += y[i]; }
+      }
     }
   }
   const int n_evict = n_tok - append_run_fits(st, dv.n_sink, n_tok);

@@ -375,11 +375,11 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCa
   {
     const int c = blockIdx.z * 8 + warp, r = tile * R + c;
     if (r >= tc.n_nodes * G) return;
-    if (dv.rec_ml[record(u.n_parts - 1) + c].y < 0.f) return;   // an absent node (the last part holds the tree)
+    const float2 last = __ldcg(&dv.rec_ml[record(u.n_parts - 1) + c]);
     float m = -CUDART_INF_F, l = 0.f;
     LaneVec<D> acc;
     acc.zero();
-    constexpr int U = 4;   // records in flight
+    constexpr int U = 8;   // records in flight
     for (int p0 = 0; p0 < u.n_parts; p0 += U) {
       float2 ml[U];
       LaneVec<D> o[U];
@@ -389,6 +389,7 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCa
         ml[i] = __ldcg(&dv.rec_ml[rec]);
         o[i].load_l2(dv.rec_o + rec * D, lane);
       }
+      if (last.y < 0.f) return;   // an absent node (the last part holds the tree)
 #pragma unroll
       for (int i = 0; i < U; ++i) {
         if (p0 + i >= u.n_parts) break;
