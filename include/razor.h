@@ -238,7 +238,7 @@ RAZOR_API int razor_decode_attention_multi(razor_cache_t* cache, int32_t layer, 
  * razor_append_tree: path device int32 [B, n_nodes]: node path[b][i] is the i-th token appended to sequence b, for
  * i < n_accept[b] (razor_verify_tree's path); NULL: the nodes 0, 1, .. themselves.  Entries outside [0, n_nodes) read
  * the nearest node.  n_accept host [B], 0 .. n_nodes (the host mirrors every length, so the counts are read back after
- * verification, once for all layers).
+ * verification, once for all layers; for the same reason a capturing stream is refused, INVALID_ARG).
  *
  * razor_verify_tree: target device [B, rows, vocab], dtype RAZOR_F32 or RAZOR_BF16, element strides target_stride_b and
  * target_stride_row: row 0 holds the target's probabilities for the token after the sequence, row 1 + t those for the

@@ -736,6 +736,10 @@ int razor_append_tree(razor_cache_t* c, int32_t layer, const void* k_draft, cons
     most = std::max(most, n_accept[b]);
   }
   if (most == 0) return RAZOR_OK;
+  // a replay would move the device's lengths and not the host's
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  RZ_CUDA(cudaStreamIsCapturing((cudaStream_t)stream, &capture));
+  if (capture != cudaStreamCaptureStatusNone) return RAZOR_E_INVALID_ARG;
   RZ_CUDA(launch_append_tree(c->dv, cfg.dtype, layer, k_draft, v_draft, kv_stride_b, kv_stride_t, path, n_nodes, n_accept,
                              cfg.batch, (cudaStream_t)stream));
   c->note_write(layer, razor_cache::kWriteBulk);
@@ -774,7 +778,7 @@ int razor_decode_attention_tree(razor_cache_t* c, int32_t layer, const void* q, 
   if (cfg.dtype == RAZOR_BF16)
     RZ_CUDA(launch_tree_mma(c->dv, c->pool_pages, layer, tc, rec_rows, c->n_sms, (cudaStream_t)stream));
   else
-    RZ_CUDA(launch_tree_rows(c->dv, cfg.dtype, layer, tc, longest, rec_rows, c->n_sms, (cudaStream_t)stream));
+    RZ_CUDA(launch_tree_rows(c->dv, layer, tc, longest, rec_rows, c->n_sms, (cudaStream_t)stream));
   c->last_writer_layer = -1;
   c->writes_since_decode.clear();   // an ordinary launch: everything before it has completed when it starts
   c->writes_overflow = false;

@@ -281,7 +281,7 @@ cudaError_t launch_tree_wide(const DeviceView& dv, long long pool_pages, int lay
 cudaError_t launch_tree_mma(const DeviceView& dv, long long pool_pages, int layer, const TreeCall& call, long long rec_rows,
                             int n_sms, cudaStream_t stream);
 // longest: tokens of the longest head (sizes the parts); rec_rows: rows the record area of the workspace has.
-cudaError_t launch_tree_rows(const DeviceView& dv, int dtype, int layer, const TreeCall& call, int longest, long long rec_rows,
+cudaError_t launch_tree_rows(const DeviceView& dv, int layer, const TreeCall& call, int longest, long long rec_rows,
                         int n_sms, cudaStream_t stream);
 // Appends n_accept[b] (host, [B]) rows of k, v to every sequence, picked by path (device [B, n_nodes] or NULL).
 cudaError_t launch_append_tree(const DeviceView& dv, int dtype, int layer, const void* k, const void* v, int64_t kv_stride_b,

@@ -1,11 +1,14 @@
-// Attention of a tree of drafted tokens over the compressed cache (a verify step of speculative decoding).
+// Attention of a tree of drafted tokens over an fp32 cache (the reference configurations; a bf16 cache runs on the
+// tensor-core kernels).
 //
 // A node attends to every kept token of its head, to the compensation token with its count (Eq. 5), and to itself and
 // its ancestors in the tree; the drafts' K and V are read from the caller's buffers and the cache stays as it is.
 // Query rows of a KV head: r = t * group + j for node t and query head j of the group.
 //
-// This file holds the CUDA-core kernel: groups of lanes that cover a row take the tokens of a part in turn, each
-// keeping the online softmax of eight query rows in registers; parts leave partial records that a combine kernel folds.
+// The tensor cores have no fp32 product, so this runs on the CUDA cores: groups of lanes that cover a row of 16 bytes a
+// lane take the tokens of a part in turn, each keeping the online softmax of eight query rows in registers (a K row is
+// then used eight times); parts leave partial records that a combine kernel folds.  What bounds it is the shuffles of the
+// dot products: about a hundred instructions a token and eight rows.
 #include <math_constants.h>
 
 #include <algorithm>
@@ -19,8 +22,9 @@ namespace {
 constexpr int kRowsThreads = 256;
 constexpr int kRowsTile = 8;    // query rows of a CTA
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kRowsThreads) tree_rows_kernel(DeviceView dv, int layer, TreeCall tc) {
+  using T = float;
   using Geo = RowGeom<T, D>;
   constexpr int LPR = Geo::kLpr, EPL = Geo::kEpl, NGRP = kRowsThreads / LPR;
   __shared__ TreeMask mask;
@@ -180,10 +184,10 @@ __global__ void __launch_bounds__(128) tree_rows_combine_kernel(DeviceView dv, T
   acc.store(tc.out + (((size_t)b * tc.n_nodes + t) * dv.n_kv_heads * G + (size_t)g * G + j) * D, lane);
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t rows_launch(const DeviceView& dv, int layer, const TreeCall& tc, cudaStream_t s) {
   const int rows = tc.n_nodes * dv.group;
-  tree_rows_kernel<T, D><<<dim3(dv.n_heads, (rows + kRowsTile - 1) / kRowsTile, tc.n_splits), kRowsThreads, 0, s>>>(dv, layer, tc);
+  tree_rows_kernel<D><<<dim3(dv.n_heads, (rows + kRowsTile - 1) / kRowsTile, tc.n_splits), kRowsThreads, 0, s>>>(dv, layer, tc);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || tc.n_splits == 1) return e;
   tree_rows_combine_kernel<D><<<dim3(dv.n_heads, (rows + 3) / 4), 128, 0, s>>>(dv, tc);
@@ -192,7 +196,7 @@ cudaError_t rows_launch(const DeviceView& dv, int layer, const TreeCall& tc, cud
 
 }  // namespace
 
-cudaError_t launch_tree_rows(const DeviceView& dv, int dtype, int layer, const TreeCall& call, int longest, long long rec_rows,
+cudaError_t launch_tree_rows(const DeviceView& dv, int layer, const TreeCall& call, int longest, long long rec_rows,
                         int n_sms, cudaStream_t s) {
   TreeCall tc = call;
   // Parts: about four CTAs per SM in all, at least 256 tokens to a part, no more than the records have rows for.
@@ -201,9 +205,7 @@ cudaError_t launch_tree_rows(const DeviceView& dv, int dtype, int layer, const T
   const long long room = rec_rows / (dv.n_heads * rows);
   tc.n_splits = (int)std::max(1LL, std::min({want, (longest + 255LL) / 256, room, 65535LL}));
   tc.rec_rows = (int)rows;
-  if (dtype == RAZOR_BF16)
-    return dv.head_dim == 128 ? rows_launch<__nv_bfloat16, 128>(dv, layer, tc, s) : rows_launch<__nv_bfloat16, 64>(dv, layer, tc, s);
-  return dv.head_dim == 128 ? rows_launch<float, 128>(dv, layer, tc, s) : rows_launch<float, 64>(dv, layer, tc, s);
+  return dv.head_dim == 128 ? rows_launch<128>(dv, layer, tc, s) : rows_launch<64>(dv, layer, tc, s);
 }
 
 }  // namespace razor

@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       for (int k = 0; k < LC; ++k) {
         const int r = min(row0 + my_c + k * LW, rows - 1);
         my_node[k] = r >> lg;
-        place[k] = (my_node[k] * dv.n_kv_heads * G + (r & (G - 1))) * D;
+        place[k] = my_node[k] * dv.n_kv_heads * G + (r & (G - 1));
       }
 
       // ---- the tree (items that hold its tokens; with ALiBi, all: a row's position is its node's depth)
@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         const float l_all = ((lp[0] + lp[NC]) + (lp[2 * NC] + lp[3 * NC])) + w_seed[k];
         const float inv = direct ? 1.f / l_all : 1.f;
         const bool is_node = (live[k] >> lane & 1) != 0;
-        table[c] = make_float4(inv, w_seed[k] * inv, __int_as_float(direct ? place[k] : c * D), __int_as_float(row0 + c0 + c < rows && (!direct || is_node)));
+        table[c] = make_float4(inv, w_seed[k] * inv, __int_as_float(direct ? place[k] : c), __int_as_float(row0 + c0 + c < rows && (!direct || is_node)));
         if (!direct && quarter == 0)   // (a negative sum marks an absent node's row for the combine kernel)
           dv.rec_ml[(size_t)it.rec * R + c0 + c] = make_float2(m_lane[k], it.draft && !is_node ? -1.f : l_all);
       }
@@ -572,7 +572,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float4 w = table[cb + e];
-            if (__float_as_int(w.w)) dst[__float_as_int(w.z)] = fmaf(w.y, v_hat, w.x * acc[cb + e]);
+            if (__float_as_int(w.w)) dst[(size_t)__float_as_int(w.z) * D] = fmaf(w.y, v_hat, w.x * acc[cb + e]);
           }
         }
         // The NaN and infinities that were taken out of the drafts' V reach the rows that see them.
@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               const float y = __bfloat162float(((const __nv_bfloat16*)tc.v)[(size_t)b * tc.kv_stride_b + (size_t)nd * tc.kv_stride_t + (size_t)g_kv * D + tk]);
               if (!(fabsf(y) < CUDART_INF_F)) bad += y;
             }
-            if (bad != 0.f && __float_as_int(table[c].w)) dst[__float_as_int(table[c].z)] += bad;   // (this thread's own store)
+            if (bad != 0.f && __float_as_int(table[c].w)) dst[(size_t)__float_as_int(table[c].z) * D] += bad;   // (this thread's own store)
           }
         }
       }

@@ -372,39 +372,37 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCa
   const int b = u.head / dv.n_kv_heads, g = u.head % dv.n_kv_heads;
   // the first part is the last item of its span, the others are the first of theirs
   auto record = [&](int p) { return ((size_t)((u.first_span + p) * tc.n_tiles + tile) * 2 + (p == 0 ? 1 : 0)) * R; };
-  {
-    const int c = blockIdx.z * 8 + warp, r = tile * R + c;
-    if (r >= tc.n_nodes * G) return;
-    const float2 last = __ldcg(&dv.rec_ml[record(u.n_parts - 1) + c]);
-    float m = -CUDART_INF_F, l = 0.f;
-    LaneVec<D> acc;
-    acc.zero();
-    constexpr int U = 8;   // records in flight
-    for (int p0 = 0; p0 < u.n_parts; p0 += U) {
-      float2 ml[U];
-      LaneVec<D> o[U];
+  const int c = blockIdx.z * 8 + warp, r = tile * R + c;
+  if (r >= tc.n_nodes * G) return;
+  const float2 last = __ldcg(&dv.rec_ml[record(u.n_parts - 1) + c]);
+  float m = -CUDART_INF_F, l = 0.f;
+  LaneVec<D> acc;
+  acc.zero();
+  constexpr int U = 8;   // records in flight
+  for (int p0 = 0; p0 < u.n_parts; p0 += U) {
+    float2 ml[U];
+    LaneVec<D> o[U];
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const size_t rec = record(min(p0 + i, u.n_parts - 1)) + c;
-        ml[i] = __ldcg(&dv.rec_ml[rec]);
-        o[i].load_l2(dv.rec_o + rec * D, lane);
-      }
-      if (last.y < 0.f) return;   // an absent node (the last part holds the tree)
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        if (p0 + i >= u.n_parts) break;
-        const float mn = fmaxf(m, ml[i].x), mu = mn == -CUDART_INF_F ? 0.f : mn;
-        const float c_old = fast_exp2(m - mu), c_new = fast_exp2(ml[i].x - mu);
-        l = l * c_old + ml[i].y * c_new;
-        acc.scale(c_old);
-        acc.fma(c_new, o[i]);
-        m = mn;
-      }
+    for (int i = 0; i < U; ++i) {
+      const size_t rec = record(min(p0 + i, u.n_parts - 1)) + c;
+      ml[i] = __ldcg(&dv.rec_ml[rec]);
+      o[i].load_l2(dv.rec_o + rec * D, lane);
     }
-    acc.scale(1.f / l);
-    const int t = r / G, j = r % G;
-    acc.store(tc.out + (((size_t)b * tc.n_nodes + t) * dv.n_kv_heads * G + (size_t)g * G + j) * D, lane);
+    if (last.y < 0.f) return;   // an absent node (the last part holds the tree)
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (p0 + i >= u.n_parts) break;
+      const float mn = fmaxf(m, ml[i].x), mu = mn == -CUDART_INF_F ? 0.f : mn;
+      const float c_old = fast_exp2(m - mu), c_new = fast_exp2(ml[i].x - mu);
+      l = l * c_old + ml[i].y * c_new;
+      acc.scale(c_old);
+      acc.fma(c_new, o[i]);
+      m = mn;
+    }
   }
+  acc.scale(1.f / l);
+  const int t = r / G, j = r % G;
+  acc.store(tc.out + (((size_t)b * tc.n_nodes + t) * dv.n_kv_heads * G + (size_t)g * G + j) * D, lane);
 }
 
 bool make_map(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4],

@@ -331,6 +331,48 @@ def test_refusals_leave_the_cache_usable():
     cache.close()
 
 
+@pytest.mark.parametrize("seed", range(14))
+def test_random_shapes(seed):
+    """Groups, head sizes, lengths, windows, sinks and trees at random: heads that spans cut anywhere, several tiles of rows,
+    more heads than SMs."""
+    rng = np.random.default_rng(7000 + seed)
+    group, D = int(rng.choice([1, 2, 4, 8])), int(rng.choice([64, 128]))
+    B, Hkv = (int(rng.integers(1, 4)), int(rng.integers(1, 5))) if seed % 3 else (9, 40 // group)
+    top = 40 if seed % 3 == 0 else int(rng.choice([30, 600, 5000]))
+    lens = [int(x) for x in rng.integers(0, top + 1, B)]
+    wins = [int(x) for x in rng.integers(0, max(1, top // 2) + 1, B)]
+    T = int(rng.integers(1, rz.TREE_MAX_NODES + 1))
+    w = synth.Workload("any", B, 1, Hkv * group, Hkv, D, "bf16", lens, wins, int(rng.integers(0, 20)), min(1, Hkv - 1), 0, seed)
+    use_comp = int(rng.integers(0, 4) > 0)
+    cache, K, V = _compress(w, shuffle=int(rng.integers(0, 3)), use_comp=use_comp)
+    q, k, v = _drafts(w, T, 3, fused=bool(rng.integers(0, 2)))
+    heads = {(b, g) for b in range(B) for g in range(Hkv)} if seed % 3 else {(b, int(rng.integers(Hkv))) for b in range(B)}
+    _check(w, cache, _refs(w, K, V), q, k, v, _random_parents(rng, B, T, chain=seed % 5 == 0, holes=True),
+           use_comp=bool(use_comp), heads=heads)
+    cache.close()
+
+
+def test_tree_attention_on_another_stream():
+    """Every call on a stream of its own, ordered by events: inputs written there just before, results read there."""
+    w = synth.Workload("stream", 2, 1, 8, 2, 128, "bf16", [1500, 77], [300, 50], 4, 1, 16, 29)
+    cache, K, V = _compress(w, max_new=16)
+    q, k, v = _drafts(w, 30, 1)
+    parent = torch.from_numpy(_random_parents(np.random.default_rng(1), 2, 30)).to(DEV)
+    want = cache.decode_tree(0, q, k, v, parent).clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        q2, k2, v2 = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+        for _ in range(20):
+            q2.zero_(), k2.zero_(), v2.zero_()
+            q2.copy_(q), k2.copy_(k), v2.copy_(v)
+            got = cache.decode_tree(0, q2, k2, v2, parent)
+        q2.fill_(float("nan"))       # (behind the call: it has read its queries)
+    side.synchronize()
+    assert torch.equal(got, want)
+    cache.close()
+
+
 # ----------------------------------------------------------------------------- append of a path
 @pytest.mark.parametrize("dtype,D,T,n_sink,windows", [
     ("bf16", 128, 6, 4, [60, 30, 3]), ("bf16", 64, 40, 4, [12, 100, 0]), ("f32", 128, 9, 0, [1, 2, 50]),
@@ -378,6 +420,24 @@ def test_path_entries_outside_the_tree_read_the_nearest_node():
         for n in (0, 2, 3, 3):
             ref.append(k[b, n, g].cpu(), v[b, n, g].cpu())
         check_head_state(cache, ref, 4, 50, bool(w.retrieval(0)[g]))
+    cache.close()
+
+
+def test_append_of_a_path_is_refused_on_a_capturing_stream():
+    """A replay would move the device's lengths and not the host's."""
+    w = synth.Workload("capture", 1, 1, 2, 2, 128, "bf16", [20], [50], 4, 1, 8, 4)
+    cache, K, V = _compress(w, max_new=8)
+    _, k, v = _drafts(w, 4, 1)
+    graph, x = torch.cuda.CUDAGraph(), torch.zeros(4, device=DEV)
+    with torch.cuda.graph(graph):
+        x.add_(1)
+        with pytest.raises(rz.RazorError) as e:
+            cache.append_tree(0, k, v, None, [2])
+    assert e.value.status == -1
+    graph.replay()
+    assert cache.export(0, 0, 0)["kept_pos"].numel() == 20
+    cache.append_tree(0, k, v, None, [2])
+    assert cache.export(0, 0, 0)["kept_pos"].numel() == 22
     cache.close()
 
 
@@ -441,7 +501,8 @@ def _verify_check(parent, p, q, tokens, u, r, dtype=torch.float32):
     (64, 1, 2, True, True, torch.float32), (40, 7, 5, True, False, torch.float32), (30, 12, 255, False, False, torch.float32),
     (30, 12, 256, True, False, torch.bfloat16), (20, 5, 257, True, True, torch.float32), (9, 128, 1000, True, False, torch.float32),
     (9, 128, 1000, False, False, torch.bfloat16), (5, 127, 2049, True, True, torch.bfloat16), (4, 7, 32000, True, True, torch.float32),
-    (3, 26, 50257, False, False, torch.float32), (2, 30, 128256, True, False, torch.float32), (3, 4, 1, True, False, torch.float32)])
+    (3, 26, 50257, False, False, torch.float32), (2, 30, 128256, True, False, torch.float32), (3, 4, 1, True, False, torch.float32),
+    (2, 9, 140001, True, False, torch.bfloat16), (40, 20, 2000, True, False, torch.bfloat16), (1, 2, 2200001, True, False, torch.float32)])
 def test_verification_matches_the_oracle(B, T, V, sampled, chain, dtype):
     rng = np.random.default_rng(B * 1000 + T)
     kept = _verify_check(*_verify_case(rng, B, T, V, sampled, chain=chain, holes=not chain), dtype=dtype)
@@ -455,9 +516,11 @@ def test_looked_up_drafts_that_are_often_right():
     assert kept >= 20
 
 
-def test_verification_on_the_borders():
+@pytest.mark.parametrize("copies", [1, 2])
+def test_verification_on_the_borders(copies):
     """u and r of zero, r of the largest fp32 below one, rows with long runs of zeros, one-hot rows, rows without any
-    weight, NaN and infinite entries, sibling tokens that repeat, tokens outside the vocabulary."""
+    weight, NaN and infinite entries, sibling tokens that repeat, tokens outside the vocabulary; rows kept in registers and,
+    with more sequences, streamed."""
     rng = np.random.default_rng(4)
     B, T, V = 12, 6, 700
     parent, p, q, tokens, u, r = _verify_case(rng, B, T, V, True)
@@ -474,11 +537,35 @@ def test_verification_on_the_borders():
     tokens[9] = tokens[9, 0]                   # siblings of one token
     tokens[10, ::2] = [-1, V, 1 << 30]
     parent[11] = [-1] * T
+    parent, p, q, tokens = (np.concatenate([x] * copies) for x in (parent, p, q, tokens))
+    B *= copies
     for rr in (0.0, 0.5, float(np.nextafter(np.float32(1), np.float32(0)))):
         for uu in (0.0, 0.3, float(np.nextafter(np.float32(1), np.float32(0)))):
             uv, rv = np.full((B, T), uu, np.float32), np.full(B, rr, np.float32)
             _verify_check(parent, p, q, tokens, uv, rv)
             _verify_check(parent, p, None, tokens, uv, rv)
+
+
+def test_verification_in_a_graph():
+    rng = np.random.default_rng(12)
+    cases = [_verify_case(rng, 5, 9, 3001, True) for _ in range(2)]
+    bufs = [torch.from_numpy(np.ascontiguousarray(x)).to(DEV) for x in cases[0]]
+    bufs[1:3] = [x.float() for x in bufs[1:3]]
+    call = lambda: rz.razor_verify_tree(bufs[1], bufs[2], bufs[3], bufs[0], bufs[4], bufs[5])  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = call()
+    for case in cases:
+        for buf, x in zip(bufs, case):
+            buf.copy_(torch.from_numpy(np.ascontiguousarray(x)))
+        graph.replay()
+        P, Q = to_f64(bufs[1]), to_f64(bufs[2])
+        for b in range(5):
+            path, token = orc.verify_tree(P[b], Q[b], case[3][b], case[0][b], case[4][b], case[5][b])
+            assert got["accepted"][b].item() == len(path) and got["token"][b].item() == token
+            assert got["path"][b].tolist() == path + [-1] * (9 - len(path))
 
 
 def test_verification_of_strided_rows():
@@ -534,4 +621,66 @@ def test_rounds_of_speculative_decoding():
                 check_head_state(cache, ref, 4, w.window[b], bool(retr[g]))
         moved += sum(counts)
     assert moved > 8 and cache.device_status() == 0
+    cache.close()
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_tree_calls_among_the_others(seed):
+    """Random sessions that mix the tree calls with single steps, long appends, rounds and decodes on one layer: each of
+    them goes on from the state the one before has left."""
+    rng = np.random.default_rng(400 + seed)
+    group, D, cap = int(rng.choice([1, 4])), int(rng.choice([64, 128])), 260
+    w = synth.Workload("mixed", 2, 1, 2 * group, 2, D, "bf16", [int(rng.integers(0, 400)), 90], [int(rng.integers(8, 120)), 30], 4, 1, cap, 800 + seed)
+    cache, K, V = _compress(w, max_new=cap, shuffle=seed)
+    refs, retr, scale = _refs(w, K, V, extra=cap), w.retrieval(0), 1 / math.sqrt(D)
+    used = [0, 0]
+
+    def appended(k, v, rows):
+        kb, vb = k.cpu(), v.cpu()
+        for (b, g), ref in refs.items():
+            for n in rows[b]:
+                ref.append(kb[b, n, g], vb[b, n, g])
+        for b in range(2):
+            used[b] += len(rows[b])
+
+    def expect(q, out):
+        qh, out = to_f64(q), to_f64(out)
+        for (b, g), ref in refs.items():
+            for j in range(group):
+                want = orc.multi_query_attention(qh[b, :, g * group + j], ref.K[:ref.n], ref.V[:ref.n], 4, w.window[b], bool(retr[g]), scale)
+                assert np.abs(out[b, :, g * group + j] - want).max() <= TOL_OUT["bf16"]
+
+    for step in range(24):
+        kind = rng.choice(["tree", "path", "step", "append", "round", "decode"])
+        T = int(rng.integers(1, 30))
+        q, k, v = _drafts(w, T, 1000 * seed + step)
+        if kind == "tree":
+            _check(w, cache, refs, q, k, v, _random_parents(rng, 2, T, holes=True))
+        elif kind == "path":
+            counts = [int(min(rng.integers(0, T + 1), cap - u)) for u in used]
+            path = np.full((2, T), -1, dtype=np.int32)
+            for b in range(2):
+                path[b, :counts[b]] = np.sort(rng.permutation(T)[:counts[b]])
+            cache.append_tree(0, k, v, torch.from_numpy(path).to(DEV), counts)
+            appended(k, v, [path[b, :counts[b]].tolist() for b in range(2)])
+        elif max(used) + T > cap:
+            continue
+        elif kind == "step":
+            out = cache.decode_step(0, k[:, 0].contiguous(), v[:, 0].contiguous(), q[:, 0].contiguous())
+            appended(k, v, [[0], [0]])
+            expect(q[:, :1], out[:, None])
+        elif kind == "append":
+            cache.append_many(0, k, v)
+            appended(k, v, [list(range(T))] * 2)
+        elif kind == "round":
+            T = min(T, 8)                          # (no window is shorter)
+            q, k, v = (x[:, :T].contiguous() for x in (q, k, v))
+            cache.append_many(0, k, v)
+            appended(k, v, [list(range(T))] * 2)
+            expect(q, cache.decode_multi(0, q))
+        elif min(ref.n for ref in refs.values()) > 0:
+            expect(q[:, :1], cache.decode(0, q[:, 0].contiguous())[:, None])
+        for (b, g), ref in refs.items():
+            check_head_state(cache, ref, 4, w.window[b], bool(retr[g]))
+    assert cache.device_status() == 0
     cache.close()
