@@ -1,9 +1,9 @@
-// Attention of a tree of drafted tokens over a bf16 cache, on the tensor cores.
+// Attention of a tree of drafted tokens over a bf16 cache, on the tensor cores: up to 64 query rows per KV head (nodes x
+// query heads of the group), and every ALiBi cache.
 //
-// The work per KV head is a short block of query rows (nodes x query heads of the group: from one to a thousand)
-// against a long stream of tokens, so the products are taken the other way round from a prompt's: TOKENS are the
-// 128-row operand and the query rows the narrow one,
-//     S^T = K Q^T          [128 tokens x R rows],     R = 32, 64 or 128 rows of a tile,
+// A short block of query rows stands against a long stream of tokens, so the products are taken the other way round from
+// a prompt's: TOKENS are the 128-row operand and the query rows the narrow one,
+//     S^T = K Q^T          [128 tokens x R rows],     R = 32, 64 or 128 (ALiBi) rows of a tile,
 //     O^T = V^T P^T        [D x R rows], contraction over the tokens,
 // and no lane of the tensor memory, no tensor-core row and no softmax thread stands idle when the rows are few.  A thread
 // owns one token, which also makes masks cheap: beyond the head's end, or which nodes see this draft, is decided per
@@ -12,17 +12,21 @@
 // (the V operand is read once for both), so that a weight keeps fp32-like accuracy; the two halves of the accumulator are
 // added at the end.
 //
+// What bounds it is the stream of pages out of HBM: 8 nodes on the 32K multi-head shape (8 x 32 heads, 1.40 GB of kept
+// pages) 210-214 us = 6.6 TB/s, 1.02 of the measured copy rate; 64 nodes 240 us (285 when the power cap holds the clock
+// near 1.5 GHz: then the softmax warps, 2500 cycles a step against the copies' 2640 at full clock, fall behind).
+//
 // Work: every head's slots in steps of 128 tokens plus one step for the tree's own tokens (their visibility is a bit mask
 // per thread).  All heads' steps are laid end to end and cut into equal spans, one per CTA; with several tiles of rows
 // the tiles of a span run in neighbouring CTAs at the same time, so that the cache comes out of HBM once and out of L2 for
-// the others.  The cut is made on the device from the head states - a scan over the heads, about a microsecond - so a
-// call costs the host nothing but the launch, and a captured graph follows the cache as it grows.  A head that a cut runs
-// through leaves one partial record per span; tree_combine_kernel folds them.
+// the others.  The cut is made on the device from the head states - a scan over the heads, two microseconds with the rest of
+// the set-up - so a call costs the host nothing but the launch, and a captured graph follows the cache as it grows.  A
+// head that a cut runs through leaves one partial record per span; tree_combine_kernel folds them.
 //
-// A CTA (one per SM): softmax warps (one per tensor-memory lane quarter and group of columns), a producer
-// warp (TMA: pages of the pool, whose rows are stored in the swizzle of the operand layout; drafts and queries through
-// maps of their own) and a warp that issues the matrix instructions.  S is double-buffered, so the scores of the next
-// step are computed during the softmax of this one.
+// A CTA (one per SM): eight softmax warps (one per tensor-memory lane quarter and group of columns), a producer warp (TMA:
+// pages of the pool, whose rows are stored in the swizzle of the operand layout; drafts and queries through maps of their
+// own) and two warps that issue the matrix instructions.  S is double-buffered, so the scores of the next step are
+// computed during the softmax of this one.
 //
 // The running maximum of a row is a reference that may lag: weights are 2^(s - m), floats, as exact at 2^20 as at one.  It
 // is moved (and the accumulator rescaled) only when a score outruns it by 2^kLag; the four warps of a column group agree on

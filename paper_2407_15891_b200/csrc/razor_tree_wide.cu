@@ -9,6 +9,12 @@
 // weights are two products against the same V.  Spans, producer, masks of hidden rows and the lagging maximum are the other
 // kernel's (so are the reasons for them); the two warps that share rows agree on a move of the maximum.
 //
+// What bounds it is the softmax warps: 2680 cycles a step, of which the exponentials and the splitting of the weights take
+// 1160 (one exponential per score is 1024 cycles of the special-function units by itself), loads of S and maxima 480, the
+// wait for the product before 380; the tensor cores work 1536.  64 nodes on the 128K grouped-query shape (256 rows against
+// 16 KV heads, 0.37 GB of kept pages): 150 us = 630 TFLOP/s over 4 D flops a (row, token) pair, 0.37 of the measured
+// cuBLAS rate (170-180 us under a continuous load's power cap); the other form took 214.
+//
 // Tensor memory (512 columns): S twice 128, P 64 columns of bf16 pairs for the heads and 64 for the remainders, O D.
 // ALiBi caches stay with the other kernel: there a token's position is one thread's, here it would be every thread's.
 #include "razor_tree_tc.cuh"
@@ -24,6 +30,7 @@ struct WideCtl {
   uint32_t need[4][2];        // [lane quarter][step parity]: step + 1 when a score outran the reference
   float top[2][2][kRows];     // [move parity][half]: a row's maximum in that half of a step
   float sum[2][kRows];        // [half]: a row's sum of weights
+  alignas(16) float turn[kSoftWarps][32][20];   // a warp's rows, on their way from a thread each to neighbouring lanes
 };
 
 template <int D>
@@ -419,27 +426,40 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         const float inv = direct ? 1.f / l_all : 1.f;
         if (!direct && half == 0)   // (a negative sum marks an absent node's row for the combine kernel)
           dv.rec_ml[(size_t)it.rec * kRows + row] = make_float2(m_ref, it.draft && !live ? -1.f : l_all);
-        if (direct ? live : is_row) {
-          float* dst = (direct ? tc.out + (((size_t)b * n_nodes + node) * dv.n_kv_heads * G + (size_t)g_kv * G + j) * D
-                               : dv.rec_o + ((size_t)it.rec * kRows + row) * D) + half * HD;
-          const float4* v_hat = (const float4*)(dv.comp_mean + hs * 2 * D + D + half * HD);
+        // Sixteen dimensions at a time through shared memory, so that four neighbouring lanes store a row's 64 bytes.
+        const size_t row_at = direct ? (((size_t)b * n_nodes + node) * dv.n_kv_heads * G + (size_t)g_kv * G + j) * D : ((size_t)it.rec * kRows + row) * D;
+        const uint32_t wanted = __ballot_sync(0xffffffffu, direct ? live : is_row);
+        float* all = direct ? tc.out : dv.rec_o;
+        const float4* v_hat = (const float4*)(dv.comp_mean + hs * 2 * D + D + half * HD);
+        float (*turn)[20] = ctl->turn[warp];   // (rows 80 bytes apart: 16-byte accesses of eight lanes hit different banks)
 #pragma unroll
-          for (int c = 0; c < HD; c += 4) {
-            const float4 vh = it.seed ? v_hat[c / 4] : make_float4(0.f, 0.f, 0.f, 0.f);
-            *(float4*)(dst + c) = make_float4(fmaf(w_seed, vh.x, acc[c]) * inv, fmaf(w_seed, vh.y, acc[c + 1]) * inv,
-                                              fmaf(w_seed, vh.z, acc[c + 2]) * inv, fmaf(w_seed, vh.w, acc[c + 3]) * inv);
+        for (int c = 0; c < HD; c += 16) {
+#pragma unroll
+          for (int e = 0; e < 16; e += 4) {
+            const float4 vh = it.seed ? v_hat[(c + e) / 4] : make_float4(0.f, 0.f, 0.f, 0.f);
+            *(float4*)&turn[lane][e] = make_float4(fmaf(w_seed, vh.x, acc[c + e]) * inv, fmaf(w_seed, vh.y, acc[c + e + 1]) * inv,
+                                                   fmaf(w_seed, vh.z, acc[c + e + 2]) * inv, fmaf(w_seed, vh.w, acc[c + e + 3]) * inv);
           }
-          // The NaN and infinities that were taken out of the drafts' V reach the rows that see them.
-          if (it.draft && (bad_v[0] | bad_v[1] | bad_v[2] | bad_v[3]) != 0) {
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int to = k * 8 + lane / 4;
+            const size_t at = __shfl_sync(0xffffffffu, row_at, to);
+            if (wanted >> to & 1) *(float4*)(all + at + half * HD + c + lane % 4 * 4) = *(const float4*)&turn[to][lane % 4 * 4];
+          }
+          __syncwarp();
+        }
+        // The NaN and infinities that were taken out of the drafts' V reach the rows that see them.
+        if (it.draft && (bad_v[0] | bad_v[1] | bad_v[2] | bad_v[3]) != 0 && (direct ? live : is_row)) {
+          float* dst = all + row_at + half * HD;   // (stored by lanes of this warp, before its last __syncwarp)
 #pragma unroll 1
-            for (int nd = 0; nd <= node; ++nd) {
-              if (!(bad_v[nd >> 5] >> (nd & 31) & 1) || !walk_sees(parent, node, nd)) continue;
-              const __nv_bfloat16* src = (const __nv_bfloat16*)tc.v + (size_t)b * tc.kv_stride_b + (size_t)nd * tc.kv_stride_t + (size_t)g_kv * D + half * HD;
+          for (int nd = 0; nd <= node; ++nd) {
+            if (!(bad_v[nd >> 5] >> (nd & 31) & 1) || !walk_sees(parent, node, nd)) continue;
+            const __nv_bfloat16* src = (const __nv_bfloat16*)tc.v + (size_t)b * tc.kv_stride_b + (size_t)nd * tc.kv_stride_t + (size_t)g_kv * D + half * HD;
 #pragma unroll 1
-              for (int c = 0; c < HD; ++c) {
-                const float y = __bfloat162float(src[c]);
-                if (!(fabsf(y) < CUDART_INF_F)) dst[c] += y;   // (this thread's own store)
-              }
+            for (int c = 0; c < HD; ++c) {
+              const float y = __bfloat162float(src[c]);
+              if (!(fabsf(y) < CUDART_INF_F)) dst[c] += y;
             }
           }
         }
