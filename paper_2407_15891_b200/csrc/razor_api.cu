@@ -9,6 +9,7 @@
 #include <vector>
 
 #include "razor_internal.h"
+#include "razor_spec.h"
 
 using namespace razor;
 
@@ -136,6 +137,7 @@ struct razor_cache {
   razor_config_t cfg;
   Layout lay;
   DeviceView dv;
+  TreeUnit* tree_units = nullptr;   // in the workspace
   long long pool_pages = 0, next_page = 0;
   int n_sms = 148;
   DecodeTuning tune{3, 80, 32, 0, 0, 0, 12};
@@ -169,6 +171,13 @@ struct razor_cache {
     last_writer_layer = layer;
     if (writes_since_decode.size() < 256) writes_since_decode.emplace_back(layer, kind);
     else writes_overflow = true;
+  }
+  // Whether a kernel that writes this layer may be in flight still, behind one that let its successor start at once.
+  bool may_be_written(int layer) const {
+    if (writes_overflow) return true;
+    for (const auto& w : writes_since_decode)
+      if (w.first == layer) return true;
+    return false;
   }
 };
 
@@ -260,7 +269,7 @@ int razor_cache_create(razor_cache_t** out, const razor_config_t* cfg, void* poo
   dv.alibi_slopes = (float*)(ws + lay.slopes);
   dv.round_items = (RoundItem*)(ws + lay.round_items);
   dv.round_units = (RoundUnit*)(ws + lay.round_units);
-  dv.tree_units = (TreeUnit*)(ws + lay.tree_units);
+  c->tree_units = (TreeUnit*)(ws + lay.tree_units);
   dv.alibi = 0;
   dv.n_heads = cfg->batch * cfg->n_kv_heads;
   dv.n_kv_heads = cfg->n_kv_heads;
@@ -645,7 +654,7 @@ int razor_append(razor_cache_t* c, int32_t layer, const void* k_new, const void*
   if (((uintptr_t)k_new | (uintptr_t)v_new) & 15) return RAZOR_E_MISALIGNED;
   LayerHost& L = c->layers[layer];
   if (L.appended_max() >= c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
-  const int early_reads = c->last_writer_layer != layer;
+  const int early_reads = c->last_writer_layer != layer && !c->may_be_written(layer);
   RZ_CUDA(launch_append(c->dv, c->cfg.dtype, layer, k_new, v_new, early_reads, (cudaStream_t)stream));
   c->note_write(layer, razor_cache::kWriteOneToken);
   // Host mirror of the kernel's state update.
@@ -771,7 +780,7 @@ int razor_decode_attention_tree(razor_cache_t* c, int32_t layer, const void* q, 
   int longest = 0;
   for (const HeadState& h : c->layers[layer].hs) longest = std::max(longest, h.len);
   TreeCall tc = {};
-  tc.q = q; tc.k = k_draft; tc.v = v_draft; tc.parent = parent; tc.out = out;
+  tc.q = q; tc.k = k_draft; tc.v = v_draft; tc.parent = parent; tc.out = out; tc.units = c->tree_units;
   tc.q_stride_b = q_stride_b; tc.q_stride_t = q_stride_t; tc.kv_stride_b = kv_stride_b; tc.kv_stride_t = kv_stride_t;
   tc.n_nodes = n_nodes;
   const long long rec_rows = (long long)c->lay.max_items * kMaxGroup;
@@ -779,8 +788,10 @@ int razor_decode_attention_tree(razor_cache_t* c, int32_t layer, const void* q, 
     RZ_CUDA(launch_tree_mma(c->dv, c->pool_pages, layer, tc, rec_rows, c->n_sms, (cudaStream_t)stream));
   else
     RZ_CUDA(launch_tree_rows(c->dv, layer, tc, longest, rec_rows, c->n_sms, (cudaStream_t)stream));
+  // The kernels wait for everything before them ahead of their first access to memory and let nothing start before
+  // they end: whatever is launched next finds all earlier writes complete.
   c->last_writer_layer = -1;
-  c->writes_since_decode.clear();   // an ordinary launch: everything before it has completed when it starts
+  c->writes_since_decode.clear();
   c->writes_overflow = false;
   return RAZOR_OK;
 }

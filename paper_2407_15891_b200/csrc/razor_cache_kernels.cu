@@ -1,6 +1,7 @@
 // Cache-building kernels: prefill-end compression (Algorithm 1, Eq. 4), decode-token
 // append with fold-on-evict, and the logical-order export used for snapshots and parity checks.
 #include "razor_common.cuh"
+#include "razor_spec.h"
 #include "razor_sync.cuh"
 
 namespace razor {

@@ -139,7 +139,6 @@ enum : int32_t {
 
 struct RoundItem;
 struct RoundUnit;
-struct TreeUnit;
 // Pointers into the caller's workspace, plus the dimensions the kernels need.
 struct DeviceView {
   uint8_t* pool;            // pages: [page][K rows | V rows][16][D]
@@ -163,7 +162,6 @@ struct DeviceView {
   float* alibi_slopes;      // [L][Hq]  ALiBi slopes l_h times log2(e); read only when alibi != 0
   RoundItem* round_items;   // [kRoundMaxItems]  work list of the round kernel's launch in flight
   RoundUnit* round_units;   // [kRoundMaxUnits]  its units in several parts
-  TreeUnit* tree_units;     // [kTreeMaxSpans]   heads that the running tree launch has cut
   int32_t alibi;            // 1: logits get - l_h (m - n) (Eq. 1), from razor_cache_set_alibi
   int32_t n_heads;          // B*Hkv
   int32_t n_kv_heads;
@@ -255,53 +253,6 @@ struct RoundJobs {
 };
 cudaError_t launch_round(const DeviceView& dv, long long pool_pages, int layer, const RoundJobs& jb, const void* q,
                          float* out, int n_sms, cudaStream_t stream);
-// ---- speculative decoding (razor_tree.cu, razor_verify.cu, append_tree_kernel in razor_cache_kernels.cu)
-constexpr int kTreeMaxNodes = RAZOR_TREE_MAX_NODES;
-// One razor_decode_attention_tree call.  Strides in elements, between sequences (b) and between nodes (t).
-struct TreeCall {
-  const void* q;
-  const void* k;
-  const void* v;
-  const int32_t* parent;   // device [B, n_nodes]
-  float* out;
-  int64_t q_stride_b, q_stride_t, kv_stride_b, kv_stride_t;
-  int32_t n_nodes;
-  // set by the launchers.  CUDA-core kernel: parts of a head's tokens, rows of a partial record.  Tensor-core kernel:
-  // tiles of query rows, spans of the heads' steps laid end to end, steps a span has at least.
-  int32_t n_splits, rec_rows, n_tiles, n_spans, min_span;
-};
-constexpr int kTreeMaxSpans = 1024;
-// A head that a span's cut runs through for the first time (listed under that span): its parts lie in the spans
-// first_span, first_span + 1, ..; n_parts = 0: nothing to fold.
-struct TreeUnit {
-  int32_t head, first_span, n_parts, pad;
-};
-cudaError_t launch_tree_wide(const DeviceView& dv, long long pool_pages, int layer, const TreeCall& call, long long rec_rows,
-                             int n_sms, cudaStream_t stream);   // more than 64 query rows per KV head, no ALiBi
-cudaError_t launch_tree_mma(const DeviceView& dv, long long pool_pages, int layer, const TreeCall& call, long long rec_rows,
-                            int n_sms, cudaStream_t stream);
-// longest: tokens of the longest head (sizes the parts); rec_rows: rows the record area of the workspace has.
-cudaError_t launch_tree_rows(const DeviceView& dv, int layer, const TreeCall& call, int longest, long long rec_rows,
-                        int n_sms, cudaStream_t stream);
-// Appends n_accept[b] (host, [B]) rows of k, v to every sequence, picked by path (device [B, n_nodes] or NULL).
-cudaError_t launch_append_tree(const DeviceView& dv, int dtype, int layer, const void* k, const void* v, int64_t kv_stride_b,
-                               int64_t kv_stride_t, const int32_t* path, int n_nodes, const int32_t* n_accept, int batch,
-                               cudaStream_t stream);
-struct VerifyCall {
-  const void* target;
-  const void* draft;       // NULL: the drafts were not drawn at random
-  const int32_t* tokens;
-  const int32_t* parent;
-  const float* u_accept;
-  const float* u_sample;
-  int32_t* n_accepted;
-  int32_t* path;
-  int32_t* next_token;
-  int64_t target_stride_b, target_stride_row, draft_stride_b, draft_stride_row;   // elements
-  int32_t batch, n_nodes, vocab;
-  int32_t seg_len;         // set by the launcher
-};
-cudaError_t launch_verify(const VerifyCall& call, int dtype, int n_sms, cudaStream_t stream);
 cudaError_t launch_wait_selftest(const DeviceView& dv, unsigned long long limit_ns, cudaStream_t stream);
 cudaError_t launch_export(const DeviceView& dv, int dtype, int layer, int head, int32_t* kept_pos, void* K, void* V,
                           float* mean_k, float* mean_v, float* sum_k, float* sum_v, cudaStream_t stream);

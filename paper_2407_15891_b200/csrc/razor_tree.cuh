@@ -4,7 +4,7 @@
 
 #include <stdint.h>
 
-#include "razor_internal.h"
+#include "razor_spec.h"
 
 namespace razor {
 

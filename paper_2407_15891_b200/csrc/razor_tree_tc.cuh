@@ -252,9 +252,9 @@ __device__ __forceinline__ void tree_find_span(const DeviceView& dv, const HeadS
       while (e + 1 < n && cut(e + 1) < u0 + w) e += 1;
       u.n_parts = e - span + 2;
     }
-    if (tile == 0) dv.tree_units[span] = u;
+    if (tile == 0) tc.units[span] = u;
   }
-  if (x0 >= x1 && tile == 0 && tid == 0) dv.tree_units[span] = TreeUnit{0, 0, 0, 0};
+  if (x0 >= x1 && tile == 0 && tid == 0) tc.units[span] = TreeUnit{0, 0, 0, 0};
 }
 
 // The producer warp: publishes the span's items and copies queries, pages and drafts into their rings.  A stage holds 128
@@ -366,7 +366,7 @@ __device__ __forceinline__ void tree_produce(const DeviceView& dv, const CUtenso
 template <int D, int R>
 __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCall tc) {
   cudaGridDependencySynchronize();
-  const TreeUnit u = dv.tree_units[blockIdx.x];
+  const TreeUnit u = tc.units[blockIdx.x];
   if (u.n_parts == 0) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tile = blockIdx.y, G = dv.group;
   const int b = u.head / dv.n_kv_heads, g = u.head % dv.n_kv_heads;

@@ -10,20 +10,21 @@
 // rejected children and S = 1 - their probabilities, no pass over the row needed.  Where the walk ends, the next token
 // is the first y whose running sum of W exceeds r sum(W).
 //
-// What bounds it: one read of the last node's rows (one more out of L2 for every further rejected child there), and a
-// chain of dependent steps.  So a sequence is a cluster of CTAs that share the row: each takes a contiguous run of
-// segments, keeps the segment sums in shared memory, and the CTAs trade one partial sum per pass through distributed
-// shared memory.  The walk itself runs in every CTA of the cluster on values fetched up front (one p and one q value
-// per node), with the same arithmetic on the same operands, so all of them take the same decisions without talking.
-// The token is found by the CTA whose run the threshold falls into: it scans its segment sums and reads one segment
-// again.  Everything is summed in 64 bits: a running sum in 32 would move the border between two tokens by more than
-// a rare token's whole probability.
+// What bounds it: for large batches one read of the last node's rows (64 chains of 7 over 128256 tokens, 66 MB in fp32: 27.4 us),
+// for small ones a chain of dependent steps (16 trees of 63: up to a dozen rejections in one sequence, 38-47 us).  So a
+// sequence is a cluster of CTAs that share the row: each takes a contiguous run of segments, keeps the segment sums in
+// shared memory, and the CTAs trade their warps' partial sums once a pass through distributed shared memory.  The walk
+// itself runs in every CTA of the cluster on values fetched up front (one p and one q value per node), with the same
+// arithmetic on the same operands, so all of them take the same decisions without talking.  The token is found by the
+// CTA whose run the threshold falls into: it scans its segment sums and reads one segment again.  Everything is summed in
+// 64 bits: a running sum in 32 would move the border between two tokens by more than a rare token's whole probability.
 #include <cooperative_groups.h>
 #include <math_constants.h>
 
 #include <algorithm>
 
 #include "razor_common.cuh"
+#include "razor_spec.h"
 
 namespace cg = cooperative_groups;
 
@@ -32,7 +33,7 @@ namespace {
 
 constexpr int kVerifyThreads = 512;
 constexpr int kVerifyWarps = kVerifyThreads / 32;
-constexpr int kVerifyCluster = 8;       // CTAs that share a sequence (the portable cluster size)
+constexpr int kVerifyCluster = 8;       // most CTAs that share a sequence (the portable cluster size)
 constexpr int kMaxSegs = 1024;          // segments of a CTA's share of a row
 constexpr int kUnroll = 8;              // neighbouring values of a row that a lane takes at a time
 constexpr int kSegUnit = 32 * kUnroll;  // a segment is a multiple of this
@@ -69,6 +70,9 @@ __device__ __forceinline__ void load_row(const __nv_bfloat16* row, int i, int hi
 // max(x, 0) by the sign bit: the library's maximum of two doubles runs at a quarter of an addition's rate.  (x is no NaN.)
 __device__ __forceinline__ double at_least_0(double x) { return __double2hiint(x) < 0 ? 0.0 : x; }
 
+constexpr int kParts = kVerifyCluster * kVerifyWarps;
+static_assert(kParts == 128 && kUnroll == 8, "four sums to a lane; eight values to a tree of sums");
+
 struct VerifySmem {
   double seg_sum[kMaxSegs];
   double part[2][kVerifyCluster][kVerifyWarps];   // every warp's sum of every CTA's share, written by its owner; passes take turns
@@ -104,8 +108,6 @@ __device__ __forceinline__ double running_sum(double x, int lane) {
 
 // kKeep: a row's values stay in registers while its node is the current one, so that every rejected child after the
 // first costs no memory access (needs rows of at most kVerifyCluster * kVerifyWarps * kKeepSegs units, 131072 values).
-constexpr int kParts = kVerifyCluster * kVerifyWarps;
-static_assert(kParts == 128 && kUnroll == 8, "four sums to a lane; eight values to a tree of sums");
 // The CTAs' sums from their warps': lane r < kVerifyCluster gets CTA r's, and all lanes the whole (in the same order in
 // every CTA of the cluster).
 __device__ __forceinline__ double cta_part(const double (*part)[kVerifyWarps], int lane) {
@@ -143,6 +145,7 @@ __global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(V
     sm.p_child[t] = ok ? raw_prob(target + (size_t)(a + 1) * vc.target_stride_row + x) : 0.f;
     sm.q_child[t] = ok && draft ? raw_prob(draft + (size_t)(a + 1) * vc.draft_stride_row + x) : 1.f;
   }
+  for (int i = tid; i < 2 * kParts; i += kVerifyThreads) (&sm.part[0][0][0])[i] = 0.0;   // (a smaller cluster's missing CTAs add nothing)
   // this CTA's share of a row: n_segs segments of seg_len values from segment seg0 on
   const int seg_len = vc.seg_len, all_segs = (V + seg_len - 1) / seg_len;
   const int per = (all_segs + n_ranks - 1) / n_ranks;
@@ -372,16 +375,20 @@ __global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(V
 
 cudaError_t launch_verify(const VerifyCall& call, int dtype, int n_sms, cudaStream_t stream) {
   VerifyCall vc = call;
+  // CTAs to a sequence: as many as are resident at once (two to an SM), so that a large batch does not run in a wave and a
+  // bit (64 sequences over 128256 tokens, one pass each: 8 to a sequence 33.6 us, 4 27.4 us).
+  int ranks = kVerifyCluster;
+  while (ranks > 1 && (long long)vc.batch * ranks > 2LL * n_sms) ranks /= 2;
   // segments: at most kMaxSegs to a CTA
   const long long units = ((long long)vc.vocab + kSegUnit - 1) / kSegUnit;
-  vc.seg_len = (int)(kSegUnit * ((units + (long long)kVerifyCluster * kMaxSegs - 1) / ((long long)kVerifyCluster * kMaxSegs)));
+  vc.seg_len = (int)(kSegUnit * ((units + (long long)ranks * kMaxSegs - 1) / ((long long)ranks * kMaxSegs)));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)vc.batch * kVerifyCluster);
+  cfg.gridDim = dim3((unsigned)vc.batch * ranks);
   cfg.blockDim = dim3(kVerifyThreads);
   cfg.stream = stream;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = kVerifyCluster;
+  at[0].val.clusterDim.x = ranks;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;

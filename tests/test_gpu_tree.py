@@ -373,6 +373,12 @@ def test_tree_attention_on_another_stream():
     cache.close()
 
 
+@pytest.mark.parametrize("B", [37, 38, 75, 149, 300, 700])
+def test_verification_of_large_batches(B):
+    """More sequences than CTAs fit at eight to a sequence, then at four, two and one."""
+    assert _verify_check(*_verify_case(np.random.default_rng(B), B, 4, 700, True)) > 0
+
+
 # ----------------------------------------------------------------------------- append of a path
 @pytest.mark.parametrize("dtype,D,T,n_sink,windows", [
     ("bf16", 128, 6, 4, [60, 30, 3]), ("bf16", 64, 40, 4, [12, 100, 0]), ("f32", 128, 9, 0, [1, 2, 50]),
@@ -407,6 +413,40 @@ def test_append_of_a_path_is_as_many_single_appends(dtype, D, T, n_sink, windows
         for (b, g), ref in refs.items():
             ref.append(k1[b, 0, g].cpu(), v1[b, 0, g].cpu())
             check_head_state(cache, ref, n_sink, windows[b], bool(retr[g]))
+    cache.close()
+
+
+def test_layers_appended_to_in_turn_without_a_decode_between():
+    """Paths and single tokens appended to two layers in turn, with nothing in between that waits: an append may start
+    while the one before is in flight, and has to find what the last append of its own layer left."""
+    w = synth.Workload("turn", 16, 2, 8, 8, 128, "bf16", [100] * 16, [20] * 16, 4, 1, 200, 41)
+    cache = make_cache(w, max_new=200)
+    heads = [(0, 0), (7, 3), (15, 7), (15, 0)]
+    refs = []
+    for layer in range(2):
+        K, V = synth.make_dense_kv(w, layer, DEV)
+        cache.compress(layer, K, V, w.ctx_len, w.retrieval(layer), w.window)
+        refs.append({(b, g): HeadRef(layer, b, g, K[b, g], V[b, g], 100, 200) for b, g in heads})
+    drafts = [_drafts(w, 12, 300 + i) for i in range(2)]
+    ones = [[x[:, i].contiguous() for x in drafts[0][1:]] for i in range(3)]
+    counts = [12, 5] * 8
+    torch.cuda.synchronize()
+    for _ in range(6):
+        cache.append_tree(0, drafts[0][1], drafts[0][2], None, counts)
+        for i in range(3):
+            cache.append(1, *ones[i])
+            cache.append(0, *ones[i])
+        cache.append_tree(1, drafts[1][1], drafts[1][2], None, counts)
+    for layer in range(2):
+        kv = [x.cpu() for x in drafts[layer][1:]]
+        for (b, g), ref in refs[layer].items():
+            for _ in range(6):
+                path = [(kv[0][b, i, g], kv[1][b, i, g]) for i in range(counts[b])]
+                single = [(ones[i][0][b, g].cpu(), ones[i][1][b, g].cpu()) for i in range(3)]
+                for k, v in (path + single if layer == 0 else single + path):
+                    ref.append(k, v)
+            check_head_state(cache, ref, 4, 20, bool(w.retrieval(layer)[g]))
+    assert cache.device_status() == 0
     cache.close()
 
 
