@@ -777,8 +777,6 @@ int razor_decode_attention_tree(razor_cache_t* c, int32_t layer, const void* q, 
   rc = check_draft_strides(q_stride_b, q_stride_t, (int64_t)cfg.n_q_heads * cfg.head_dim, cfg.batch, n_nodes, esz(cfg));
   if (!rc) rc = check_draft_strides(kv_stride_b, kv_stride_t, (int64_t)cfg.n_kv_heads * cfg.head_dim, cfg.batch, n_nodes, esz(cfg));
   if (rc) return rc;
-  int longest = 0;
-  for (const HeadState& h : c->layers[layer].hs) longest = std::max(longest, h.len);
   TreeCall tc = {};
   tc.q = q; tc.k = k_draft; tc.v = v_draft; tc.parent = parent; tc.out = out; tc.units = c->tree_units;
   tc.q_stride_b = q_stride_b; tc.q_stride_t = q_stride_t; tc.kv_stride_b = kv_stride_b; tc.kv_stride_t = kv_stride_t;
@@ -787,7 +785,7 @@ int razor_decode_attention_tree(razor_cache_t* c, int32_t layer, const void* q, 
   if (cfg.dtype == RAZOR_BF16)
     RZ_CUDA(launch_tree_mma(c->dv, c->pool_pages, layer, tc, rec_rows, c->n_sms, (cudaStream_t)stream));
   else
-    RZ_CUDA(launch_tree_rows(c->dv, layer, tc, longest, rec_rows, c->n_sms, (cudaStream_t)stream));
+    RZ_CUDA(launch_tree_rows(c->dv, layer, tc, rec_rows, c->n_sms, (cudaStream_t)stream));
   // The kernels wait for everything before them ahead of their first access to memory and let nothing start before
   // they end: whatever is launched next finds all earlier writes complete.
   c->last_writer_layer = -1;

@@ -24,17 +24,15 @@ struct TreeCall {
   TreeUnit* units;         // [kTreeMaxSpans] in the workspace: heads that the launch has cut
   int64_t q_stride_b, q_stride_t, kv_stride_b, kv_stride_t;
   int32_t n_nodes;
-  // set by the launchers.  CUDA-core kernel: parts of a head's tokens, rows of a partial record.  Tensor-core kernel:
-  // tiles of query rows, spans of the heads' steps laid end to end, steps a span has at least.
-  int32_t n_splits, rec_rows, n_tiles, n_spans, min_span;
+  // set by the launchers: tiles of query rows, spans of the heads' steps laid end to end, steps a span has at least
+  int32_t n_tiles, n_spans, min_span;
 };
 cudaError_t launch_tree_wide(const DeviceView& dv, long long pool_pages, int layer, const TreeCall& call, long long rec_rows,
                              int n_sms, cudaStream_t stream);   // more than 64 query rows per KV head, no ALiBi
 cudaError_t launch_tree_mma(const DeviceView& dv, long long pool_pages, int layer, const TreeCall& call, long long rec_rows,
                             int n_sms, cudaStream_t stream);
-// longest: tokens of the longest head (sizes the parts); rec_rows: rows the record area of the workspace has.
-cudaError_t launch_tree_rows(const DeviceView& dv, int layer, const TreeCall& call, int longest, long long rec_rows,
-                             int n_sms, cudaStream_t stream);
+cudaError_t launch_tree_rows(const DeviceView& dv, int layer, const TreeCall& call, long long rec_rows, int n_sms,
+                             cudaStream_t stream);   // fp32 caches
 // Appends n_accept[b] (host, [B]) rows of k, v to every sequence, picked by path (device [B, n_nodes] or NULL).
 cudaError_t launch_append_tree(const DeviceView& dv, int dtype, int layer, const void* k, const void* v, int64_t kv_stride_b,
                                int64_t kv_stride_t, const int32_t* path, int n_nodes, const int32_t* n_accept, int batch,

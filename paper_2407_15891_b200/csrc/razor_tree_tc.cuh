@@ -257,6 +257,26 @@ __device__ __forceinline__ void tree_find_span(const DeviceView& dv, const HeadS
   if (x0 >= x1 && tile == 0 && tid == 0) tc.units[span] = TreeUnit{0, 0, 0, 0};
 }
 
+// The next item of a span that has `todo` steps left, from step y of a head on; takes its steps off todo.
+__device__ __forceinline__ TreeItem tree_item(const DeviceView& dv, int head, int y, long long& todo, const HeadState& st) {
+  TreeItem it;
+  it.head = todo > 0 ? head : -1;
+  it.begin = it.end = it.draft = it.seed = 0;
+  it.rec = -1;
+  it.st = st;
+  const int steps = head_steps(st.len);
+  if (todo > 0) {
+    const int y1 = (int)min((long long)(steps + 1), y + todo);
+    it.begin = y;
+    it.end = min(y1, steps);
+    it.draft = y1 == steps + 1;
+    it.seed = y == 0 && dv.use_comp && st.n_drop > 0 && st.window >= 0;
+    if (y > 0 || !it.draft) it.rec = ((int)blockIdx.x * 2 + (y > 0 ? 0 : 1));
+    todo -= y1 - y;
+  }
+  return it;
+}
+
 // The producer warp: publishes the span's items and copies queries, pages and drafts into their rings.  A stage holds 128
 // tokens of K or of V as [octet][64-element half][8 tokens][128 B], each KB in the 128-byte swizzle: for the matrix unit
 // the tokens are rows of a K-major operand or the contraction index of an MN-major one.
@@ -276,21 +296,7 @@ __device__ __forceinline__ void tree_produce(const DeviceView& dv, const CUtenso
   bool ok = true;
   HeadState st = sp.st;
   for (;; ++gi) {
-    TreeItem it;
-    it.head = todo > 0 ? head : -1;
-    it.begin = it.end = it.draft = it.seed = 0;
-    it.rec = -1;
-    it.st = st;
-    const int steps = head_steps(st.len);
-    if (todo > 0) {
-      const int y1 = (int)min((long long)(steps + 1), y + todo);
-      it.begin = y;
-      it.end = min(y1, steps);
-      it.draft = y1 == steps + 1;
-      it.seed = y == 0 && dv.use_comp && st.n_drop > 0 && st.window >= 0;
-      if (y > 0 || !it.draft) it.rec = ((int)blockIdx.x * 2 + (y > 0 ? 0 : 1));
-      todo -= y1 - y;
-    }
+    const TreeItem it = tree_item(dv, head, y, todo, st);
     const int slot = gi % kItemSlots;
     if (gi >= kItemSlots) ok = warp_wait(&p->item_empty[slot], (gi / kItemSlots - 1) & 1, abort_flag);
     if (!ok) break;
@@ -405,7 +411,7 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCa
   acc.store(tc.out + (((size_t)b * tc.n_nodes + t) * dv.n_kv_heads * G + (size_t)g * G + j) * D, lane);
 }
 
-bool make_map(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4],
+[[maybe_unused]] bool make_map(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4],
               const cuuint32_t (&box)[5], CUtensorMapSwizzle swizzle) {
   const EncodeTiledFn encode = encode_tiled_fn();
   const cuuint32_t es[5] = {1, 1, 1, 1, 1};
@@ -417,9 +423,16 @@ bool make_map(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[5], c
 struct TreeMaps {
   CUtensorMap pool, q, k, v;
 };
-// Tensor maps of a call, and how it is cut: tiles of R rows, spans (at most one CTA to an SM).
+// How a call is cut: tiles of R rows, spans (at most one CTA to an SM).
+template <int R>
+void tree_cut(const DeviceView& dv, long long rec_rows, int n_sms, TreeCall& tc) {
+  tc.n_tiles = (int)(((long long)tc.n_nodes * dv.group + R - 1) / R);
+  tc.n_spans = std::max(1, std::min({n_sms / tc.n_tiles, kTreeMaxSpans, (int)(rec_rows / (2LL * R * tc.n_tiles))}));
+  tc.min_span = 4;
+}
+// Tensor maps of a call.
 template <int D, int R>
-bool tree_prepare(const DeviceView& dv, long long pool_pages, long long rec_rows, int n_sms, TreeCall& tc, TreeMaps& m) {
+bool tree_maps(const DeviceView& dv, long long pool_pages, const TreeCall& tc, TreeMaps& m) {
   constexpr cuuint64_t RB = D * 2;
   constexpr cuuint32_t H = D / 64;
   const cuuint64_t B = (cuuint64_t)(dv.n_heads / dv.n_kv_heads), T = (cuuint64_t)tc.n_nodes, G = (cuuint64_t)dv.group;
@@ -427,26 +440,19 @@ bool tree_prepare(const DeviceView& dv, long long pool_pages, long long rec_rows
   // (a stride that separates nothing may be anything in the call, and must be a legal one in the map)
   const cuuint64_t qt = T > 1 ? (cuuint64_t)tc.q_stride_t * 2 : Hq * RB, kt = T > 1 ? (cuuint64_t)tc.kv_stride_t * 2 : Hkv * RB;
   const cuuint64_t qb = B > 1 ? (cuuint64_t)tc.q_stride_b * 2 : Hq * RB, kb = B > 1 ? (cuuint64_t)tc.kv_stride_b * 2 : Hkv * RB;
-  tc.n_tiles = (int)((T * G + R - 1) / R);
-  tc.n_spans = std::max(1, std::min({n_sms / tc.n_tiles, kTreeMaxSpans, (int)(rec_rows / (2LL * R * tc.n_tiles))}));
-  tc.min_span = 4;
   // pool: eight tokens of a 64-element half are 1 KB in the stage; [octet][half] as the operand layout has them
   return make_map(&m.pool, dv.pool, {64, 8, H, 2, 2 * (cuuint64_t)pool_pages}, {RB, 128, 8 * RB, 16 * RB}, {64, 8, H, 2, 1}, CU_TENSOR_MAP_SWIZZLE_NONE) &&
          make_map(&m.q, tc.q, {64, Hq, T, H, B}, {RB, qt, 128, qb}, {64, (cuuint32_t)G, (cuuint32_t)(R / G), 1, 1}, CU_TENSOR_MAP_SWIZZLE_128B) &&
          make_map(&m.k, tc.k, {64, T, H, Hkv, B}, {kt, 128, RB, kb}, {64, 8, H, 1, 1}, CU_TENSOR_MAP_SWIZZLE_128B) &&
          make_map(&m.v, tc.v, {64, T, H, Hkv, B}, {kt, 128, RB, kb}, {64, 8, H, 1, 1}, CU_TENSOR_MAP_SWIZZLE_128B);
 }
-template <int D, int R, typename Kernel>
-cudaError_t tree_launch(Kernel kernel, int smem_bytes, const DeviceView& dv, long long pool_pages, int layer, const TreeCall& call,
-                        long long rec_rows, int n_sms, cudaStream_t s) {
-  TreeCall tc = call;
-  TreeMaps m;
-  if (!tree_prepare<D, R>(dv, pool_pages, rec_rows, n_sms, tc, m)) return cudaErrorInvalidValue;
+// The kernel over all spans and tiles, and the one that folds its records.  Both are launched as programmatic dependents:
+// barriers, tensor memory and descriptors are set up while the kernel before finishes, and everything else waits for it.
+template <int D, int R, typename... P, typename... A>
+cudaError_t tree_run(void (*kernel)(P...), int smem_bytes, const DeviceView& dv, const TreeCall& tc, cudaStream_t s, A... args) {
   // (set at every call: it costs less than a microsecond, and is kept per device)
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes);
   if (e != cudaSuccess) return e;
-  // Both kernels are launched as programmatic dependents: barriers, tensor memory and descriptors are set up while the
-  // kernel before finishes, and everything else waits for it.
   cudaLaunchConfig_t cfg = {};
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -457,12 +463,21 @@ cudaError_t tree_launch(Kernel kernel, int smem_bytes, const DeviceView& dv, lon
   cfg.stream = s;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, kernel, dv, m.pool, m.q, m.k, m.v, layer, tc);
+  e = cudaLaunchKernelEx(&cfg, kernel, args...);
   if (e != cudaSuccess || tc.n_spans == 1) return e;
   cfg.gridDim = dim3(tc.n_spans, tc.n_tiles, R / 8);
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, tree_combine_kernel<D, R>, dv, tc);
+}
+template <int D, int R, typename Kernel>
+cudaError_t tree_launch(Kernel kernel, int smem_bytes, const DeviceView& dv, long long pool_pages, int layer, const TreeCall& call,
+                        long long rec_rows, int n_sms, cudaStream_t s) {
+  TreeCall tc = call;
+  tree_cut<R>(dv, rec_rows, n_sms, tc);
+  TreeMaps m;
+  if (!tree_maps<D, R>(dv, pool_pages, tc, m)) return cudaErrorInvalidValue;
+  return tree_run<D, R>(kernel, smem_bytes, dv, tc, s, dv, m.pool, m.q, m.k, m.v, layer, tc);
 }
 
 }  // namespace

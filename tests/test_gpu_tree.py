@@ -219,9 +219,10 @@ def test_what_a_node_does_not_see_cannot_reach_it(dtype, group, D, more):
     cache.close()
 
 
-def test_a_long_context_in_many_parts_is_repeatable():
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_long_context_in_many_parts_is_repeatable(dtype):
     """32K tokens of few heads: every head is cut into parts.  Against the oracle, and twice the same bits."""
-    w = synth.Workload("long", 2, 1, 8, 2, 128, "bf16", [32771, 20000], [5000, 3000], 4, 1, 0, 19)
+    w = synth.Workload("long", 2, 1, 8, 2, 128, dtype, [32771, 20000], [5000, 3000], 4, 1, 0, 19)
     cache, K, V = _compress(w)
     q, k, v = _drafts(w, 24, 10)
     parent = _random_parents(np.random.default_rng(1), 2, 24)
@@ -332,7 +333,8 @@ def test_refusals_leave_the_cache_usable():
 
 
 @pytest.mark.parametrize("seed", range(14))
-def test_random_shapes(seed):
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_random_shapes(dtype, seed):
     """Groups, head sizes, lengths, windows, sinks and trees at random: heads that spans cut anywhere, several tiles of rows,
     more heads than SMs."""
     rng = np.random.default_rng(7000 + seed)
@@ -342,7 +344,7 @@ def test_random_shapes(seed):
     lens = [int(x) for x in rng.integers(0, top + 1, B)]
     wins = [int(x) for x in rng.integers(0, max(1, top // 2) + 1, B)]
     T = int(rng.integers(1, rz.TREE_MAX_NODES + 1))
-    w = synth.Workload("any", B, 1, Hkv * group, Hkv, D, "bf16", lens, wins, int(rng.integers(0, 20)), min(1, Hkv - 1), 0, seed)
+    w = synth.Workload("any", B, 1, Hkv * group, Hkv, D, dtype, lens, wins, int(rng.integers(0, 20)), min(1, Hkv - 1), 0, seed)
     use_comp = int(rng.integers(0, 4) > 0)
     cache, K, V = _compress(w, shuffle=int(rng.integers(0, 3)), use_comp=use_comp)
     q, k, v = _drafts(w, T, 3, fused=bool(rng.integers(0, 2)))
