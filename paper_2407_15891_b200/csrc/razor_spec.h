@@ -9,10 +9,10 @@ namespace razor {
 
 constexpr int kTreeMaxNodes = RAZOR_TREE_MAX_NODES;
 constexpr int kTreeMaxSpans = 1024;
-// A head that a span's cut runs through for the first time (listed under that span): its parts lie in the spans
-// first_span, first_span + 1, ..; n_parts = 0: nothing to fold.
+// A head that a span starts inside (listed under that span): its parts lie in the spans first_span, first_span + 1, ..;
+// n_parts = 0: the span starts with a head.  turn: the span's number among those that start inside the head.
 struct TreeUnit {
-  int32_t head, first_span, n_parts, pad;
+  int32_t head, first_span, n_parts, turn;
 };
 // One razor_decode_attention_tree call.  Strides in elements, between sequences (b) and between nodes (t).
 struct TreeCall {

@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1) tree_rows_kernel(DeviceView d
 #pragma unroll
   for (int e = 0; e < RL; ++e) node[e] = min(row0 + my_row + e, rows - 1) / G;
   int head = sp.head, y = sp.step, mask_b = -1;
-  long long todo = sp.len;
+  long long todo = sp.head < 0 ? 0 : sp.end - sp.begin;
   HeadState st = sp.st;
   while (todo > 0) {
     const TreeItem it = tree_item(dv, head, y, todo, st);

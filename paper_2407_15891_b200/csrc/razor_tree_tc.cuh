@@ -22,6 +22,9 @@ constexpr int kSoftWarps = 8, kTreeThreads = (kSoftWarps + 4) * 32;   // softmax
 // adds to an accumulator: over a span of the 32K shape (147 steps, 1200 additions) that bias alone put 1.6e-5 of the
 // result's norm into it; every eight steps, with everything else, 3e-6.
 constexpr int kFlush = 8;
+// What a head costs beside its steps, in steps (33 nodes on 32 short D = 64 heads: 0 32-34 us, 3 30-33, 5 28-30, 8 32; 26
+// nodes on 128 ragged heads: 0 133-137, 3 130-132, 5 122-129, 8 121).
+constexpr int kHeadCost = 5;
 constexpr int kItemSlots = 3;
 constexpr int kMaxStages = 4;                   // of K and of V
 constexpr int kSmemMax = 232448;
@@ -200,14 +203,17 @@ __device__ __forceinline__ bool drop_non_finite(uint4& x) {
   return hit;
 }
 
-// What a CTA is to do: `len` steps from step `step` of head `head` (state `st`) on; head < 0: nothing.
+// What a CTA is to do: the steps begin .. end of all the heads' steps laid end to end, the first of them step `step` of head
+// `head` (state `st`); head < 0: nothing.
 struct TreeSpan {
   int head, step;
-  long long len;
+  long long begin, end;
   HeadState st;
 };
-// All heads' steps laid end to end (a head's cache steps, then one for the tree), cut into spans of equal length; the CTA's
-// own span is left at scratch + 256 (1 KB of shared memory), to be read behind a barrier.
+// All heads' steps laid end to end (a head's cache steps, then one for the tree), cut into spans of equal cost; the CTA's own
+// span is left at scratch + 256 (1 KB of shared memory), to be read behind a barrier.  A head costs its steps and kHeadCost
+// more (queries, the compensation token's logit, results); that much lies in front of its first step, and a cut there is a
+// cut between two heads.
 __device__ __forceinline__ void tree_find_span(const DeviceView& dv, const HeadState* states, const TreeCall& tc, int span,
                                                int tile, uint8_t* scratch) {
   constexpr int NT = kTreeThreads;
@@ -216,8 +222,9 @@ __device__ __forceinline__ void tree_find_span(const DeviceView& dv, const HeadS
   TreeSpan* out = (TreeSpan*)(scratch + 256);
   const int per = (dv.n_heads + NT - 1) / NT;
   const int h0 = min(dv.n_heads, tid * per), h1 = min(dv.n_heads, h0 + per);
+  auto cost = [&](int h) { return head_steps(states[h].len) + 1 + kHeadCost; };
   long long mine = 0;
-  for (int h = h0; h < h1; ++h) mine += head_steps(states[h].len) + 1;
+  for (int h = h0; h < h1; ++h) mine += cost(h);
   long long upto = mine;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
@@ -225,7 +232,7 @@ __device__ __forceinline__ void tree_find_span(const DeviceView& dv, const HeadS
     if (lane >= off) upto += y;
   }
   if (lane == 31) warp_tot[warp] = upto;
-  if (tid == 0) *out = TreeSpan{-1, 0, 0, HeadState{0, 0, 0, 0}};
+  if (tid == 0) *out = TreeSpan{-1, 0, 0, 0, HeadState{0, 0, 0, 0}};
   __syncthreads();
   long long before = 0, total = 0;
   for (int w = 0; w < NT / 32; ++w) {
@@ -233,27 +240,46 @@ __device__ __forceinline__ void tree_find_span(const DeviceView& dv, const HeadS
     total += warp_tot[w];
   }
   before += upto - mine;
-  const int n = (int)min((long long)tc.n_spans, max(1LL, (total + tc.min_span - 1) / tc.min_span));
+  const int n = (int)min((long long)tc.n_spans, max(1LL, total / tc.min_span));   // (a span is longer than kHeadCost)
   auto cut = [&](int s) { return total * s / n; };
+  // where a cut is: head h, whose cost starts at u0 (kHeadCost of each head before it are no steps)
+  auto find = [&](long long x, int& h, long long& u0) {
+    u0 = before;
+    h = h0;
+    for (int w; u0 + (w = cost(h)) <= x; ++h) u0 += w;
+  };
   const long long x0 = span < n ? cut(span) : total, x1 = span < n ? cut(span + 1) : total;
   if (x0 < x1 && before <= x0 && x0 < before + mine) {
-    long long u0 = before;
-    int h = h0, w = head_steps(states[h0].len) + 1;
-    while (u0 + w <= x0) {
-      u0 += w;
-      h += 1;
-      w = head_steps(states[h].len) + 1;
+    int h;
+    long long u0;
+    find(x0, h, u0);
+    const long long u = u0 + kHeadCost, step = max(0LL, x0 - u);   // (u: the head's first step)
+    out->head = h;
+    out->step = (int)step;
+    out->begin = u0 - (long long)kHeadCost * h + step;
+    out->st = states[h];
+    // the spans that start inside a head share the work of folding its parts
+    TreeUnit t{h, 0, 0, 0};
+    if (step > 0) {
+      auto span_of = [&](long long x) {   // the span that a step lies in
+        int s = (int)(x * n / total);
+        while (cut(s) > x) s -= 1;
+        while (cut(s + 1) <= x) s += 1;
+        return s;
+      };
+      t.first_span = span_of(u);
+      t.n_parts = span_of(u0 + cost(h) - 1) - t.first_span + 1;
+      t.turn = span - t.first_span - 1;
     }
-    *out = TreeSpan{h, (int)(x0 - u0), x1 - x0, states[h]};
-    // the span in which a head is cut for the first time lists it for the combine kernel
-    TreeUnit u{h, span - 1, 0, 0};
-    if (x0 > u0 && cut(span - 1) <= u0) {
-      int e = span;
-      while (e + 1 < n && cut(e + 1) < u0 + w) e += 1;
-      u.n_parts = e - span + 2;
-    }
-    if (tile == 0) tc.units[span] = u;
+    if (tile == 0) tc.units[span] = t;
   }
+  if (x1 < total && before <= x1 && x1 < before + mine) {
+    int h;
+    long long u0;
+    find(x1, h, u0);
+    out->end = u0 - (long long)kHeadCost * h + max(0LL, x1 - u0 - kHeadCost);
+  }
+  if (x1 == total && tid == 0) out->end = total - (long long)kHeadCost * dv.n_heads;
   if (x0 >= x1 && tile == 0 && tid == 0) tc.units[span] = TreeUnit{0, 0, 0, 0};
 }
 
@@ -292,7 +318,7 @@ __device__ __forceinline__ void tree_produce(const DeviceView& dv, const CUtenso
   volatile int* abort_flag = &p->abort_flag;
   unsigned gk = 0, gi = 0, gq = 0;   // steps issued, items published, query tiles issued
   int head = sp.head, y = sp.step;
-  long long todo = sp.len;
+  long long todo = sp.head < 0 ? 0 : sp.end - sp.begin;
   bool ok = true;
   HeadState st = sp.st;
   for (;; ++gi) {
@@ -367,10 +393,15 @@ __device__ __forceinline__ void tree_produce(const DeviceView& dv, const CUtenso
   }
 }
 
-// Folds the partial records of the heads that a cut ran through, parts in order: a warp per query row.
-// grid = (spans, tiles, R / 8).
+// Folds the partial records of the heads that a cut ran through, in an order that depends on their number alone.
+// grid = (spans, tiles, R / 8).  The spans that start inside a head take its rows in turn; a row's records are shared out to
+// as many warps as leave each about eight, since what costs here is the latency of one record after the other (32 nodes over
+// two long heads of 54 parts each: the whole call 79 us when the rows of a head were one span's and a warp took each, 56 so).
 template <int D, int R>
 __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCall tc) {
+  constexpr int U = 8;   // records in flight
+  __shared__ float part_o[8][D];
+  __shared__ float2 part_ml[8];
   cudaGridDependencySynchronize();
   const TreeUnit u = tc.units[blockIdx.x];
   if (u.n_parts == 0) return;
@@ -378,37 +409,63 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCa
   const int b = u.head / dv.n_kv_heads, g = u.head % dv.n_kv_heads;
   // the first part is the last item of its span, the others are the first of theirs
   auto record = [&](int p) { return ((size_t)((u.first_span + p) * tc.n_tiles + tile) * 2 + (p == 0 ? 1 : 0)) * R; };
-  const int c = blockIdx.z * 8 + warp, r = tile * R + c;
-  if (r >= tc.n_nodes * G) return;
-  const float2 last = __ldcg(&dv.rec_ml[record(u.n_parts - 1) + c]);
-  float m = -CUDART_INF_F, l = 0.f;
-  LaneVec<D> acc;
-  acc.zero();
-  constexpr int U = 8;   // records in flight
-  for (int p0 = 0; p0 < u.n_parts; p0 += U) {
-    float2 ml[U];
-    LaneVec<D> o[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const size_t rec = record(min(p0 + i, u.n_parts - 1)) + c;
-      ml[i] = __ldcg(&dv.rec_ml[rec]);
-      o[i].load_l2(dv.rec_o + rec * D, lane);
-    }
-    if (last.y < 0.f) return;   // an absent node (the last part holds the tree)
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (p0 + i >= u.n_parts) break;
-      const float mn = fmaxf(m, ml[i].x), mu = mn == -CUDART_INF_F ? 0.f : mn;
-      const float c_old = fast_exp2(m - mu), c_new = fast_exp2(ml[i].x - mu);
-      l = l * c_old + ml[i].y * c_new;
+  const int rows = min(R, tc.n_nodes * G - tile * R), among = u.n_parts - 1;
+  const int W = u.n_parts <= U ? 1 : (u.n_parts <= 2 * U ? 2 : (u.n_parts <= 4 * U ? 4 : 8));   // warps to a row
+  const int rows_at_once = 8 / W;
+  for (int k0 = blockIdx.z * rows_at_once; u.turn + k0 * among < rows; k0 += gridDim.z * rows_at_once) {
+    const int c = u.turn + (k0 + warp / W) * among;
+    const bool mine = c < rows;
+    float m = -CUDART_INF_F, l = 0.f;
+    LaneVec<D> acc;
+    acc.zero();
+    auto add = [&](const float2& ml, const LaneVec<D>& o) {
+      const float mn = fmaxf(m, ml.x), mu = mn == -CUDART_INF_F ? 0.f : mn;
+      const float c_old = fast_exp2(m - mu), c_new = fast_exp2(ml.x - mu);
+      l = l * c_old + ml.y * c_new;
       acc.scale(c_old);
-      acc.fma(c_new, o[i]);
+      acc.fma(c_new, o);
       m = mn;
+    };
+    bool live = mine;
+    if (mine) {
+      const float2 last = __ldcg(&dv.rec_ml[record(u.n_parts - 1) + c]);
+      for (int p0 = warp % W; p0 < u.n_parts; p0 += U * W) {
+        float2 ml[U];
+        LaneVec<D> o[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          const size_t rec = record(min(p0 + i * W, u.n_parts - 1)) + c;
+          ml[i] = __ldcg(&dv.rec_ml[rec]);
+          o[i].load_l2(dv.rec_o + rec * D, lane);
+        }
+        live = last.y >= 0.f;   // (an absent node otherwise: the last part holds the tree)
+        if (!live) break;
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          if (p0 + i * W >= u.n_parts) break;
+          add(ml[i], o[i]);
+        }
+      }
     }
+    if (W > 1) {
+      __syncthreads();   // (the turn before has been read)
+      if (warp % W != 0) {
+        acc.store(part_o[warp], lane);
+        if (lane == 0) part_ml[warp] = make_float2(m, l);
+      }
+      __syncthreads();
+      if (warp % W != 0) continue;
+      for (int i = 1; i < W; ++i) {
+        LaneVec<D> o;
+        o.load_shared(part_o[warp + i], lane);
+        add(part_ml[warp + i], o);
+      }
+    }
+    if (!live) continue;
+    acc.scale(1.f / l);
+    const int r = tile * R + c, t = r / G, j = r % G;
+    acc.store(tc.out + (((size_t)b * tc.n_nodes + t) * dv.n_kv_heads * G + (size_t)g * G + j) * D, lane);
   }
-  acc.scale(1.f / l);
-  const int t = r / G, j = r % G;
-  acc.store(tc.out + (((size_t)b * tc.n_nodes + t) * dv.n_kv_heads * G + (size_t)g * G + j) * D, lane);
 }
 
 [[maybe_unused]] bool make_map(CUtensorMap* map, const void* base, const cuuint64_t (&dims)[5], const cuuint64_t (&strides)[4],
@@ -428,7 +485,7 @@ template <int R>
 void tree_cut(const DeviceView& dv, long long rec_rows, int n_sms, TreeCall& tc) {
   tc.n_tiles = (int)(((long long)tc.n_nodes * dv.group + R - 1) / R);
   tc.n_spans = std::max(1, std::min({n_sms / tc.n_tiles, kTreeMaxSpans, (int)(rec_rows / (2LL * R * tc.n_tiles))}));
-  tc.min_span = 4;
+  tc.min_span = kHeadCost + 1;
 }
 // Tensor maps of a call.
 template <int D, int R>
