@@ -11,7 +11,7 @@
 // is the first y whose running sum of W exceeds r sum(W).
 //
 // What bounds it: for large batches one read of the last node's rows (64 chains of 7 over 128256 tokens, 66 MB in fp32: 27.4 us),
-// for small ones a chain of dependent steps (16 trees of 63: up to a dozen rejections in one sequence, 38-47 us).  So a
+// for small ones a chain of dependent steps (16 trees of 63: up to a dozen rejections in one sequence, 41-53 us).  So a
 // sequence is a cluster of CTAs that share the row: each takes a contiguous run of segments, keeps the segment sums in
 // shared memory, and the CTAs trade their warps' partial sums once a pass through distributed shared memory.  The walk
 // itself runs in every CTA of the cluster on values fetched up front (one p and one q value per node), with the same

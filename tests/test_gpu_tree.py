@@ -232,6 +232,18 @@ def test_a_long_context_in_many_parts_is_repeatable(dtype):
     cache.close()
 
 
+@pytest.mark.parametrize("nodes,group,D,dtype,n_ctx", [
+    (1, 1, 128, "bf16", 40000), (20, 4, 128, "bf16", 40001), (7, 8, 64, "bf16", 40015), (33, 4, 64, "bf16", 12345),
+    (128, 8, 128, "bf16", 9001), (3, 2, 128, "f32", 40000), (40, 1, 64, "f32", 20001), (2, 1, 128, "bf16", 1500)])
+def test_a_single_head_cut_into_many_parts(nodes, group, D, dtype, n_ctx):
+    """One KV head alone: as many parts as spans, or as the shorter contexts have steps for, folded by several warps to a row."""
+    w = synth.Workload("single", 1, 1, group, 1, D, dtype, [n_ctx], [64], 4, 1, 0, nodes)
+    cache, K, V = _compress(w)
+    q, k, v = _drafts(w, nodes, 6)
+    _check(w, cache, _refs(w, K, V), q, k, v, _random_parents(np.random.default_rng(nodes), 1, nodes, holes=True))
+    cache.close()
+
+
 def test_tree_attention_in_a_graph_follows_the_cache():
     """Captured on a stream of its own and replayed after appends have grown the cache: a replay attends to the cache as it
     then is, and another call's shape in between does not disturb it."""
