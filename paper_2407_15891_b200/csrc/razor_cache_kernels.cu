@@ -517,7 +517,9 @@ __global__ void append_chunk_finalize_kernel(DeviceView dv, int layer, int n_tok
 // path[b][0 .. n_b), each sequence its own number.  The state afterwards is what n_b single appends would leave
 // (append_fate decides per token, as in append_chunk_kernel; the folded rows are summed thread group by thread group in
 // a fixed order).  The runs are short - a handful of rows of 256 bytes per head - so the kernel is a chain of
-// latencies (state, path, rows, sums); one CTA per head, the loads of a group's rows independent of one another.
+// latencies (state, path, rows, sums); one CTA per head, the loads of a group's rows independent of one another.  Measured
+// alone and cold: 7 rows in each of 4 x 8 heads 4.5-5.7 us, 128 rows in each of 64 x 8 heads (34 MB of drafts, the window evicted)
+// 14 us.
 constexpr int kAppendTreeChunk = 1024;   // sequences of a launch: their counts travel as a kernel argument
 struct AppendCounts {
   uint8_t n[kAppendTreeChunk];
