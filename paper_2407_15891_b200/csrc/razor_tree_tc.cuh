@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(256) tree_combine_kernel(DeviceView dv, TreeCa
           ml[i] = __ldcg(&dv.rec_ml[rec]);
           o[i].load_l2(dv.rec_o + rec * D, lane);
         }
-        live = last.y >= 0.f;   // (an absent node otherwise: the last part holds the tree)
+        live = !(last.y < 0.f);   // (an absent node otherwise: the last part holds the tree; the sum of a row that sees a NaN is a NaN)
         if (!live) break;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
