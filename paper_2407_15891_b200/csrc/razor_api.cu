@@ -133,6 +133,38 @@ void razor::note_cuda_error(cudaError_t e) {
   (void)cudaGetLastError();
 }
 
+// Which layers the library's kernels that may still be in flight write.
+struct WriteTrack {
+  // Layer whose pages, state or sums the last kernel launched for this cache wrote (-1: it wrote none, a decode).
+  // An append of another layer may read before it waits for that kernel.
+  int last_writer_layer = -1;
+  // Kernels launched since the last decode launch that write a layer: (layer, kind).  A decode kernel waits for
+  // everything before it and only then lets its successors start, so these are the only library kernels that
+  // can still be in flight while the NEXT decode kernel runs the part that precedes its own dependency wait.
+  enum { kWriteOneToken = 1, kWriteBulk = 2 };
+  std::vector<std::pair<int, int>> writes_since_decode;
+  bool writes_overflow = false;
+  void note_write(int layer, int kind) {
+    last_writer_layer = layer;
+    if (writes_since_decode.size() < 256) writes_since_decode.emplace_back(layer, kind);
+    else writes_overflow = true;
+  }
+  // A kernel was launched that waits for everything before it ahead of its first access to memory the library writes,
+  // and lets nothing start before it has: whatever is launched next finds all earlier writes complete.
+  void note_wait() {
+    last_writer_layer = -1;
+    writes_since_decode.clear();
+    writes_overflow = false;
+  }
+  // Whether a kernel that writes this layer may be in flight still, behind one that let its successor start at once.
+  bool may_be_written(int layer) const {
+    if (writes_overflow) return true;
+    for (const auto& w : writes_since_decode)
+      if (w.first == layer) return true;
+    return false;
+  }
+};
+
 struct razor_cache {
   razor_config_t cfg;
   Layout lay;
@@ -158,26 +190,20 @@ struct razor_cache {
   uint8_t* pinned_round = nullptr;
   cudaEvent_t round_done[kRoundSlots] = {};
   int round_slot = 0;
-  // Layer whose pages, state or sums the last kernel launched for this cache wrote (-1: it wrote none, a decode).
-  // An append of another layer may read before it waits for that kernel.
-  int last_writer_layer = -1;
-  // Kernels launched since the last decode launch that write a layer: (layer, kind).  A decode kernel waits for
-  // everything before it and only then lets its successors start, so these are the only library kernels that
-  // can still be in flight while the NEXT decode kernel runs the part that precedes its own dependency wait.
-  enum { kWriteOneToken = 1, kWriteBulk = 2 };
-  std::vector<std::pair<int, int>> writes_since_decode;
-  bool writes_overflow = false;
-  void note_write(int layer, int kind) {
-    last_writer_layer = layer;
-    if (writes_since_decode.size() < 256) writes_since_decode.emplace_back(layer, kind);
-    else writes_overflow = true;
-  }
-  // Whether a kernel that writes this layer may be in flight still, behind one that let its successor start at once.
-  bool may_be_written(int layer) const {
-    if (writes_overflow) return true;
-    for (const auto& w : writes_since_decode)
-      if (w.first == layer) return true;
-    return false;
+  // What is in flight among the calls that run, and among those of the capture in progress: in a graph's replay a kernel
+  // finds what was captured before it, and eager calls find nothing of a capture.
+  WriteTrack eager, captured;
+  unsigned long long capture_id = 0;   // the capture that `captured` belongs to
+  WriteTrack& track(cudaStream_t stream) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    unsigned long long id = 0;
+    if (cudaStreamGetCaptureInfo(stream, &status, &id) != cudaSuccess) (void)cudaGetLastError();   // (such a stream takes no launch either)
+    if (status == cudaStreamCaptureStatusNone) return eager;
+    if (id != capture_id) {   // a graph's first kernel starts behind all that was launched before the graph: `eager` is more than can be in flight
+      capture_id = id;
+      captured = eager;
+    }
+    return captured;
   }
 };
 
@@ -522,7 +548,7 @@ int compress_impl(razor_cache* c, int layer, const std::vector<SeqIn>& seqs, con
   long long slices = ceil_div((long long)c->n_sms * 48, heads_in_call);
   const long long by_rows = n_max >= 8 * 512 ? n_max / 512 : std::max(1, n_max / 64);
   slices = std::max(1LL, std::min({slices, (long long)kCompressMaxSlices, room, by_rows}));
-  c->note_write(layer, razor_cache::kWriteBulk);
+  c->track(stream).note_write(layer, WriteTrack::kWriteBulk);
   ce = launch_compress(c->dv, cfg.dtype, layer, (int)seqs.size(), (int)slices, n_plan, stream);
   if (ce != cudaSuccess) return fail_enqueued(ce);
   // ---- commit
@@ -654,9 +680,10 @@ int razor_append(razor_cache_t* c, int32_t layer, const void* k_new, const void*
   if (((uintptr_t)k_new | (uintptr_t)v_new) & 15) return RAZOR_E_MISALIGNED;
   LayerHost& L = c->layers[layer];
   if (L.appended_max() >= c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
-  const int early_reads = c->last_writer_layer != layer && !c->may_be_written(layer);
+  WriteTrack& track = c->track((cudaStream_t)stream);
+  const int early_reads = track.last_writer_layer != layer && !track.may_be_written(layer);
   RZ_CUDA(launch_append(c->dv, c->cfg.dtype, layer, k_new, v_new, early_reads, (cudaStream_t)stream));
-  c->note_write(layer, razor_cache::kWriteOneToken);
+  track.note_write(layer, WriteTrack::kWriteOneToken);
   // Host mirror of the kernel's state update.
   const int n_sink = c->cfg.n_sink;
   for (HeadState& h : L.hs) {
@@ -704,7 +731,7 @@ int razor_append_many(razor_cache_t* c, int32_t layer, const void* k_new, const 
     slices = (int)best;
   }
   RZ_CUDA(launch_append_many(c->dv, c->cfg.dtype, layer, k_new, v_new, n_tokens, slices, (cudaStream_t)stream));
-  c->note_write(layer, razor_cache::kWriteBulk);
+  c->track((cudaStream_t)stream).note_write(layer, WriteTrack::kWriteBulk);
   const int n_sink = c->cfg.n_sink;
   for (HeadState& h : L.hs) h = state_after_run(h, n_sink, n_tokens);   // host mirror of the kernels' state update
   for (int32_t& n : L.appended) n += n_tokens;
@@ -751,7 +778,7 @@ int razor_append_tree(razor_cache_t* c, int32_t layer, const void* k_draft, cons
   if (capture != cudaStreamCaptureStatusNone) return RAZOR_E_INVALID_ARG;
   RZ_CUDA(launch_append_tree(c->dv, cfg.dtype, layer, k_draft, v_draft, kv_stride_b, kv_stride_t, path, n_nodes, n_accept,
                              cfg.batch, (cudaStream_t)stream));
-  c->note_write(layer, razor_cache::kWriteBulk);
+  c->track((cudaStream_t)stream).note_write(layer, WriteTrack::kWriteBulk);
   for (int b = 0; b < cfg.batch; ++b) {   // host mirror of the kernel's state update
     if (n_accept[b] == 0) continue;
     for (int g = 0; g < cfg.n_kv_heads; ++g) {
@@ -786,11 +813,7 @@ int razor_decode_attention_tree(razor_cache_t* c, int32_t layer, const void* q, 
     RZ_CUDA(launch_tree_mma(c->dv, c->pool_pages, layer, tc, rec_rows, c->n_sms, (cudaStream_t)stream));
   else
     RZ_CUDA(launch_tree_rows(c->dv, layer, tc, rec_rows, c->n_sms, (cudaStream_t)stream));
-  // The kernels wait for everything before them ahead of their first access to memory and let nothing start before
-  // they end: whatever is launched next finds all earlier writes complete.
-  c->last_writer_layer = -1;
-  c->writes_since_decode.clear();
-  c->writes_overflow = false;
+  c->track((cudaStream_t)stream).note_wait();   // (they let nothing start before they end)
   return RAZOR_OK;
 }
 
@@ -929,9 +952,7 @@ static int round_impl(razor_cache_t* c, int32_t layer, const void* q, float* out
   RZ_CUDA(cudaEventRecord(c->round_done[slot], s));
   const RoundJobs jb{(int32_t)items.size(), (int32_t)multi.size(), n_tokens, 0};
   RZ_CUDA(launch_round(c->dv, c->pool_pages, layer, jb, q, out, c->n_sms, s));
-  c->last_writer_layer = -1;
-  c->writes_since_decode.clear();   // an ordinary launch: everything before it has completed when it starts
-  c->writes_overflow = false;
+  c->track(s).note_wait();   // (an ordinary launch: everything before it has completed when it starts)
   return RAZOR_OK;
 }
 
@@ -943,15 +964,15 @@ static int round_impl(razor_cache_t* c, int32_t layer, const void* q, float* out
 // before ring_head for a head that evicted.  Anything else (a bulk append, a compression, more appends): no early
 // copies.  For CTA i the count covers the leading pages of its span's first work item, cut at the first such
 // page and at the item's length as it is now.
-static void plan_early_prefetch(const razor_cache* c, int layer, DecodeJobs& jb) {
+static void plan_early_prefetch(const razor_cache* c, const WriteTrack& track, int layer, DecodeJobs& jb) {
   std::memset(jb.early, 0, sizeof(jb.early));
   jb.state_stable = 0;
-  if (c->tune.early_prefetch <= 0 || c->writes_overflow) return;
+  if (c->tune.early_prefetch <= 0 || track.writes_overflow) return;
   int n_writes = 0;
   bool only_appends = true;
-  for (const auto& wr : c->writes_since_decode) {
+  for (const auto& wr : track.writes_since_decode) {
     if (wr.first != layer) continue;
-    only_appends &= wr.second == razor_cache::kWriteOneToken;
+    only_appends &= wr.second == WriteTrack::kWriteOneToken;
     n_writes += 1;
   }
   jb.state_stable = n_writes == 0 ? 1 : 0;   // nothing in flight writes this layer's head states
@@ -1040,12 +1061,11 @@ static int decode_impl(razor_cache_t* c, int32_t layer, const void* q, float* ou
   const LayerHost& L = c->layers[layer];
   DecodeJobs jb{L.n_items, L.n_jobs, L.n_spans, L.jobs[L.n_spans], L.n_multi, n_tokens, tok_stride, q_after, 0, {},
                 k_new, v_new};
-  plan_early_prefetch(c, layer, jb);
+  WriteTrack& track = c->track((cudaStream_t)stream);
+  plan_early_prefetch(c, track, layer, jb);
   RZ_CUDA(launch_decode(c->dv, c->cfg.dtype, layer, jb, q, out, c->n_sms, c->tune,
                         (cudaStream_t)stream));
-  c->last_writer_layer = -1;
-  c->writes_since_decode.clear();
-  c->writes_overflow = false;
+  track.note_wait();
   return RAZOR_OK;
 }
 
@@ -1087,7 +1107,7 @@ int razor_decode_step(razor_cache_t* c, int32_t layer, const void* k_new, const 
     L.sched_valid = false;
     return rc;
   }
-  c->note_write(layer, razor_cache::kWriteOneToken);   // the launch stores the new rows late: the next one must leave them alone
+  c->track((cudaStream_t)stream).note_write(layer, WriteTrack::kWriteOneToken);   // the launch stores the new rows late: the next one must leave them alone
   return RAZOR_OK;
 }
 
