@@ -398,7 +398,7 @@ struct SeqIn {
   int n_ctx, window;
 };
 
-int ensure_schedule(razor_cache* c, int layer, cudaStream_t stream, bool upload, int rows);
+int ensure_schedule(razor_cache* c, int layer, cudaStream_t stream, bool upload, int rows, bool on_device = false);
 
 // Shared body of razor_compress / razor_compress_seq: the plan (C0), page allocation, uploads, launch.
 int compress_impl(razor_cache* c, int layer, const std::vector<SeqIn>& seqs, const uint8_t* retr, int n_sink,
@@ -569,14 +569,17 @@ int compress_impl(razor_cache* c, int layer, const std::vector<SeqIn>& seqs, con
   // With the layer complete, its decode schedule is planned and sent to the device here, behind the compression
   // kernels, rather than in front of the layer's first decode launch, where the copies would sit between two
   // kernels that otherwise overlap.  (A failure here is not an error of the compression: the decode call plans again.)
-  // An empty layer (the start of a chunked prefill, or of ragged rounds) has nothing to plan yet.
-  bool any_token = false;
-  for (const HeadState& h : L.hs) any_token |= h.len > 0;
-  if (any_token && L.n_done == cfg.batch) (void)ensure_schedule(c, layer, stream, true, cfg.n_q_heads / cfg.n_kv_heads);
+  // That goes for a layer without a token too: a few appends do not make its plan stale, and a decode call behind them
+  // finds it there, a captured one among them.  Its plan is an empty item per head, and compress_plan_kernel has written it
+  // where this call covered the whole batch (64 x 8 heads: two copies would have cost 15 us of stream time).
+  bool empty = (int)seqs.size() == cfg.batch;
+  for (const HeadState& h : L.hs) empty &= h.len == 0;
+  if (L.n_done == cfg.batch) (void)ensure_schedule(c, layer, stream, true, cfg.n_q_heads / cfg.n_kv_heads, empty);
   return RAZOR_OK;
 }
 
-int ensure_schedule(razor_cache* c, int layer, cudaStream_t stream, bool upload, int rows) {
+// on_device: the plan that this call will come to is on the device already.
+int ensure_schedule(razor_cache* c, int layer, cudaStream_t stream, bool upload, int rows, bool on_device) {
   LayerHost& L = c->layers[layer];
   // (which heads the streaming kernel folds itself depends on the rows of a KV head's tile in this launch)
   const bool stale = !L.sched_valid || L.sched_rows != rows || (long long)L.growth_tokens * 4 >= (long long)L.chunk_pages * kPageTokens;
@@ -597,7 +600,9 @@ int ensure_schedule(razor_cache* c, int layer, cudaStream_t stream, bool upload,
   L.n_multi = info.n_multi;
   L.chunk_pages = info.chunk_pages;
   L.growth_tokens = 0;
-  if (upload) {
+  if (upload && on_device) {
+    L.sched_valid = true;
+  } else if (upload) {
     if (!L.upload_done) RZ_CUDA(cudaEventCreateWithFlags(&L.upload_done, cudaEventDisableTiming));
     RZ_CUDA(cudaMemcpyAsync(c->dv.items + (size_t)layer * c->lay.max_items, L.items, (size_t)n * sizeof(WorkItem),
                             cudaMemcpyHostToDevice, stream));

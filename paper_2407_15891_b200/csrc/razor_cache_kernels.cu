@@ -188,6 +188,14 @@ __global__ void __launch_bounds__(256) compress_plan_kernel(DeviceView dv, int l
   if (threadIdx.x == 0) {
     dv.state[hs] = HeadState{pl.len, pl.n_drop, 0, pl.window};
     dv.ring_valid[hs] = 0;   // nobody has summed the rows of the new window
+    // A layer whose heads are all empty has a schedule of one item per head, in the heads' order (build_schedule with no
+    // pages).  Any other schedule is sent behind this kernel and overwrites what stands here.
+    if (pl.len == 0) {
+      dv.items[(size_t)layer * dv.max_items + pl.head] = WorkItem{pl.head, 0, -1, 0, 1, 0, 0, 0};
+      int32_t* jobs = dv.jobs + (size_t)layer * (dv.max_items + 1);
+      jobs[pl.head] = pl.head;
+      if (pl.head == dv.n_heads - 1) jobs[dv.n_heads] = dv.n_heads;
+    }
   }
 }
 

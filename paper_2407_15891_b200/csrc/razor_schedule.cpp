@@ -40,11 +40,20 @@ int build_schedule(const int32_t* pages, int n_heads, const SchedParams& sp, int
   const int static_pct = std::min(100, std::max(0, sp.static_pct));
   const int tail_per_cta = std::max(1, sp.tail_items_per_cta);
 
+  long long total = 0;
+  for (int h = 0; h < n_heads; ++h) total += pages[h];
+  if (total == 0 && n_heads <= max_items) {   // nothing to cut: an empty item per head (what the rest comes to, without its lists)
+    for (int h = 0; h < n_heads; ++h) {
+      out[h] = WorkItem{h, 0, -1, 0, 1, 0, 0, 0};
+      jobs[h] = h;
+    }
+    jobs[n_heads] = n_heads;
+    if (info) *info = SchedInfo{n_heads, n_heads, 0, min_chunk, min_chunk, 0};
+    return n_heads;
+  }
   std::vector<int> order(n_heads);
   std::iota(order.begin(), order.end(), 0);
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return pages[a] > pages[b]; });
-  long long total = 0;
-  for (int h = 0; h < n_heads; ++h) total += pages[h];
 
   // Spans: equal, at least min_chunk pages, at most one per CTA.
   const long long static_pages = total * static_pct / 100;

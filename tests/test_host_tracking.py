@@ -39,6 +39,7 @@ def lib(tmp_path_factory):
     lib.razor_cache_destroy.argtypes = [vp]
     lib.razor_query_bytes.argtypes = [C.POINTER(rz.RazorConfig), vp, vp, vp, C.POINTER(sz), C.POINTER(sz)]
     lib.razor_compress.argtypes = [vp, i32, vp, vp, i64, i64, i64, vp, vp, i32, vp, vp]
+    lib.razor_compress_seq.argtypes = [vp, i32, i32, vp, vp, i64, i64, i32, vp, i32, i32, vp]
     lib.razor_append.argtypes = [vp, i32, vp, vp, vp]
     lib.razor_append_many.argtypes = [vp, i32, vp, vp, i32, vp]
     lib.razor_append_tree.argtypes = [vp, i32, vp, vp, i64, i64, vp, i32, vp, vp]
@@ -68,6 +69,10 @@ class Host:
     def compress(self, layer, stream=A):
         n = self.n_ctx
         return self.lib.razor_compress(self.h, layer, PTR, PTR, 4 * n * 128, n * 128, 128, self.ctx, self.retr, 4, self.win, stream)
+
+    def compress_seq(self, layer, b, stream=A):
+        n = self.n_ctx
+        return self.lib.razor_compress_seq(self.h, layer, b, PTR, PTR, n * 128, 128, n, self.retr, 4, 200, stream)
 
     def append(self, layer, stream=A):
         return self.lib.razor_append(self.h, layer, PTR, PTR, stream)
@@ -167,3 +172,28 @@ def test_steps_and_paths_are_writes(host):
         assert host.tree(1) == 0 and host.append(0) == 0
         assert host.seen["append_early"] == 1
         assert host.tree(0) == 0
+
+
+def test_a_layer_that_started_empty_has_a_schedule(lib):
+    """A few tokens after an empty start, a captured decode finds a schedule on the device and uploads none: an upload that is
+    only captured would leave the next eager decode without."""
+    h = Host(lib, n_ctx=0)
+    # the plan that the compression kernel writes for such a layer: an empty item per head, a job each
+    items, n = (C.c_int32 * 40)(), C.c_int32(0)
+    assert lib.razor_schedule_query(h.h, 0, items, 8, C.byref(n)) == 0 and n.value == 8
+    assert list(items) == [x for head in range(8) for x in (head, 0, -1, 1, head)]
+    assert h.seen["uploads"] == 2           # one plan of the compression for each layer
+    for call in (h.decode, h.step):
+        assert h.compress(0) == 0 and h.append(0) == 0 and h.append_tree(0, (4, 0)) == 0
+        uploads = h.seen["uploads"]
+        lib.fake_capture(B, 5)
+        assert call(0, B) == 0
+        lib.fake_capture(B, 0)
+        assert h.decode(0) == 0
+        assert h.seen["captured_uploads"] == h.seen["captured_records"] == 0 and h.seen["uploads"] == uploads
+    # one sequence emptied again while the other goes on: the device holds another plan for the rest, all of it is sent
+    uploads = h.seen["uploads"]
+    assert h.compress_seq(0, 1) == 0
+    assert h.seen["uploads"] == uploads + 3     # the compression's plan, items, jobs
+    assert h.decode(0) == 0 and h.seen["uploads"] == uploads + 3
+    h.close()
