@@ -21,6 +21,8 @@
  *   - Work is enqueued on the CUDA stream passed as `stream` (a cudaStream_t cast to void*; NULL is
  *     the default stream) and is asynchronous with respect to the host.  All calls on one cache
  *     must be stream-ordered with respect to each other (they share scratch buffers).
+ *   - Made for CUDA graphs: razor_decode_attention_tree and razor_verify_tree.  The other calls on a cache keep plans
+ *     and lengths on the host, which a replay does not repeat.
  *   - Storage dtype of K, V and q is config.dtype; compensation sums/means and outputs are fp32.
  *   - The library never applies rotary embeddings: K and q arrive after the rotary transformation,
  *     as the paper's cache does (Section 3.2, text below Eq. 4).

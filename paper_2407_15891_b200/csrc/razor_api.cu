@@ -611,8 +611,11 @@ int ensure_schedule(razor_cache* c, int layer, cudaStream_t stream, bool upload,
     if (L.n_multi)
       RZ_CUDA(cudaMemcpyAsync(c->dv.multi + (size_t)layer * nh, L.multi, (size_t)L.n_multi * sizeof(MultiHead),
                               cudaMemcpyHostToDevice, stream));
-    RZ_CUDA(cudaEventRecord(L.upload_done, stream));
-    L.sched_valid = true;
+    // On a capturing stream nothing has been sent: the next call that runs plans and sends its own.
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    RZ_CUDA(cudaStreamIsCapturing(stream, &capture));
+    L.sched_valid = capture == cudaStreamCaptureStatusNone;
+    if (L.sched_valid) RZ_CUDA(cudaEventRecord(L.upload_done, stream));
   } else {
     L.sched_valid = false;   // the device copy no longer matches; the next decode uploads again
   }

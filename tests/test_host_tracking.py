@@ -197,3 +197,21 @@ def test_a_layer_that_started_empty_has_a_schedule(lib):
     assert h.seen["uploads"] == uploads + 3     # the compression's plan, items, jobs
     assert h.decode(0) == 0 and h.seen["uploads"] == uploads + 3
     h.close()
+
+
+def test_a_schedule_that_was_only_captured_has_not_been_sent(lib):
+    """A call whose schedule is stale, captured: the copies are in the graph.  The next call that runs sends its own, and the
+    event that guards the staging area is not the graph's."""
+    for n_ctx in (0, 900):               # (two tokens of two query heads: another schedule than the one-token decode's)
+        h = Host(lib, n_ctx=n_ctx)
+        lib.fake_reset()
+        assert h.lib.razor_append_many(h.h, 0, PTR, PTR, 3, A) == 0
+        lib.fake_capture(B, 5)
+        assert h.round(0, 2, B) == 0
+        lib.fake_capture(B, 0)
+        seen = h.seen
+        assert seen["captured_uploads"] > 0 and seen["captured_records"] == 0 and seen["uploads"] == 0
+        assert h.round(0, 2) == 0
+        assert h.seen["uploads"] == seen["captured_uploads"] and h.seen["records"] == 1
+        assert h.round(0, 2) == 0 and h.seen["uploads"] == seen["captured_uploads"]
+        h.close()
