@@ -233,9 +233,11 @@ RAZOR_API int razor_decode_attention_multi(razor_cache_t* cache, int32_t layer, 
  *
  * razor_decode_attention_tree: out device fp32 [B, n_nodes, Hq, D] contiguous, 16-byte aligned.  Node t attends to every
  * kept token of its KV head, to the compensation token with its count (Eq. 5), and to itself and its ancestors.  An
- * absent node's rows of out are left as they were.  With ALiBi (razor_cache_set_alibi) a node's position is the tokens
- * seen so far plus its depth.  q, k_draft, v_draft, parent may be written by the kernel directly before this call; they,
- * and out, must not change until it has run.  Captured in a CUDA graph, a replay attends to the cache as it then is.
+ * absent node's rows of out are left as they were.  What is not finite shows in the rows that see it and in no other: a
+ * NaN in q or in a K makes its rows NaN; a NaN or an infinity in a V appears in that dimension of them (from a cached bf16 V
+ * row an infinity may come out as a NaN).  With ALiBi (razor_cache_set_alibi) a node's position is the tokens seen so far
+ * plus its depth.  q, k_draft, v_draft, parent may be written by the kernel directly before this call; they, and out, must
+ * not change until it has run.  Captured in a CUDA graph, a replay attends to the cache as it then is.
  *
  * razor_append_tree: path device int32 [B, n_nodes]: node path[b][i] is the i-th token appended to sequence b, for
  * i < n_accept[b] (razor_verify_tree's path); NULL: the nodes 0, 1, .. themselves.  Entries outside [0, n_nodes) read

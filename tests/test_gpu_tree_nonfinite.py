@@ -124,3 +124,26 @@ def test_an_infinity_in_a_drafts_k(dtype, group, D, T, alibi, n_ctx):
                     seen.add("below" if 1 in lines[t] else "away")
     assert seen == {"nan", "below", "away"}
     cache.close()
+
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+@pytest.mark.parametrize("n_ctx", [LONG, SHORT])
+@pytest.mark.parametrize("dtype,group,D,T,alibi", KERNELS)
+def test_a_cached_v_that_is_not_finite(dtype, group, D, T, alibi, n_ctx, bad):
+    """Dimension 10 of the last cached token's V: that dimension of every live row is not finite - the infinity itself from fp32
+    caches, which weigh a row once, possibly a NaN from bf16 ones, whose weights come in two parts of either sign - and every
+    other dimension keeps its bits.  (The last token: the weight that ALiBi's penalty leaves it is not zero.)"""
+    w, cache, K, V, q, k, v, parent, _ = _setup(dtype, group, D, T, alibi, n_ctx)
+    live = [t for t, line in enumerate(orc.tree_lines(parent)) if line is not None]
+    clean = _call(cache, q, k, v, parent)
+    V[0, 0, n_ctx - 1, 10] = bad
+    cache.compress(0, K, V, w.ctx_len, w.retrieval(0), w.window)
+    out = _call(cache, q, k, v, parent)
+    assert not torch.isfinite(out[live][..., 10]).any()
+    if dtype == "f32" and not math.isnan(bad):
+        assert (out[live][..., 10] == bad).all()
+    rest = [d for d in range(D) if d != 10]
+    assert torch.equal(out[..., rest], clean[..., rest])
+    absent = [t for t in range(T) if t not in live]
+    assert (out[absent] == MARK).all()
+    cache.close()
