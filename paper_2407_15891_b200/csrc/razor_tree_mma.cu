@@ -13,8 +13,9 @@
 // added at the end.
 //
 // What bounds it is the stream of pages out of HBM: 8 nodes on the 32K multi-head shape (8 x 32 heads, 1.40 GB of kept
-// pages) 210-214 us = 6.6 TB/s, 1.02 of the measured copy rate; 64 nodes 240 us (285 when the power cap holds the clock
-// near 1.5 GHz: then the softmax warps, 2500 cycles a step against the copies' 2640 at full clock, fall behind).
+// pages) 224-226 us under continuous load = 6.2 TB/s, 0.97 of the measured copy rate (210-214 us in runs of 60 calls); 64
+// nodes 286-290 us with the clock held near 1.5 GHz by the power cap, where the softmax warps (2500 cycles a step against
+// the copies' 2640 at full clock) fall behind, 240 us at full clock.
 //
 // Work: every head's slots in steps of 128 tokens plus one step for the tree's own tokens (their visibility is a bit mask
 // per thread).  All heads' steps are laid end to end and cut into equal spans, one per CTA; with several tiles of rows

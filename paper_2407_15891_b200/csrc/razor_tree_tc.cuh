@@ -20,10 +20,15 @@ constexpr int kStepPages = kTok / kPageTokens;
 constexpr int kSoftWarps = 8, kTreeThreads = (kSoftWarps + 4) * 32;   // softmax warps; of four more, one copies, one issues the scores' products, one the outputs', and one has no part
 // Steps whose products add up in tensor memory before the softmax warps take the sum out.  The matrix unit truncates when it
 // adds to an accumulator: over a span of the 32K shape (147 steps, 1200 additions) that bias alone put 1.6e-5 of the
-// result's norm into it; every eight steps, with everything else, 3e-6.
+// result's norm into it (2.2e-5 to 4.5e-5 over single heads of 150 steps a span, where every eight steps leave 2.5e-6 to 3.4e-6,
+// everything else included).
 constexpr int kFlush = 8;
-// What a head costs beside its steps, in steps (33 nodes on 32 short D = 64 heads: 0 32-34 us, 3 30-33, 5 28-30, 8 32; 26
-// nodes on 128 ragged heads: 0 133-137, 3 130-132, 5 122-129, 8 121).
+// What a head costs beside its steps, in steps.  Chosen on two shapes (33 nodes on 32 short D = 64 heads: 0 32-34 us, 3 30-33,
+// 5 28-30, 8 32; 26 nodes on 128 ragged heads: 0 133-137, 3 130-132, 5 122-129, 8 121).  On fifteen others, eight drawn at random
+// among them, 0 costs up to a quarter more where heads are short and many (40 heads of 1114 tokens, 236 rows each: 36
+// against 29 us; 240 of 92 tokens, 32 rows: 23 against 20), is level on long ones, and is 1.5-2 us faster for twenty
+// short heads or fewer (16 -> 14 us: there the smallest span, which is longer than this, leaves SMs idle); 8 stays within 8 %
+// either way.
 constexpr int kHeadCost = 5;
 constexpr int kItemSlots = 3;
 constexpr int kMaxStages = 4;                   // of K and of V

@@ -9,12 +9,14 @@
 // weights are two products against the same V.  Spans, producer, masks of hidden rows and the lagging maximum are the other
 // kernel's (so are the reasons for them); the two warps that share rows agree on a move of the maximum.
 //
-// What bounds it: the arithmetic on a step's 16384 scores in eight warps, 2700 cycles (weights and their splitting 1160,
-// loads of S and maxima 480, waits and stores the rest) against 1536 of the tensor cores.  64 nodes on the 128K grouped-query
-// shape (256 rows against 16 KV heads, 0.37 GB of kept pages): 147 us = 640 TFLOP/s over 4 D flops a (row, token) pair, 0.38 of
-// the measured cuBLAS rate (174 us under a continuous load's power cap); the other form took 214.  Timing-only variants say
-// that no single piece is the limit: 148 us without the remainder product, 143 with every page out of L2, and the same within
-// 2 % with two groups of warps that take turns at the steps or with four threads to a row.
+// 64 nodes on the 128K grouped-query shape (256 rows against 16 KV heads, 0.37 GB of kept pages): 173-175 us under continuous
+// load = 540 TFLOP/s over 4 D flops a (row, token) pair, 0.38 of cuBLAS's measured rate under the same power cap and 0.32 of
+// its burst rate (147 us in short runs at full clock); the other form took 214 there.
+// What bounds it has not been found.  A step takes about 2700 cycles (weights and their splitting 1160, loads of S and
+// maxima 480, waits and stores the rest) against 1536 of the tensor cores, but no pipe is over 42 % and the schedulers issue
+// in 39 % of the cycles: two softmax warps to a scheduler wait for most of a step.  Timing-only variants moved little: 148 us
+// for 151 without the remainder product, 143 with every page out of L2, and the same within 2 % with two groups of warps
+// that take turns at the steps or with four threads to a row.
 //
 // Tensor memory (512 columns): S twice 128, P 64 columns of bf16 pairs for the heads and 64 for the remainders, O D.
 // ALiBi caches stay with the other kernel: there a token's position is one thread's, here it would be every thread's.

@@ -10,8 +10,9 @@
 // rejected children and S = 1 - their probabilities, no pass over the row needed.  Where the walk ends, the next token
 // is the first y whose running sum of W exceeds r sum(W).
 //
-// What bounds it: for large batches one read of the last node's rows (64 chains of 7 over 128256 tokens, 66 MB in fp32: 27.4 us),
-// for small ones a chain of dependent steps (16 trees of 63: up to a dozen rejections in one sequence, 41-53 us).  So a
+// What bounds it: for large batches one read of the last node's rows (64 chains of 7 over 128256 tokens, 66 MB in fp32: 27 us,
+// 0.37 of the measured copy rate; what keeps the streaming loop below that has not been measured), for small ones a chain of
+// dependent steps (16 trees of 63: up to a dozen rejections in one sequence, 38-53 us with the inputs).  So a
 // sequence is a cluster of CTAs that share the row: each takes a contiguous run of segments, keeps the segment sums in
 // shared memory, and the CTAs trade their warps' partial sums once a pass through distributed shared memory.  The walk
 // itself runs in every CTA of the cluster on values fetched up front (one p and one q value per node), with the same
@@ -106,8 +107,6 @@ __device__ __forceinline__ double running_sum(double x, int lane) {
   return x;
 }
 
-// kKeep: a row's values stay in registers while its node is the current one, so that every rejected child after the
-// first costs no memory access (needs rows of at most kVerifyCluster * kVerifyWarps * kKeepSegs units, 131072 values).
 // The CTAs' sums from their warps': lane r < kVerifyCluster gets CTA r's, and all lanes the whole (in the same order in
 // every CTA of the cluster).
 __device__ __forceinline__ double cta_part(const double (*part)[kVerifyWarps], int lane) {
@@ -124,6 +123,8 @@ __device__ __forceinline__ double all_parts(const double (*part)[kVerifyWarps], 
   return x;
 }
 
+// kKeep: a row's values stay in registers while its node is the current one, so that every rejected child after the
+// first costs no memory access (needs rows of at most kVerifyCluster * kVerifyWarps * kKeepSegs units, 131072 values).
 template <typename T, bool kKeep>
 __global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(VerifyCall vc) {
   __shared__ VerifySmem sm;
@@ -376,7 +377,7 @@ __global__ void __launch_bounds__(kVerifyThreads, kKeep ? 1 : 2) verify_kernel(V
 cudaError_t launch_verify(const VerifyCall& call, int dtype, int n_sms, cudaStream_t stream) {
   VerifyCall vc = call;
   // CTAs to a sequence: as many as are resident at once (two to an SM), so that a large batch does not run in a wave and a
-  // bit (64 sequences over 128256 tokens, one pass each: 8 to a sequence 33.6 us, 4 27.4 us).
+  // bit (64 sequences over 128256 tokens, one pass each: 8 to a sequence 33.6 us, 4 27 us).
   int ranks = kVerifyCluster;
   while (ranks > 1 && (long long)vc.batch * ranks > 2LL * n_sms) ranks /= 2;
   // segments: at most kMaxSegs to a CTA
