@@ -215,3 +215,40 @@ def test_a_schedule_that_was_only_captured_has_not_been_sent(lib):
         assert h.seen["uploads"] == seen["captured_uploads"] and h.seen["records"] == 1
         assert h.round(0, 2) == 0 and h.seen["uploads"] == seen["captured_uploads"]
         h.close()
+
+
+def test_the_tree_calls_refuse_before_anything_is_launched(lib, host):
+    """Every argument the header rules out, on a layer that is ready: the status, and no launch."""
+    base = dict(layer=0, q=PTR, qb=4 * 1024, qt=1024, k=PTR, v=PTR, kb=4 * 512, kt=512, parent=PTR, n=4, out=PTR)
+
+    def tree(**kw):
+        a = dict(base, **kw)
+        return lib.razor_decode_attention_tree(host.h, a["layer"], a["q"], a["qb"], a["qt"], a["k"], a["v"], a["kb"], a["kt"],
+                                               a["parent"], a["n"], a["out"], A)
+
+    def path(counts=(1, 1), **kw):
+        a = dict(base, path=None, **kw)
+        return lib.razor_append_tree(host.h, a["layer"], a["k"], a["v"], a["kb"], a["kt"], a["path"], a["n"],
+                                     (C.c_int32 * 2)(*counts) if counts else None, A)
+
+    before = host.seen["launches"]
+    for kw, status in [(dict(layer=2), -1), (dict(layer=-1), -1), (dict(n=0), -1), (dict(n=rz.TREE_MAX_NODES + 1), -1),
+                       *[(dict([(name, None)]), -2) for name in ("q", "k", "v", "parent", "out")],
+                       *[(dict([(name, PTR + 8)]), -8) for name in ("q", "k", "v", "out")], (dict(parent=PTR + 2), -8),
+                       (dict(qt=1028), -8), (dict(kt=516), -8), (dict(qb=4100), -8), (dict(kb=2052), -8), (dict(qt=1016), -1),
+                       (dict(kt=504), -1), (dict(kb=504), -1), (dict(qb=0), -1), (dict(qt=-1024), -1), (dict(kt=1 << 37), -1)]:
+        assert tree(**kw) == status, kw
+    for counts, kw, status in [((5, 0), {}, -1), ((-1, 0), {}, -1), (None, {}, -2), ((1, 1), dict(k=None), -2), ((1, 1), dict(v=None), -2),
+                               ((1, 1), dict(layer=2), -1), ((1, 1), dict(n=0), -1), ((1, 1), dict(n=129), -1), ((1, 1), dict(kt=508), -8),
+                               ((1, 1), dict(v=PTR + 8), -8), ((1, 1), dict(kb=8), -1)]:
+        assert path(counts, **kw) == status, (counts, kw)
+    assert path((0, 0)) == 0 and host.seen["launches"] == before
+    lib.fake_capture(A, 9)
+    assert path() == -1 and host.seen["launches"] == before
+    lib.fake_capture(A, 0)
+    for _ in range(99):
+        assert path((4, 0)) == 0
+    assert path((4, 4)) == 0 and path((1, 0)) == -5 and path((0, 4)) == 0     # 400 to a sequence, each on its own
+    assert host.append(0) == -5 and tree() == 0
+    # a stride that separates nothing may be anything
+    assert tree(n=1, qt=0, kt=3) == 0
