@@ -24,8 +24,8 @@
  *   - Made for CUDA graphs: razor_decode_attention_tree and razor_verify_tree.  The other calls on a cache keep plans
  *     and lengths on the host, which a replay does not repeat.
  *   - Storage dtype of K, V and q is config.dtype; compensation sums/means and outputs are fp32.
- *   - The library never applies rotary embeddings: K and q arrive after the rotary transformation,
- *     as the paper's cache does (Section 3.2, text below Eq. 4).
+ *   - The cache and attention calls never apply rotary embeddings: K and q arrive after the rotary transformation,
+ *     as in the paper's cache (Section 3.2, text below Eq. 4).  razor_rope applies it.
  */
 #ifndef RAZOR_H_
 #define RAZOR_H_
@@ -380,6 +380,48 @@ RAZOR_API int razor_cache_device_status(razor_cache_t* cache, int32_t* status, v
  */
 RAZOR_API int razor_cache_set_alibi(razor_cache_t* cache, const float* slopes, void* stream);
 RAZOR_API int razor_cache_set_head_windows(razor_cache_t* cache, int32_t layer, const int32_t* window_h);
+
+/*
+ * Rotary positions of queries and keys: the step between a model's projection and the calls above, which take K and q
+ * after it (Section 3.2).  One launch turns both.
+ *   q, k       host structs describing device rows [B, n_tokens, n_heads, head_dim]; element strides, innermost dimension
+ *              contiguous; base pointers 16-byte aligned, strides multiples of 16 bytes.  The input may be a column range
+ *              of a fused projection, the output another layout (keys as [B, Hkv, N, D]) or the input itself (the same
+ *              pointer and strides); any other overlap is undefined.  NULL, or n_heads = 0: none.
+ *   positions  device int32 [B, n_tokens] contiguous, any values (negative ones turn backwards); NULL: 0, 1, ..
+ *   head_dim   up to 256, a multiple of 16 bytes; dtype RAZOR_F32 or RAZOR_BF16
+ *   rotated    R: the first R values of a row turn (even, 2 <= R <= head_dim), the others are carried over
+ *   inv_freq   host double [R / 2]: angle per position of each pair, in radians (razor_rope_frequencies gives the usual
+ *              ones); angles are right to 32 bits at any position an int32 can hold
+ *   gain       factor on the turned values
+ *   interleaved  0: pair i is (x_i, x_(i + R/2)); 1: (x_2i, x_(2i+1))
+ *   inverse    1: turns back (the transposed rotation, the gradient with respect to x); gain applies as it is
+ * With pair (a, b) at position p:  y_a = gain (x_a cos(p w) - x_b sin(p w)),  y_b = gain (x_b cos(p w) + x_a sin(p w)),
+ * in 32 bits, rounded once.  Nothing is kept from call to call; a captured call replays.
+ * razor_rope_frequencies (host only): w_i = base^(-2i/R), for contexts `factor` times original_len
+ *   RAZOR_ROPE_PLAIN    as it is (factor and original_len are not looked at)
+ *   RAZOR_ROPE_LINEAR   w / factor
+ *   RAZOR_ROPE_NTK      base * factor^(R / (R - 2)) in base's place
+ *   RAZOR_ROPE_YARN     w for pairs that make 32 turns or more over original_len, w / factor for those that make at most
+ *                       one, a ramp over i between; gain 0.1 ln(factor) + 1
+ *   RAZOR_ROPE_BANDED   the same by the number of turns t = original_len w / 2 pi: w from 4 on, w / factor up to 1, linear
+ *                       in t between
+ *   gain: may be NULL; 1 except as said.
+ * Errors: NULL_PTR, INVALID_ARG, UNSUPPORTED_DIM, MISALIGNED, CUDA.
+ */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t in_stride_b, in_stride_t, in_stride_h;    /* elements */
+  int64_t out_stride_b, out_stride_t, out_stride_h;
+  int32_t n_heads;
+} razor_rope_rows_t;
+enum { RAZOR_ROPE_PLAIN = 0, RAZOR_ROPE_LINEAR = 1, RAZOR_ROPE_NTK = 2, RAZOR_ROPE_YARN = 3, RAZOR_ROPE_BANDED = 4 };
+RAZOR_API int razor_rope_frequencies(int32_t rotated, double base, int32_t scaling, double factor, int32_t original_len,
+                                     double* inv_freq, float* gain);
+RAZOR_API int razor_rope(const razor_rope_rows_t* q, const razor_rope_rows_t* k, const int32_t* positions, int32_t batch,
+                         int32_t n_tokens, int32_t head_dim, int32_t rotated, int32_t dtype, const double* inv_freq, float gain,
+                         int32_t interleaved, int32_t inverse, void* stream);
 
 /*
  * Retrieval-head identification, the arithmetic of Section 3.3.  The model is run (by the caller) on

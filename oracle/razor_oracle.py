@@ -406,3 +406,22 @@ def verify_tree(target: np.ndarray, draft: Optional[np.ndarray], tokens: Sequenc
     over = np.nonzero((upto > float(r) * upto[-1]) & (w > 0))[0]
     with_weight = np.nonzero(w > 0)[0]
     return path, int(over[0]) if len(over) else int(with_weight[-1]) if len(with_weight) else -1
+
+
+# ----------------------------------------------------------------------------- around the cache
+def rope(x, positions, inv_freq, interleaved=False, inverse=False, gain=1.0):
+    """x [..., D], positions [...] (of the leading dimensions it broadcasts to), inv_freq [R / 2]: the first R values turned."""
+    x = np.asarray(x, dtype=np.float64)
+    w = np.asarray(inv_freq, dtype=np.float64)
+    R = 2 * w.size
+    angle = np.asarray(positions, dtype=np.float64)[..., None] * w * (-1.0 if inverse else 1.0)
+    z = x[..., :R].reshape(*x.shape[:-1], R // 2, 2) if interleaved else np.stack([x[..., :R // 2], x[..., R // 2:R]], -1)
+    z = (z[..., 0] + 1j * z[..., 1]) * np.exp(1j * angle)
+    out = x.copy()
+    if interleaved:
+        out[..., 0:R:2], out[..., 1:R:2] = z.real, z.imag
+    else:
+        out[..., :R // 2], out[..., R // 2:R] = z.real, z.imag
+    # the gain belongs to the turned values only
+    out[..., :R] *= gain
+    return out

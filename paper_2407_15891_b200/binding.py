@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
@@ -30,7 +31,7 @@ SYMBOLS = [
     "razor_decode_attention_tree", "razor_append_tree", "razor_verify_tree", "razor_cache_export", "razor_cache_stats", "razor_schedule_plan",
     "razor_schedule_query", "razor_schedule_combine_heads", "razor_cache_set_option", "razor_cache_device_status", "razor_cache_wait_selftest", "razor_cache_set_alibi", "razor_cache_set_head_windows",
     "razor_compensation_mean_static", "razor_head_scores_scratch_bytes", "razor_head_scores",
-    "razor_select_retrieval_heads", "razor_cache_reset", "razor_cache_destroy", "razor_status_string",
+    "razor_select_retrieval_heads", "razor_rope_frequencies", "razor_rope", "razor_cache_reset", "razor_cache_destroy", "razor_status_string",
     "razor_last_cuda_error", "razor_version",
 ]
 
@@ -51,6 +52,10 @@ class RazorConfig(C.Structure):
         ("max_ctx_len", C.c_int32), ("max_new_tokens", C.c_int32), ("use_compensation", C.c_int32),
         ("page_shuffle_seed", C.c_int32), ("sm_scale", C.c_float),
     ]
+
+
+# razor_rope_rows_t: in, out, strides of in and out over (batch, token, head), heads
+RopeRows = struct.Struct("@PP6qi4x")
 
 
 _lib: Optional[C.CDLL] = None
@@ -96,6 +101,9 @@ def load() -> C.CDLL:
     lib.razor_head_scores_scratch_bytes.argtypes = [i32, i32, C.POINTER(sz)]
     lib.razor_head_scores.argtypes = [vp, vp, i32, i32, i32, i32, i32, C.c_float, vp, vp, vp, sz, vp]
     lib.razor_select_retrieval_heads.argtypes = [vp, vp, i32, C.c_float, C.c_float, vp]
+    lib.razor_rope_frequencies.argtypes = [i32, C.c_double, i32, C.c_double, i32, vp, C.POINTER(C.c_float)]
+    lib.razor_rope.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, C.c_float,
+                               i32, i32, vp]
     lib.razor_cache_reset.argtypes = [vp]
     lib.razor_cache_destroy.argtypes = [vp]
     lib.razor_status_string.argtypes = [C.c_int]
@@ -415,6 +423,52 @@ def razor_select_retrieval_heads(echo, induction, frac_induction: float = 0.14, 
     _check(load().razor_select_retrieval_heads(e.ctypes.data, i.ctypes.data, e.size, frac_induction, frac_echo,
                                                mask.ctypes.data), "razor_select_retrieval_heads")
     return mask
+
+
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "banded": 4}
+
+
+def razor_rope_frequencies(rotated: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                           original_len: int = 0) -> Tuple[np.ndarray, float]:
+    """Host-only: -> (angle per position of every pair, float64 [rotated / 2]; gain of the turned values)."""
+    w, gain = np.empty(max(1, rotated // 2), dtype=np.float64), C.c_float(1.0)
+    _check(load().razor_rope_frequencies(rotated, base, ROPE_SCALINGS[scaling], factor, original_len, w.ctypes.data,
+                                         C.byref(gain)), "razor_rope_frequencies")
+    return w, gain.value
+
+
+def _rope_rows(x: Optional[torch.Tensor], out: Optional[torch.Tensor]) -> Optional[bytes]:
+    if x is None:
+        assert out is None
+        return None
+    shape, (x_b, x_t, x_h, x_d), (o_b, o_t, o_h, o_d) = x.shape, x.stride(), out.stride()
+    assert out.shape == shape and out.dtype is x.dtype and out.device == x.device and x_d == 1 and o_d == 1
+    return RopeRows.pack(x.data_ptr(), out.data_ptr(), x_b, x_t, x_h, o_b, o_t, o_h, shape[2])
+
+
+def razor_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], inv_freq: np.ndarray,
+               positions: Optional[torch.Tensor] = None, interleaved: bool = False, inverse: bool = False, gain: float = 1.0,
+               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
+    """q, k (either may be None): device [B, T, heads, D] fp32 or bf16, strided, innermost dimension contiguous; inv_freq host
+    float64 [R / 2]; positions device int32 [B, T] (None: 0, 1, ..).  -> (q_out, k_out): the tensors given (the inputs
+    themselves turn in place), or new contiguous ones."""
+    x = q if q is not None else k
+    B, T, _, D = x.shape
+    dev, dtype = x.device, x.dtype
+    assert q is None or k is None or (k.shape[:2] == q.shape[:2] and k.shape[3] == D and k.dtype is dtype and k.device == dev)
+    assert inv_freq.dtype == np.float64 and inv_freq.ndim == 1 and inv_freq.strides == (8,)
+    if positions is not None:
+        assert positions.shape == (B, T) and positions.dtype is torch.int32 and positions.is_contiguous()
+        assert positions.device == dev
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=dtype, device=dev)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=dtype, device=dev)
+    rq, rk = _rope_rows(q, q_out), _rope_rows(k, k_out)
+    with _on(dev):
+        _check(load().razor_rope(rq, rk, _ptr(positions), B, T, D, 2 * inv_freq.size, _VERIFY_DTYPES[dtype],
+                                 inv_freq.__array_interface__["data"][0], gain, interleaved, inverse, _stream(stream)), "razor_rope")
+    return q_out, k_out
 
 
 def razor_cache_reset(cache: int) -> None:
