@@ -424,6 +424,39 @@ RAZOR_API int razor_rope(const razor_rope_rows_t* q, const razor_rope_rows_t* k,
                          int32_t interleaved, int32_t inverse, void* stream);
 
 /*
+ * Attention of prompt tokens over dense K and V: what a prefill computes from the rows that razor_compress packs
+ * afterwards.  Causal, with a sliding window and the first n_sink tokens for each KV head - the sets Algorithm 1 keeps -, or
+ * everything (a retrieval head).  No cache is needed.
+ *   q          device bf16 [B, n_tokens, Hq, D], element strides q_stride_b / q_stride_t, the heads of a token contiguous
+ *   K, V       device bf16 [B, Hkv, n_ctx, D], element strides kv_stride_b / _h / _n (razor_compress's buffers)
+ *   window     device int32 [B, Hkv]: recent tokens a head's queries see, their own included; < 0: everything (the queries
+ *              of a KV head's group see the same).  NULL: every head sees everything
+ *   q_len      device int32 [B]: queries of each sequence, its first q_len rows of q; NULL: n_tokens.  ctx_len device int32
+ *              [B]: tokens of K and V; NULL: n_ctx.  (Values outside 0 .. n_tokens and 0 .. n_ctx count as the nearest.)
+ *   out        device bf16 [B, n_tokens, Hq, D] contiguous; rows at or beyond q_len[b] are left as they were
+ * Query t of sequence b sits at position m = ctx_len[b] - q_len[b] + t (a prompt's later chunk attends to what came before it;
+ * a single token is a decode step over a context that is not compressed) and sees key n when n <= m and (n < n_sink or
+ * window < 0 or m - n < window).  out = softmax(sm_scale q.k) v over those, in fp32 with weights rounded to bf16 for the
+ * product with V; zeros when there are none.  sm_scale 0 means 1/sqrt(head_dim).
+ * What is not finite shows in the rows that see it and in no other: a NaN or an infinity in q or in a K makes rows NaN, one in
+ * a V appears in its dimension.  Rows of K and V that no query sees may hold anything.
+ * head_dim 64 or 128; Hq / Hkv up to 128.  Bases 16-byte aligned, strides multiples of 16 bytes and at least head_dim (of a
+ * dimension of size one they are not looked at); workspace 256-byte aligned, its content on entry does not matter, calls that
+ * may run at the same time need their own (captured graphs that are replayed side by side too).
+ * The lengths and windows are read on the device: a replay of a captured call uses what they hold then.
+ * Every wait in the kernel is bounded in time; should one ever run out, rows of the call are left NaN or as they were.
+ * Errors: NULL_PTR, INVALID_ARG, UNSUPPORTED_DIM, MISALIGNED, POOL_TOO_SMALL (workspace), CAPACITY (over 2^30 units of work), CUDA.
+ */
+RAZOR_API int razor_window_attention_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                                     int32_t n_tokens, size_t* bytes);
+RAZOR_API int razor_window_attention(const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* K, const void* V,
+                                     int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_n, const int32_t* window,
+                                     const int32_t* q_len, const int32_t* ctx_len, int32_t batch, int32_t n_tokens,
+                                     int32_t n_ctx, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                     int32_t n_sink, float sm_scale, void* out, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
+/*
  * Retrieval-head identification, the arithmetic of Section 3.3.  The model is run (by the caller) on
  * `period` random tokens repeated several times; for one layer's heads this call takes their
  * post-rotary queries and keys on that input and returns, per head, the echo score (causal-softmax

@@ -425,3 +425,18 @@ def rope(x, positions, inv_freq, interleaved=False, inverse=False, gain=1.0):
     # the gain belongs to the turned values only
     out[..., :R] *= gain
     return out
+
+
+def window_attention(q, K, V, ctx, window, n_sink, scale):
+    """One query head: q [T, D] at positions ctx - T .. ctx - 1 over K, V [>= ctx, D]; window < 0: everything.  Rows that see
+    nothing are zeros."""
+    q, K, V = (np.asarray(x, dtype=np.float64) for x in (q, K, V))
+    out = np.zeros_like(q)
+    for t in range(q.shape[0]):
+        m = ctx - q.shape[0] + t
+        see = [n for n in range(m + 1) if n < n_sink or window < 0 or m - n < window]
+        if see:
+            s = K[see] @ q[t] * scale
+            w = np.exp(s - s.max())
+            out[t] = w @ V[see] / w.sum()
+    return out

@@ -31,7 +31,8 @@ SYMBOLS = [
     "razor_decode_attention_tree", "razor_append_tree", "razor_verify_tree", "razor_cache_export", "razor_cache_stats", "razor_schedule_plan",
     "razor_schedule_query", "razor_schedule_combine_heads", "razor_cache_set_option", "razor_cache_device_status", "razor_cache_wait_selftest", "razor_cache_set_alibi", "razor_cache_set_head_windows",
     "razor_compensation_mean_static", "razor_head_scores_scratch_bytes", "razor_head_scores",
-    "razor_select_retrieval_heads", "razor_rope_frequencies", "razor_rope", "razor_cache_reset", "razor_cache_destroy", "razor_status_string",
+    "razor_select_retrieval_heads", "razor_rope_frequencies", "razor_rope",
+    "razor_window_attention_workspace_bytes", "razor_window_attention", "razor_cache_reset", "razor_cache_destroy", "razor_status_string",
     "razor_last_cuda_error", "razor_version",
 ]
 
@@ -104,6 +105,9 @@ def load() -> C.CDLL:
     lib.razor_rope_frequencies.argtypes = [i32, C.c_double, i32, C.c_double, i32, vp, C.POINTER(C.c_float)]
     lib.razor_rope.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, C.c_float,
                                i32, i32, vp]
+    lib.razor_window_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, C.POINTER(sz)]
+    lib.razor_window_attention.argtypes = [vp, i64, i64, vp, vp, i64, i64, i64, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
+                                           i32, C.c_float, vp, vp, sz, vp]
     lib.razor_cache_reset.argtypes = [vp]
     lib.razor_cache_destroy.argtypes = [vp]
     lib.razor_status_string.argtypes = [C.c_int]
@@ -469,6 +473,46 @@ def razor_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], inv_freq: n
         _check(load().razor_rope(rq, rk, _ptr(positions), B, T, D, 2 * inv_freq.size, _VERIFY_DTYPES[dtype],
                                  inv_freq.__array_interface__["data"][0], gain, interleaved, inverse, _stream(stream)), "razor_rope")
     return q_out, k_out
+
+
+def razor_window_attention_workspace_bytes(batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, n_tokens: int) -> int:
+    need = C.c_size_t(0)
+    _check(load().razor_window_attention_workspace_bytes(batch, n_q_heads, n_kv_heads, head_dim, n_tokens, C.byref(need)),
+           "razor_window_attention_workspace_bytes")
+    return need.value
+
+
+def razor_window_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, n_sink: int,
+                           window: Optional[torch.Tensor] = None, q_len: Optional[torch.Tensor] = None,
+                           ctx_len: Optional[torch.Tensor] = None, sm_scale: float = 0.0, out: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """q bf16 [B, T, Hq, D] (strided over b and t), K, V bf16 [B, Hkv, N, D] (strided, the same strides); window int32
+    [B, Hkv], q_len, ctx_len int32 [B] on the device or None.  -> out bf16 [B, T, Hq, D]; rows beyond a sequence's queries are
+    left as they are (zeros when `out` is not given).  workspace: uint8, razor_window_attention_workspace_bytes long; one is
+    allocated when none is given (on the current stream: give one with a `stream` of your own)."""
+    (B, T, Hq, D), (_, Hk, N, _), dev = q.shape, K.shape, q.device
+    q_b, q_t, q_h, q_d = q.stride()
+    kv = K.stride()
+    assert q.dtype is torch.bfloat16 and K.dtype is torch.bfloat16 and V.dtype is torch.bfloat16
+    assert K.shape == V.shape == (B, Hk, N, D) and kv == V.stride() and kv[3] == 1 and q_d == 1 and (Hq == 1 or q_h == D)
+    assert K.device == dev and V.device == dev
+    for x, shape in ((window, (B, Hk)), (q_len, (B,)), (ctx_len, (B,))):
+        assert x is None or (x.shape == shape and x.dtype is torch.int32 and x.is_contiguous() and x.device == dev)
+    if out is None:
+        out = torch.zeros((B, T, Hq, D), dtype=torch.bfloat16, device=dev)
+    else:
+        assert out.shape == q.shape and out.dtype is torch.bfloat16 and out.is_contiguous() and out.device == dev
+    need = razor_window_attention_workspace_bytes(B, Hq, Hk, D, T)
+    with _on(dev):
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        assert workspace.device == dev and workspace.is_contiguous()
+        _check(load().razor_window_attention(q.data_ptr(), q_b, q_t, K.data_ptr(), V.data_ptr(), *kv[:3], _ptr(window),
+                                             _ptr(q_len), _ptr(ctx_len), B, T, N, Hq, Hk, D, RAZOR_BF16, n_sink, sm_scale,
+                                             out.data_ptr(), workspace.data_ptr(),
+                                             workspace.numel() * workspace.element_size(), _stream(stream)),
+               "razor_window_attention")
+    return out
 
 
 def razor_cache_reset(cache: int) -> None:

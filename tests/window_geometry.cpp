@@ -1,0 +1,76 @@
+// razor_window.h against what it stands for: the key tiles that hold a key some query of a tile sees, found one by one.
+#include <cstdio>
+#include <cstdlib>
+
+#include "razor_window.h"
+
+using namespace razor;
+
+static unsigned long long rng_state = 1;
+static int rnd(int lo, int hi) {   // lo .. hi
+  rng_state = rng_state * 6364136223846793005ull + 1442695040888963407ull;
+  return lo + (int)((rng_state >> 33) % (unsigned long long)(hi - lo + 1));
+}
+static bool sees(int m, int n, int window, int n_sink) { return n <= m && (n < n_sink || window < 0 || m - n < window); }
+#define CHECK(x) do { if (!(x)) { std::printf("line %d: %s (case %d)\n", __LINE__, #x, at); return 1; } } while (0)
+
+int main() {
+  for (int at = 0; at < 4000; ++at) {
+    const int G = rnd(1, 8), tpt = kWinTile / G;
+    const int ctx = rnd(0, 3) ? rnd(0, 1500) : rnd(0, 40), q_len = rnd(0, 5) ? rnd(0, ctx) : rnd(0, ctx + 300);
+    const int window = rnd(0, 4) == 0 ? -1 : rnd(0, 3) ? rnd(0, 700) : rnd(0, 3);
+    const int n_sink = rnd(0, 2) ? rnd(0, 5) : rnd(0, 600);
+    for (int tok0 = 0; tok0 < q_len + 2 * tpt; tok0 += 2 * tpt) {
+      const WinUnit u = win_unit(tok0, tpt, q_len, ctx, window, n_sink);
+      int live = q_len - tok0;
+      live = live < 0 ? 0 : live > 2 * tpt ? 2 * tpt : live;
+      CHECK(u.live == live);
+      CHECK((u.weight() == 0) == (live == 0) && u.n_steps >= 0);
+      CHECK(u.tile[0].n_tok + u.tile[1].n_tok == live);
+      for (int j = 1; j < u.n_steps; ++j) CHECK(u.key_tile(j) > u.key_tile(j - 1));
+      if (u.n_steps) CHECK(u.key_tile(0) >= 0 && u.key_tile(u.n_steps - 1) * kWinTile < ctx);
+      for (int i = 0; i < 2; ++i) {
+        const WinTileSteps& t = u.tile[i];
+        if (t.n_tok == 0) { CHECK(t.steps_in(0, u.n_steps) == 0); continue; }
+        CHECK(t.tok == tok0 + i * tpt && t.pos == ctx - q_len + t.tok);
+        const int first = t.pos, last = t.pos + t.n_tok - 1;
+        int n_active = 0, j_of[16];
+        for (int k = 0; k < 16; ++k) j_of[k] = -1;
+        for (int j = 0; j < u.n_steps; ++j) {
+          j_of[u.key_tile(j)] = j;
+          n_active += t.active(j);
+        }
+        CHECK(t.steps_in(0, u.n_steps) == n_active);
+        const int cut = rnd(0, u.n_steps);
+        CHECK(t.steps_in(0, cut) + t.steps_in(cut, u.n_steps) == n_active);
+        for (int kt = 0; kt * kWinTile < ctx; ++kt) {
+          bool any = false, all = true;
+          for (int m = first; m <= last; ++m)
+            for (int n = kt * kWinTile; n < (kt + 1) * kWinTile; ++n) {
+              const bool s = sees(m, n, window, n_sink);
+              any |= s;
+              all &= s;
+            }
+          // a tile that some query sees is a step the tile takes part in; one whose mask is left out is seen by all
+          if (any) CHECK(j_of[kt] >= 0 && t.active(j_of[kt]));
+          if (!win_masked(kt, first, last, window, n_sink)) CHECK(all);
+          if (all) CHECK(!win_masked(kt, first, last, window, n_sink) || last - first + 1 < 1 || n_sink > 0);
+        }
+      }
+    }
+  }
+  for (int at = 0; at < 20000; ++at) {
+    const long long total = rnd(1, 5) == 1 ? rnd(1, 30) : (long long)rnd(1, 2000000) * rnd(1, 3000);
+    const int ctas = rnd(1, kWinMaxSpans), n = win_n_spans(total, ctas);
+    CHECK(n >= 1 && n <= ctas && n <= total);
+    CHECK(win_span_begin(total, n, 0) == 0 && win_span_begin(total, n, n) == total);
+    for (int k = 0; k < 20; ++k) {
+      const int c = rnd(0, n - 1);
+      const long long b = win_span_begin(total, n, c), e = win_span_begin(total, n, c + 1);
+      CHECK(b < e);
+      CHECK(win_span_of(total, n, b) == c && win_span_of(total, n, e - 1) == c);
+    }
+  }
+  std::printf("ok\n");
+  return 0;
+}
