@@ -11,7 +11,9 @@
 //     tensor memory, mask, running maximum and sum, weights as bf16 back into tensor memory, over the scores;
 //   * warp 8: TMA copies (Q per tile, a ring of K tiles, a ring of V tiles, 128-byte swizzle) and the walk over the units;
 //   * warp 9, one thread: the matrix instructions.  S_i = Q_i K^T (both operands in shared memory), O_i += P_i V (P out of
-//     tensor memory).  While one tile is in its softmax the other one's products run: PV_0, QK_0, PV_1, QK_1, ..;
+//     tensor memory, as soon as its first half is there).  While one tile is in its softmax the other one's products run:
+//     PV_0, QK_0, PV_1, QK_1, ..  (An issuing thread for each tile was tried: the tiles then drift into step, both in their
+//     softmax at once, and 32K tokens took 9.0 ms for 8.5.)
 //   * warps 10, 11: look over the V tiles that are partly masked.  A weight of zero times a NaN or an infinity is a NaN, so
 //     such values are zeroed in shared memory, and put back into the rows that do see them at the end (rows that a mask
 //     hides from a token are never touched by it, whatever it holds).
@@ -41,8 +43,11 @@ namespace razor {
 namespace {
 
 constexpr int kWinThreads = 384;
+// Registers: 168 a thread at launch; the softmax threads, which hold a row of 128 scores, take over what the others give up.
+constexpr int kWinLaunchRegs = 168, kWinSoftmaxRegs = 216, kWinOtherRegs = 72;
+static_assert(256 * kWinSoftmaxRegs + 128 * kWinOtherRegs <= kWinThreads * kWinLaunchRegs, "no more than the block was launched with");
 constexpr int kHalfBytes = kWinTile * 128;   // 128 rows of 64 elements
-constexpr int kWinPolyEvery = 0;             // of so many pairs of exponentials one is a polynomial (0: none)
+constexpr int kWinPolyEvery = 3;             // of so many pairs of exponentials one is a polynomial (0: none)
 
 template <int D>
 struct WinCfg {
@@ -65,7 +70,7 @@ struct WinCall {
   float scale_log2;
   // workspace
   int32_t* queue;
-  longlong2* table;         // [n_units + 1]: first step and weight of every unit; the last: (total, 0)
+  int2* table;              // [n_units]: the first span with a part of the unit, and its parts (0: no query in it)
   float2* rec_ml;           // [2 * kWinMaxSpans][rec_rows]
   float* rec_o;             // [2 * kWinMaxSpans][rec_rows][D]
 };
@@ -81,7 +86,7 @@ struct WinItem {
 struct WinCtl {
   uint64_t q_full[2], q_empty[2];
   uint64_t k_full[4], k_empty[4], v_full[4], v_clean[4], v_empty[4];
-  uint64_t s_full[2], p_full[2], o_full[2];
+  uint64_t s_full[2], p_full[2][2], o_full[2];   // (P in two halves: its product begins with the first)
   uint64_t item_full[2], item_empty[2];
   uint64_t drain;
   WinItem item[2];
@@ -116,10 +121,56 @@ __device__ __forceinline__ void win_tmem_st32(uint32_t taddr, const uint32_t* v)
         "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
       : "memory");
 }
+// Scales 16 columns of this thread's lane.
+__device__ __forceinline__ void win_tmem_scale16(uint32_t taddr, float f) {
+  uint32_t o[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]), "=r"(o[8]),
+        "=r"(o[9]), "=r"(o[10]), "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
+      : "r"(taddr)
+      : "memory");
+  tmem_ld_wait_all();
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    asm volatile("" : "+r"(o[e]));
+    o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+  }
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      :
+      : "r"(taddr), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "r"(o[8]),
+        "r"(o[9]), "r"(o[10]), "r"(o[11]), "r"(o[12]), "r"(o[13]), "r"(o[14]), "r"(o[15])
+      : "memory");
+}
 __device__ __forceinline__ void win_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t win_pack2(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *(const uint32_t*)&v;
+}
+// One matrix instruction, the descriptors as (low word, high word); the second with operand A out of tensor memory.
+__device__ __forceinline__ void win_umma(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                         uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+      "setp.ne.b32 p, %6, 0;\n\t"
+      "mov.b64 a, {%1, %2};\n\t"
+      "mov.b64 b, {%3, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}"
+      :
+      : "r"(tmem_d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate));
+}
+__device__ __forceinline__ void win_umma_tmem_a(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                                uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+      "setp.ne.b32 p, %5, 0;\n\t"
+      "mov.b64 b, {%2, %3};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+      :
+      : "r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate));
 }
 // the larger of three values, NaN if one is
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
@@ -146,8 +197,9 @@ __device__ __forceinline__ WinUnit find_unit(const WinCall& c, int unit, int& b,
 // Infinities and NaNs of V that were zeroed for the sake of rows that do not see them, added to a row that does: positions
 // of the masked tiles among the row's steps.  Rare, and slow.
 template <int D, typename Add>
-__device__ __noinline__ void restore_non_finite(const WinCall& c, const WinItem& it, const WinTileSteps& t, int pos, Add add) {
+__device__ __forceinline__ void restore_non_finite(const WinCall& c, const WinItem& it, const WinTileSteps& t, int pos, Add add) {
   const __nv_bfloat16* v = c.v + it.b * c.v_stride_b + it.g * c.v_stride_h;
+#pragma unroll 1
   for (int j = it.j0; j < it.j1; ++j) {
     const int kt = it.u.key_tile(j);
     // (looked over: the tiles that are masked for either tile of the unit)
@@ -157,9 +209,11 @@ __device__ __noinline__ void restore_non_finite(const WinCall& c, const WinItem&
       looked |= o.active(j) && win_masked(kt, o.pos, o.pos + o.n_tok - 1, it.window, c.n_sink);
     }
     if (!looked || !t.active(j)) continue;
+#pragma unroll 1
     for (int n = kt * kWinTile; n < kt * kWinTile + kWinTile && n <= pos; ++n) {
       if (!(it.window < 0 || n < c.n_sink || pos - n < it.window)) continue;
       const __nv_bfloat16* row = v + (int64_t)n * c.v_stride_n;
+#pragma unroll 1
       for (int d = 0; d < D; ++d)
         if (!finite_bf16(row[d])) add(d, __bfloat162float(row[d]));
     }
@@ -214,18 +268,19 @@ __global__ void __launch_bounds__(kWinThreads, 1)
       if (k < warp) before += ctl->scan[k];
       total += ctl->scan[k];
     }
-    if (blockIdx.x == 0) {
+    n_spans = total > 0 ? win_n_spans(total, (int)gridDim.x) : 1;
+    if (blockIdx.x == gridDim.x - 1) {   // (the CTA that is likeliest to have no span)
       long long at = before;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int unit = (int)threadIdx.x * PER + i;
-        if (unit < c.n_units) c.table[unit] = make_longlong2(at, w[i]);
+        int first = 0, parts = 0;
+        if (w[i] > 0) win_unit_spans(total, n_spans, at, w[i], first, parts);
+        if (unit < c.n_units) c.table[unit] = make_int2(first, parts);
         at += w[i];
       }
-      if (threadIdx.x == 0) c.table[c.n_units] = make_longlong2(total, 0);
     }
     if (total == 0) return;
-    n_spans = win_n_spans(total, (int)gridDim.x);
     if ((int)blockIdx.x >= n_spans) return;
     span_at = win_span_begin(total, n_spans, blockIdx.x);
     span_end = win_span_begin(total, n_spans, blockIdx.x + 1);
@@ -245,7 +300,8 @@ __global__ void __launch_bounds__(kWinThreads, 1)
       mbar_init(&ctl->q_full[i], 1);
       mbar_init(&ctl->q_empty[i], 1);
       mbar_init(&ctl->s_full[i], 1);
-      mbar_init(&ctl->p_full[i], 128);
+      mbar_init(&ctl->p_full[i][0], 128);
+      mbar_init(&ctl->p_full[i][1], 128);
       mbar_init(&ctl->o_full[i], 1);
       mbar_init(&ctl->item_full[i], 1);
       mbar_init(&ctl->item_empty[i], kItemReaders);
@@ -273,6 +329,7 @@ __global__ void __launch_bounds__(kWinThreads, 1)
   const uint32_t tmem = ctl->tmem_base;
 
   if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kWinSoftmaxRegs));
     // ================================================================ softmax and epilogue: a thread per query row
     const int ti = warp >> 2;                     // tile
     const int row = (warp & 3) * 32 + lane;
@@ -303,7 +360,8 @@ __global__ void __launch_bounds__(kWinThreads, 1)
         ++n_s;
         tc_fence_after();
         if (!warp_live) {   // nobody reads these rows
-          mbar_arrive(&ctl->p_full[ti]);
+          mbar_arrive(&ctl->p_full[ti][0]);
+          mbar_arrive(&ctl->p_full[ti][1]);
           continue;
         }
         uint32_t v[kWinTile];
@@ -338,17 +396,7 @@ __global__ void __launch_bounds__(kWinThreads, 1)
           const float f = (m_to == -CUDART_INF_F || m_ref == -CUDART_INF_F) ? 0.f : fast_exp2(m_ref - m_to);
           if (!first) {
 #pragma unroll
-            for (int k = 0; k < D / 32; ++k) {
-              uint32_t o[32];
-              tmem_ld32_issue(o_addr + (uint32_t)(k * 32), o);
-              tmem_ld_wait_all();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                asm volatile("" : "+r"(o[e]));
-                o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              }
-              win_tmem_st32(o_addr + (uint32_t)(k * 32), o);
-            }
+            for (int k = 0; k < D / 16; ++k) win_tmem_scale16(o_addr + (uint32_t)(k * 16), f);
           }
           l_run *= f;
           m_ref = m_to;
@@ -377,13 +425,13 @@ __global__ void __launch_bounds__(kWinThreads, 1)
             p[e2] = win_pack2(w0, w1);
           }
           win_tmem_st32(s_addr + (uint32_t)(h * 32), p);
+          win_tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(&ctl->p_full[ti][h]);
         }
         float a0, a1;
         f2_unpack(f2_add(psum[0], psum[1]), a0, a1);
         l_run += a0 + a1;
-        win_tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(&ctl->p_full[ti]);
         first = false;
       }
       if (ok && cnt > 0) {
@@ -445,7 +493,9 @@ __global__ void __launch_bounds__(kWinThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl->item_empty[gi & 1]);
     }
-  } else if (warp == 8) {
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWinOtherRegs));
+    if (warp == 8) {
     // ================================================================ work and copies: one thread
     if (lane == 0) {
       unsigned kc = 0, vc = 0, nq[2] = {0, 0};
@@ -467,17 +517,20 @@ __global__ void __launch_bounds__(kWinThreads, 1)
           }
           w.unit = unit;
           w.poison = 0;
-          w.j0 = step;
-          w.j1 = c.spans ? (int)min((long long)weight, step + (span_end - span_at)) : weight;
-          w.slot = w.j0 == 0 && w.j1 == weight ? -1 : 2 * (int)blockIdx.x + (w.j0 == 0 ? 1 : 0);
           if (c.spans) {
-            span_at += w.j1 - w.j0;
-            if (w.j1 == weight) ++unit, step = 0;
-            else step = w.j1;
+            const long long z = min((long long)weight, step + (span_end - span_at));
+            const bool some = w.u.part(step, z, w.j0, w.j1);
+            span_at += z - step;
+            if (z == weight) ++unit, step = 0;
+            else step = (int)z;
+            if (!some) continue;
+            w.slot = w.j0 == 0 && w.j1 == w.u.n_steps ? -1 : 2 * (int)blockIdx.x + (w.j0 == 0 ? 1 : 0);
           } else {
+            w.j0 = 0;
+            w.j1 = w.u.n_steps;
+            w.slot = -1;
             unit = (int)gridDim.x + atomicAdd(c.queue, 1);
           }
-          w.j1 = min(w.j1, w.u.n_steps);   // (a unit that sees nothing has no step)
         }
         if (gi >= 2) ok = mbar_wait(&ctl->item_empty[gi & 1], ((gi >> 1) - 1) & 1, abort_flag);
         if (!ok) break;
@@ -530,74 +583,79 @@ __global__ void __launch_bounds__(kWinThreads, 1)
     if (lane == 0) {
       unsigned kc = 0, vc = 0, nq[2] = {0, 0}, np[2] = {0, 0};
       bool ok = true;
+      // descriptors as words: only the start address (low word, 16-byte units) changes
+      const uint64_t q_desc = operand_desc(smem_u32(q_tile)), k_desc = operand_desc(smem_u32(k_tile));
+      const uint64_t v_desc = operand_desc_mn(smem_u32(v_tile), kHalfBytes, 1024);
+      const uint32_t q_lo = (uint32_t)q_desc, k_lo = (uint32_t)k_desc, v_lo = (uint32_t)v_desc;
+      const uint32_t kmajor_hi = (uint32_t)(k_desc >> 32), v_hi = (uint32_t)(v_desc >> 32);
       for (unsigned gi = 0; ok; ++gi) {
         ok = mbar_wait(&ctl->item_full[gi & 1], (gi >> 1) & 1, abort_flag);
         if (!ok) break;
         const WinItem& it = ctl->item[gi & 1];
         if (it.unit < 0) break;
         const int j0 = it.j0, j1 = it.j1;
-        const WinTileSteps t[2] = {it.u.tile[0], it.u.tile[1]};
+        const WinTileSteps t0 = it.u.tile[0], t1 = it.u.tile[1];
         mbar_arrive(&ctl->item_empty[gi & 1]);
-        int left_q[2], left_p[2];
-        bool fresh[2] = {true, true};   // the accumulator holds nothing of this item yet
-#pragma unroll
-        for (int i = 0; i < 2; ++i) left_q[i] = left_p[i] = t[i].steps_in(j0, j1);
-        const int cnt[2] = {left_q[0], left_q[1]};
+        const int cnt[2] = {t0.steps_in(j0, j1), t1.steps_in(j0, j1)};
+        int left_q[2] = {cnt[0], cnt[1]}, left_p[2] = {cnt[0], cnt[1]};
         // S_i = Q_i K^T of the K tile in stage ks
-        auto qk = [&](int i, int ks) -> bool {
+        auto qk = [&](const int i, uint32_t ks) -> bool {
           if (left_q[i] == cnt[i]) {
             if (!mbar_wait(&ctl->q_full[i], nq[i] & 1, abort_flag)) return false;
             ++nq[i];
           }
           tc_fence_after();
-          const uint32_t a0 = smem_u32(q_tile + i * TB), b0 = smem_u32(k_tile + ks * TB);
+          const uint32_t a_lo = q_lo + (uint32_t)i * (TB >> 4), b_lo = k_lo + ks * (TB >> 4);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
-            const uint32_t off = (uint32_t)((kk >> 2) * kHalfBytes + (kk & 3) * 32);
-            umma_bf16_desc(tmem + (uint32_t)(i * kWinTile), operand_desc(a0 + off), operand_desc(b0 + off), kIdescQK, kk > 0);
+            const uint32_t off = (uint32_t)((kk >> 2) * kHalfBytes + (kk & 3) * 32) >> 4;
+            win_umma(tmem + (uint32_t)(i * kWinTile), a_lo + off, kmajor_hi, b_lo + off, kmajor_hi, kIdescQK, kk > 0);
           }
           umma_commit(&ctl->s_full[i]);
           if (--left_q[i] == 0) umma_commit(&ctl->q_empty[i]);
           return true;
         };
-        auto pv = [&](int i, int vs) -> bool {
-          if (!mbar_wait(&ctl->p_full[i], np[i] & 1, abort_flag)) return false;
-          ++np[i];
-          tc_fence_after();
-          const uint32_t p0 = tmem + (uint32_t)(i * kWinTile), o0 = tmem + 2 * kWinTile + (uint32_t)(i * kWinTile);
-          const uint32_t v0 = smem_u32(v_tile + vs * TB);
+        // O_i += P_i V of the V tile in stage vs
+        auto pv = [&](const int i, uint32_t vs) -> bool {
+          const uint32_t b_lo = v_lo + vs * (TB >> 4), s_col = tmem + (uint32_t)(i * kWinTile);
+          const uint32_t more = left_p[i] != cnt[i];   // the accumulator holds products of this item
 #pragma unroll
-          for (int kk = 0; kk < kWinTile / 16; ++kk)   // 16 tokens per instruction: 8 columns of bf16 pairs
-            umma_bf16_tmem_a(o0, p0 + (uint32_t)(kk * 8), operand_desc_mn(v0 + (uint32_t)(kk * 16 * 128), kHalfBytes, 1024),
-                             kIdescPV, (kk > 0 || !fresh[i]) ? 1u : 0u);
-          fresh[i] = false;
+          for (int kk = 0; kk < kWinTile / 16; ++kk) {   // 16 tokens per instruction: 8 columns of bf16 pairs
+            if (kk % (kWinTile / 32) == 0) {
+              if (!mbar_wait(&ctl->p_full[i][kk / (kWinTile / 32)], np[i] & 1, abort_flag)) return false;
+              tc_fence_after();
+            }
+            win_umma_tmem_a(tmem + 2 * kWinTile + (uint32_t)(i * kWinTile), s_col + (uint32_t)(kk * 8),
+                            b_lo + (uint32_t)(kk * 16 * 128 >> 4), v_hi, kIdescPV, kk > 0 ? 1u : more);
+          }
+          ++np[i];
           if (--left_p[i] == 0) umma_commit(&ctl->o_full[i]);
           return true;
         };
         if (j0 < j1) {
-          const int ks = kc % KS;
+          const uint32_t ks = kc % KS;
           ok = mbar_wait(&ctl->k_full[ks], (kc / KS) & 1, abort_flag);
-          if (ok && t[0].active(j0)) ok = qk(0, ks);
-          if (ok && t[1].active(j0)) ok = qk(1, ks);
+          if (ok && t0.active(j0)) ok = qk(0, ks);
+          if (ok && t1.active(j0)) ok = qk(1, ks);
           if (!ok) break;
           umma_commit(&ctl->k_empty[ks]);
           ++kc;
         }
         for (int j = j0; j < j1 && ok; ++j) {
-          const int ks = kc % KS, vs = vc % VS;
+          const uint32_t ks = kc % KS, vs = vc % VS;
           const bool next = j + 1 < j1;
           ok = mbar_wait(&ctl->v_clean[vs], (vc / VS) & 1, abort_flag);
-          if (ok && t[0].active(j)) ok = pv(0, vs);
+          if (ok && t0.active(j)) ok = pv(0, vs);
           if (ok && next) {
             ok = mbar_wait(&ctl->k_full[ks], (kc / KS) & 1, abort_flag);
-            if (ok && t[0].active(j + 1)) ok = qk(0, ks);
+            if (ok && t0.active(j + 1)) ok = qk(0, ks);
           }
-          if (ok && t[1].active(j)) ok = pv(1, vs);
+          if (ok && t1.active(j)) ok = pv(1, vs);
           if (!ok) break;
           umma_commit(&ctl->v_empty[vs]);
           ++vc;
           if (next) {
-            if (t[1].active(j + 1)) ok = qk(1, ks);
+            if (t1.active(j + 1)) ok = qk(1, ks);
             if (!ok) break;
             umma_commit(&ctl->k_empty[ks]);
             ++kc;
@@ -657,6 +715,7 @@ __global__ void __launch_bounds__(kWinThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&ctl->item_empty[gi & 1]);
     }
+    }
   }
   tc_fence_before();
   __syncthreads();
@@ -666,27 +725,23 @@ __global__ void __launch_bounds__(kWinThreads, 1)
   }
 }
 
-// Folds the records of the units that spans have cut, part by part in order: a warp per row.  grid = (units, rows / 8),
+// Folds the records of the units that spans have cut, part by part in order: a warp per row.  grid = (units, row blocks),
 // block = 256.
 template <int D>
-__global__ void __launch_bounds__(256) window_combine_kernel(const __grid_constant__ WinCall c, int ctas) {
+__global__ void __launch_bounds__(256) window_combine_kernel(const __grid_constant__ WinCall c) {
   cudaGridDependencySynchronize();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const longlong2 mine = __ldcg(&c.table[blockIdx.x]);
-  const long long total = __ldcg(&c.table[c.n_units]).x;
-  if (mine.y == 0) return;
-  const int n_spans = win_n_spans(total, ctas);
-  const int s0 = win_span_of(total, n_spans, mine.x), s1 = win_span_of(total, n_spans, mine.x + mine.y - 1);
-  if (s0 == s1) return;   // in one piece
+  const int2 spans = __ldcg(&c.table[blockIdx.x]);
+  const int s0 = spans.x, parts = spans.y;
+  if (parts <= 1) return;   // in one piece
   int b, g, window, ctx;
   const WinUnit u = find_unit(c, blockIdx.x, b, g, window, ctx);
-  const int row = blockIdx.y * 8 + warp;   // (query token of the unit, query head)
-  if (row >= u.live * c.group) return;
+  const int rows = u.live * c.group;   // (query token of the unit, query head)
+  for (int row = blockIdx.y * 8 + warp; row < rows; row += gridDim.y * 8) {
   float m = -CUDART_INF_F, l = 0.f;
   LaneVec<D> acc;
   acc.zero();
   constexpr int U = 8;
-  const int parts = s1 - s0 + 1;
   for (int p0 = 0; p0 < parts; p0 += U) {
     float2 mls[U];
     LaneVec<D> os[U];
@@ -716,6 +771,7 @@ __global__ void __launch_bounds__(256) window_combine_kernel(const __grid_consta
     *(uint2*)(dst + lane * 4) = make_uint2(win_pack2(acc.v.x, acc.v.y), win_pack2(acc.v.z, acc.v.w));
   } else {
     *(uint32_t*)(dst + lane * 2) = win_pack2(acc.v.x, acc.v.y);
+  }
   }
 }
 
@@ -750,6 +806,11 @@ cudaError_t launch_window(const WinCall& c, const void* q, int64_t q_b, int64_t 
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !opted_in[dev]) {
+    // (a block launched with fewer registers than its warpgroups share out would wait for them for ever)
+    cudaFuncAttributes fa;
+    e = cudaFuncGetAttributes(&fa, window_kernel<D>);
+    if (e != cudaSuccess) return e;
+    if (fa.numRegs < kWinLaunchRegs) return cudaErrorInvalidConfiguration;
     e = cudaFuncSetAttribute(window_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)win_smem_bytes<D>());
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) opted_in[dev] = true;
@@ -763,7 +824,7 @@ cudaError_t launch_window(const WinCall& c, const void* q, int64_t q_b, int64_t 
   e = cudaGetLastError();
   if (e != cudaSuccess || !c.spans) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(c.n_units, (c.rec_rows + 7) / 8);
+  cfg.gridDim = dim3(c.n_units, std::min(8, (c.rec_rows + 7) / 8));
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -771,7 +832,7 @@ cudaError_t launch_window(const WinCall& c, const void* q, int64_t q_b, int64_t 
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, window_combine_kernel<D>, c, ctas);
+  return cudaLaunchKernelEx(&cfg, window_combine_kernel<D>, c);
 }
 
 // Workspace: queue | table of units | (m, l) records | o records.
@@ -794,7 +855,7 @@ int win_layout(int batch, int n_q_heads, int n_kv_heads, int head_dim, int n_tok
   size_t off = 256;
   l.table = l.rec_ml = l.rec_o = off;
   if (l.units <= kWinSpanUnits) {
-    off = up(off + ((size_t)l.units + 1) * sizeof(longlong2));
+    off = up(off + (size_t)l.units * sizeof(int2));
     l.rec_ml = off;
     off = up(off + (size_t)2 * kWinMaxSpans * l.rec_rows * sizeof(float2));
     l.rec_o = off;
@@ -853,7 +914,7 @@ extern "C" int razor_window_attention(const void* q, int64_t q_stride_b, int64_t
   c.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)head_dim) : sm_scale) * 1.4426950408889634f;
   uint8_t* ws = (uint8_t*)workspace;
   c.queue = (int32_t*)ws;
-  c.table = (longlong2*)(ws + l.table);
+  c.table = (int2*)(ws + l.table);
   c.rec_ml = (float2*)(ws + l.rec_ml);
   c.rec_o = (float*)(ws + l.rec_o);
   int dev = 0, sms = 0;

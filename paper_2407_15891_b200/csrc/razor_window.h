@@ -17,6 +17,7 @@ constexpr int kWinTile = 128;          // rows of a tile of queries, tokens of a
 constexpr int kWinMaxSpans = 160;      // most CTAs that share the steps of a launch between them
 constexpr int kWinSpanUnits = 1024;    // launches of up to so many units are cut into spans, larger ones hand out whole units
 constexpr int kWinMinSpan = 4;         // steps that a span has at least
+constexpr int kWinUnitCost = 3;        // what a unit costs beside its steps (its queries' way in, its results' way out), in steps
 
 // One tile of a unit: its live tokens [tok, tok + n_tok) and the steps that it takes part in, [0, sink_end) and
 // [win_begin, win_end).
@@ -36,8 +37,15 @@ struct WinUnit {
   int32_t n_sink_steps, win_first;     // step j is key tile j below n_sink_steps, win_first + j - n_sink_steps above
   WinTileSteps tile[2];
   RAZOR_HD int key_tile(int j) const { return j < n_sink_steps ? j : win_first + (j - n_sink_steps); }
-  // what the unit counts for when the work is shared out: one with nothing to see still has its zeros to write
-  RAZOR_HD int weight() const { return live == 0 ? 0 : (n_steps > 0 ? n_steps : 1); }
+  // what the unit counts for when the work is shared out (one with nothing to see still has its zeros to write)
+  RAZOR_HD int weight() const { return live == 0 ? 0 : n_steps + kWinUnitCost; }
+  // The steps [j0, j1) that the stretch [a, z) of its weight stands for.  A cut within the unit's fixed cost moves to its
+  // start.  False: none.
+  RAZOR_HD bool part(long long a, long long z, int& j0, int& j1) const {
+    j0 = a > kWinUnitCost ? (int)(a - kWinUnitCost) : 0;
+    j1 = z > kWinUnitCost ? (int)(z - kWinUnitCost) : 0;
+    return n_steps == 0 ? a == 0 && z > 0 : j1 > j0;
+  }
 };
 
 // q_len queries at positions ctx - q_len .. ctx - 1; window < 0: a head that sees everything.  tok0: the unit's first query
@@ -94,18 +102,24 @@ RAZOR_HD inline bool win_masked(int kt, int first, int last, int window, int n_s
   return !(b <= first && (window < 0 || b < n_sink || (long long)a > (long long)last - window));
 }
 
-// Spans: the units' steps end to end, cut into n_spans pieces of equal length.
+// Spans: the units' weights end to end, cut into n_spans pieces of equal length.
 RAZOR_HD inline int win_n_spans(long long total, int ctas) {
   const long long most = total / kWinMinSpan;
   return (int)(most < 1 ? 1 : (most < ctas ? most : ctas));
 }
 RAZOR_HD inline long long win_span_begin(long long total, int n_spans, int c) { return total * c / n_spans; }
-// The span that step s lies in.
+// The span that place s lies in.
 RAZOR_HD inline int win_span_of(long long total, int n_spans, long long s) {
   int c = (int)(s * n_spans / total);
   while (c + 1 < n_spans && win_span_begin(total, n_spans, c + 1) <= s) ++c;
   while (c > 0 && win_span_begin(total, n_spans, c) > s) --c;
   return c;
+}
+
+// The spans that hold parts of a unit of weight w > 0 that begins at place s: the first and their number.
+RAZOR_HD inline void win_unit_spans(long long total, int n_spans, long long s, long long w, int& first, int& parts) {
+  first = win_span_of(total, n_spans, w > kWinUnitCost ? s + kWinUnitCost : s);
+  parts = w > kWinUnitCost ? win_span_of(total, n_spans, s + w - 1) - first + 1 : 1;
 }
 
 }  // namespace razor

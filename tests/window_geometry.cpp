@@ -71,6 +71,39 @@ int main() {
       CHECK(win_span_of(total, n, b) == c && win_span_of(total, n, e - 1) == c);
     }
   }
+  // units end to end, cut into spans: every step of every unit in one part, in order; the parts where the combining side looks
+  for (int at = 0; at < 3000; ++at) {
+    const int n = rnd(1, 12), ctas = rnd(1, 20);
+    WinUnit us[12];
+    long long begin[13] = {0};
+    for (int i = 0; i < n; ++i) {
+      us[i] = WinUnit();
+      us[i].live = rnd(0, 4) ? 5 : 0;
+      us[i].n_steps = rnd(0, 3) ? rnd(0, 40) : 0;
+      begin[i + 1] = begin[i] + us[i].weight();
+    }
+    const long long total = begin[n];
+    if (total == 0) continue;
+    const int ns = win_n_spans(total, ctas);
+    for (int i = 0; i < n; ++i) {
+      const int w = us[i].weight();
+      if (w == 0) continue;
+      int first, parts, next = 0, seen = 0;
+      win_unit_spans(total, ns, begin[i], w, first, parts);
+      for (int c = 0; c < ns; ++c) {
+        long long a = win_span_begin(total, ns, c) - begin[i], z = win_span_begin(total, ns, c + 1) - begin[i];
+        if (a < 0) a = 0;
+        if (z > w) z = w;
+        int j0 = 0, j1 = 0;
+        if (a >= z || !us[i].part(a, z, j0, j1)) continue;
+        CHECK(c == first + seen);
+        CHECK(j0 == next);
+        next = j1;
+        ++seen;
+      }
+      CHECK(seen == parts && next == us[i].n_steps);
+    }
+  }
   std::printf("ok\n");
   return 0;
 }
