@@ -24,6 +24,16 @@
  *   - Made for CUDA graphs: razor_decode_attention_tree and razor_verify_tree.  The other calls on a cache keep plans
  *     and lengths on the host, which a replay does not repeat.
  *   - Storage dtype of K, V and q is config.dtype; compensation sums/means and outputs are fp32.
+ *   - A cache of 8-bit rows (config.dtype RAZOR_I8): K, V and q are bf16 everywhere in the calls; a row that is kept is
+ *     quantised as it is written - by razor_compress, razor_compress_seq, razor_append, razor_append_many or
+ *     razor_decode_step - and held as D codes and one scale, K and V each their own: with top the row's largest magnitude,
+ *       scale = top / 127,  code = round_half_even(x * (127 / top)),  value held = scale * code   (all in fp32, IEEE),
+ *     off by at most top / 254.  A row with top < 2^-100 is held as zeros, one with a value that is not finite as NaN.
+ *     A kept token takes 2 (D + 4) bytes a KV head.  Rows that a compression drops are summed (Eq. 4) as they came, and so
+ *     are new tokens of a head without a window; a row that leaves the window counts as the values it was held with.  razor_decode_attention, _step and _multi attend to
+ *     the values held, in fp32 accuracy (a NaN in a cached K or V row, now the whole row, shows in the query rows that see it
+ *     and in no other); a round of more than 8 query rows per KV head runs block by block, each block reading the cache once.
+ *     razor_cache_export gives the values held (K and V in fp32).  The tree calls refuse such a cache (UNSUPPORTED_DIM).
  *   - The cache and attention calls never apply rotary embeddings: K and q arrive after the rotary transformation,
  *     as in the paper's cache (Section 3.2, text below Eq. 4).  razor_rope applies it.
  */
@@ -55,7 +65,7 @@ typedef enum {
   RAZOR_E_MISALIGNED = -8       /* a device pointer or stride breaks the 16-byte alignment rule */
 } razor_status;
 
-enum { RAZOR_F32 = 0, RAZOR_BF16 = 1 };
+enum { RAZOR_F32 = 0, RAZOR_BF16 = 1, RAZOR_I8 = 2 /* caches only */ };
 
 typedef struct razor_cache razor_cache_t; /* opaque host object */
 
@@ -65,7 +75,8 @@ typedef struct {
   int32_t n_q_heads;        /* Hq; must be a multiple of n_kv_heads; group = Hq/Hkv in {1,2,4,8}   */
   int32_t n_kv_heads;       /* Hkv                                                                 */
   int32_t head_dim;         /* D: 64 or 128                                                        */
-  int32_t dtype;            /* RAZOR_F32 or RAZOR_BF16: storage of K, V and q                      */
+  int32_t dtype;            /* RAZOR_F32 or RAZOR_BF16: storage of K, V and q.  RAZOR_I8: K, V and q
+                               come in as bf16, kept rows are held as 8-bit codes (see below)      */
   int32_t page_tokens;      /* tokens per page; must be 16                                         */
   int32_t n_sink;           /* N0 of Algorithm 1 (Table 2: 4); >= 0                                */
   int32_t max_ctx_len;      /* largest context length any sequence has at compression time        */
@@ -188,7 +199,7 @@ RAZOR_API int razor_decode_step(razor_cache_t* cache, int32_t layer, const void*
  *                                 attends to the kept tokens at positions <= its own (Section 3.1:
  *                                 n <= m) plus the compensation token with its count N_d (Eq. 5).
  *                                 n_tokens = 1 is razor_decode_attention.
- * Limits of the multi-token call: bf16; at least n_tokens tokens cached; every head that has dropped
+ * Limits of the multi-token call: bf16 or 8-bit rows; at least n_tokens tokens cached; every head that has dropped
  * tokens must have a window >= n_tokens (otherwise its mean would hold tokens that come after a query).
  * A round of at most 8 query rows per KV head (query heads of the group x query tokens) is one launch of
  * the streaming kernel on a tile of 2, 4 or 8 rows (matrix instructions).  A longer round runs on the
@@ -277,7 +288,7 @@ RAZOR_API int razor_verify_tree(const void* target, int64_t target_stride_b, int
 /*
  * Read back the compressed state of one (layer, sequence, KV head) in LOGICAL order (ascending
  * original position), whatever the physical slot order is.  Device outputs, any of which may be
- * NULL: kept_pos int32[n_kept]; K, V [n_kept, D] in config.dtype; comp_mean_k/v and comp_sum_k/v
+ * NULL: kept_pos int32[n_kept]; K, V [n_kept, D] in config.dtype (RAZOR_I8: the values held, fp32); comp_mean_k/v and comp_sum_k/v
  * fp32[D].  Host outputs (may be NULL): n_kept, n_drop.  n_kept is known on the host without a
  * device read, so call once with NULL device pointers to size the buffers.  Snapshot and parity probe.
  */

@@ -440,3 +440,15 @@ def window_attention(q, K, V, ctx, window, n_sink, scale):
             w = np.exp(s - s.max())
             out[t] = w @ V[see] / w.sum()
     return out
+
+
+def quantise_rows(x):
+    """Rows held in 8 bits: x [.., D] (values of bf16) -> (codes, scales, values held in fp32).  The definition is in fp32."""
+    x = np.asarray(x, dtype=np.float32)
+    with np.errstate(divide="ignore", invalid="ignore", over="ignore"):
+        top = np.abs(x).max(-1, keepdims=True)
+        fine = np.isfinite(x).all(-1, keepdims=True)
+        some = fine & (top >= np.float32(2.0 ** -100))
+        codes = np.where(some, np.rint(x * (np.float32(127) / top)), np.float32(0))
+        scale = np.where(some, top / np.float32(127), np.where(fine, np.float32(0), np.float32(np.nan)))
+    return codes.astype(np.int32), scale[..., 0].astype(np.float32), (scale * codes).astype(np.float32)

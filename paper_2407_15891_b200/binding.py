@@ -17,7 +17,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librazor.so")
 
-RAZOR_F32, RAZOR_BF16 = 0, 1
+RAZOR_F32, RAZOR_BF16, RAZOR_I8 = 0, 1, 2
 STATUS = {
     0: "RAZOR_OK", -1: "RAZOR_E_INVALID_ARG", -2: "RAZOR_E_NULL_PTR", -3: "RAZOR_E_UNSUPPORTED_DIM",
     -4: "RAZOR_E_POOL_TOO_SMALL", -5: "RAZOR_E_CAPACITY", -6: "RAZOR_E_NOT_COMPRESSED", -7: "RAZOR_E_CUDA",
@@ -160,7 +160,8 @@ def _stream(stream) -> Optional[int]:
 
 def make_config(batch, n_layers, n_q_heads, n_kv_heads, head_dim, dtype, n_sink, max_ctx_len, max_new_tokens,
                 use_compensation=1, page_shuffle_seed=0, sm_scale=0.0, page_tokens=16) -> RazorConfig:
-    dt = {torch.float32: RAZOR_F32, torch.bfloat16: RAZOR_BF16, "f32": RAZOR_F32, "bf16": RAZOR_BF16}.get(dtype, dtype)
+    dt = {torch.float32: RAZOR_F32, torch.bfloat16: RAZOR_BF16, torch.int8: RAZOR_I8, "f32": RAZOR_F32, "bf16": RAZOR_BF16,
+          "i8": RAZOR_I8}.get(dtype, dtype)
     return RazorConfig(batch, n_layers, n_q_heads, n_kv_heads, head_dim, dt, page_tokens, n_sink, max_ctx_len,
                        max_new_tokens, use_compensation, page_shuffle_seed, sm_scale)
 
@@ -538,7 +539,7 @@ class RazorCache:
             self.pool = torch.empty(self.pool_bytes, dtype=torch.uint8, device=self.device)
             self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
             self.handle = razor_cache_create(cfg, self.pool, self.pool_bytes, self.workspace, self.ws_bytes)
-        self.tdtype = torch.bfloat16 if cfg.dtype == RAZOR_BF16 else torch.float32
+        self.tdtype = torch.float32 if cfg.dtype == RAZOR_F32 else torch.bfloat16   # of K, V and q as they come in
 
     def compress(self, layer: int, K: torch.Tensor, V: torch.Tensor, ctx_len, head_is_retrieval, window) -> None:
         """K, V: [B, Hkv, N, D] device tensors (innermost dim contiguous, same strides)."""
@@ -641,7 +642,8 @@ class RazorCache:
         D = self.cfg.head_dim
         dev = self.device
         kp = torch.empty(max(n_kept, 1), dtype=torch.int32, device=dev)
-        K = torch.empty((max(n_kept, 1), D), dtype=self.tdtype, device=dev)
+        # (8-bit rows are read back as the values they stand for)
+        K = torch.empty((max(n_kept, 1), D), dtype=torch.float32 if self.cfg.dtype == RAZOR_I8 else self.tdtype, device=dev)
         V = torch.empty_like(K)
         f = [torch.empty(D, dtype=torch.float32, device=dev) for _ in range(4)]
         razor_cache_export(self.handle, layer, b, kv_head, kp, K, V, f[0], f[1], f[2], f[3])

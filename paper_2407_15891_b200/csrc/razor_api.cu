@@ -44,7 +44,7 @@ int check_config(const razor_config_t* c) {
   const int g = c->n_q_heads / c->n_kv_heads;
   if (g != 1 && g != 2 && g != 4 && g != 8) return RAZOR_E_UNSUPPORTED_DIM;
   if (c->head_dim != 64 && c->head_dim != 128) return RAZOR_E_UNSUPPORTED_DIM;
-  if (c->dtype != RAZOR_F32 && c->dtype != RAZOR_BF16) return RAZOR_E_UNSUPPORTED_DIM;
+  if (c->dtype != RAZOR_F32 && c->dtype != RAZOR_BF16 && c->dtype != RAZOR_I8) return RAZOR_E_UNSUPPORTED_DIM;
   if (c->page_tokens != kPageTokens) return RAZOR_E_UNSUPPORTED_DIM;
   if (c->n_sink < 0 || c->max_ctx_len < 0 || c->max_new_tokens < 0) return RAZOR_E_INVALID_ARG;
   if ((long long)c->max_ctx_len + c->max_new_tokens > (1LL << 30)) return RAZOR_E_INVALID_ARG;
@@ -53,8 +53,9 @@ int check_config(const razor_config_t* c) {
   return RAZOR_OK;
 }
 
-inline size_t esz(const razor_config_t& c) { return c.dtype == RAZOR_BF16 ? 2 : 4; }
-inline size_t row_bytes(const razor_config_t& c) { return (size_t)c.head_dim * esz(c); }
+inline size_t esz(const razor_config_t& c) { return c.dtype == RAZOR_F32 ? 4 : 2; }   // of K, V and q as they come in
+// of a K or V row as it is held: an 8-bit row has a scale
+inline size_t row_bytes(const razor_config_t& c) { return c.dtype == RAZOR_I8 ? (size_t)c.head_dim + 4 : (size_t)c.head_dim * esz(c); }
 inline size_t page_bytes(const razor_config_t& c) { return 2 * (size_t)kPageTokens * row_bytes(c); }
 
 Layout make_layout(const razor_config_t& c) {
@@ -766,6 +767,7 @@ int razor_append_tree(razor_cache_t* c, int32_t layer, const void* k_draft, cons
   if (!c || !k_draft || !v_draft || !n_accept) return RAZOR_E_NULL_PTR;
   int rc = layer_ready(c, layer);
   if (rc) return rc;
+  if (c->cfg.dtype == RAZOR_I8) return RAZOR_E_UNSUPPORTED_DIM;
   if (n_nodes < 1 || n_nodes > kTreeMaxNodes) return RAZOR_E_INVALID_ARG;
   if (((uintptr_t)k_draft | (uintptr_t)v_draft) & 15) return RAZOR_E_MISALIGNED;
   if ((uintptr_t)path & 3) return RAZOR_E_MISALIGNED;
@@ -805,6 +807,7 @@ int razor_decode_attention_tree(razor_cache_t* c, int32_t layer, const void* q, 
   if (!c || !q || !k_draft || !v_draft || !parent || !out) return RAZOR_E_NULL_PTR;
   int rc = layer_ready(c, layer);
   if (rc) return rc;
+  if (c->cfg.dtype == RAZOR_I8) return RAZOR_E_UNSUPPORTED_DIM;
   if (n_nodes < 1 || n_nodes > kTreeMaxNodes) return RAZOR_E_INVALID_ARG;
   if (((uintptr_t)q | (uintptr_t)k_draft | (uintptr_t)v_draft | (uintptr_t)out) & 15) return RAZOR_E_MISALIGNED;
   if ((uintptr_t)parent & 3) return RAZOR_E_MISALIGNED;
@@ -1023,7 +1026,7 @@ int razor_decode_attention_multi(razor_cache_t* c, int32_t layer, const void* q,
   if (rc) return rc;
   if (n_tokens < 1) return RAZOR_E_INVALID_ARG;
   if (n_tokens == 1) return decode_impl(c, layer, q, out, 1, 1, 0, stream);
-  if (c->cfg.dtype != RAZOR_BF16) return RAZOR_E_UNSUPPORTED_DIM;
+  if (c->cfg.dtype == RAZOR_F32) return RAZOR_E_UNSUPPORTED_DIM;
   for (const HeadState& h : c->layers[layer].hs) {
     if (h.len + h.n_drop < n_tokens) return RAZOR_E_INVALID_ARG;          // fewer tokens cached than queries
     if (h.n_drop > 0 && h.window < n_tokens) return RAZOR_E_INVALID_ARG;  // the mean would hold tokens after a query
@@ -1031,10 +1034,10 @@ int razor_decode_attention_multi(razor_cache_t* c, int32_t layer, const void* q,
   const int group0 = c->cfg.n_q_heads / c->cfg.n_kv_heads;
   // A round of more query rows per KV head than one launch of the streaming kernel takes goes to the query-tiled
   // kernel, which streams the cache once per 128 rows (tensor cores).  (An ALiBi cache with sink tokens stays on the
-  // path below.)
+  // path below, and so does one of 8-bit rows.)
   // (From 9 rows, a second launch of the streaming kernel: 32K MHA, 256 heads, 12 rows: 0.31 against 0.44 ms; 128K
   // GQA, 16 heads, 16 rows: 113 against 128 us.)
-  if ((long long)group0 * n_tokens >= c->round_tiled_min_rows && (!c->dv.alibi || c->cfg.n_sink == 0))
+  if (c->cfg.dtype == RAZOR_BF16 && (long long)group0 * n_tokens >= c->round_tiled_min_rows && (!c->dv.alibi || c->cfg.n_sink == 0))
     return round_impl(c, layer, q, out, n_tokens, stream);
   // One launch takes a tile of 2, 4 or 8 rows per KV head (query heads of the group x query tokens).  A
   // longer round runs block by block, the largest block that fits; when the round is not a multiple of
@@ -1086,8 +1089,8 @@ int razor_decode_step(razor_cache_t* c, int32_t layer, const void* k_new, const 
   LayerHost& L = c->layers[layer];
   if (L.appended_max() >= c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
   // A head with no recent window at all drops the new token at once (nothing is stored, only the sums change):
-  // that corner stays with the two separate kernels.
-  bool plain = false;
+  // that corner stays with the two separate kernels.  So does a cache of 8-bit rows: its new row has to be quantised first.
+  bool plain = c->cfg.dtype == RAZOR_I8;
   for (const HeadState& h : L.hs) plain |= (h.window == 0);
   if (plain) {
     rc = razor_append(c, layer, k_new, v_new, stream);

@@ -36,7 +36,8 @@ struct CompressSmem {
   int abort_flag;
 };
 
-template <typename T, int D>
+// Q8: the kept rows are quantised as they are packed (dropped rows are summed as they came).
+template <typename T, int D, bool Q8>
 __global__ void __launch_bounds__(kCompressThreads) compress_kernel(DeviceView dv, int layer, int n_slices) {
   using Geo = RowGeom<T, D>;
   using Smem = CompressSmem<T, D>;
@@ -146,9 +147,17 @@ __global__ void __launch_bounds__(kCompressThreads) compress_kernel(DeviceView d
           else slot = -1;
           if (slot >= 0) {
             const size_t page = (size_t)pt[slot >> 4];
-            uint4* dst = (uint4*)(dv.pool + page * dv.page_bytes + (size_t)(slot & 15) * RB) + swz(slot, lir);
-            dst[0] = kf[it];
-            dst[kPageTokens * LPR] = vf[it];   // V rows follow the 16 K rows of the page
+            if constexpr (Q8) {
+              uint8_t* at = dv.pool + page * dv.page_bytes;
+              const unsigned lanes = (unsigned)((1ull << LPR) - 1) << (par * LPR);
+              float held[EPL];
+              Q8Row<D>::store(at, slot, 0, lir, kf[it], lanes, held);
+              Q8Row<D>::store(at, slot, 1, lir, vf[it], lanes, held);
+            } else {
+              uint4* dst = (uint4*)(dv.pool + page * dv.page_bytes + (size_t)(slot & 15) * RB) + swz(slot, lir);
+              dst[0] = kf[it];
+              dst[kPageTokens * LPR] = vf[it];   // V rows follow the 16 K rows of the page
+            }
           } else {
             float a[EPL], b[EPL];
             Elem<T>::unpack(kf[it], a);
@@ -220,8 +229,9 @@ __global__ void compress_finalize_kernel(DeviceView dv, int layer, int n_slices)
 // Append: one warp per (sequence, KV head).  A head that keeps everything, or whose window is not
 // full yet, stores the new row in slot `len`.  Otherwise the oldest recent token (ring slot
 // ring_head) is folded into the fp32 compensation sums, the count grows by one, the means are
-// recomputed (Eq. 4 over every token dropped so far) and the new row takes that slot.
-template <typename T, int D>
+// recomputed (Eq. 4 over every token dropped so far) and the new row takes that slot.  (Q8: the new row is quantised; a row
+// that leaves the window counts as the values it was held with.)
+template <typename T, int D, bool Q8>
 __global__ void __launch_bounds__(64) append_kernel(DeviceView dv, int layer, const T* __restrict__ k_new,
                                                      const T* __restrict__ v_new, int early_reads) {
   using Geo = RowGeom<T, D>;
@@ -264,11 +274,12 @@ __global__ void __launch_bounds__(64) append_kernel(DeviceView dv, int layer, co
 
   const bool row_lane = active && lane < LPR;
   uint4* krow = nullptr;
+  uint8_t* at = nullptr;   // the slot's page
   float fold[2][EPL], old_sum[2][EPL];   // the row that joins the dropped set (K, V) and the sums so far
   if (row_lane) {
     if (slot >= 0) {
-      const size_t page = (size_t)dv.page_table[hs * dv.max_pages + (slot >> 4)];
-      krow = (uint4*)(dv.pool + page * dv.page_bytes + (size_t)(slot & 15) * Geo::kRowBytes) + swz(slot, lane);
+      at = dv.pool + (size_t)dv.page_table[hs * dv.max_pages + (slot >> 4)] * dv.page_bytes;
+      if constexpr (!Q8) krow = (uint4*)(at + (size_t)(slot & 15) * Geo::kRowBytes) + swz(slot, lane);
     }
     if (evict || fold_new) {
       const float* sum = dv.comp_sum + hs * 2 * D + lane * EPL;
@@ -276,8 +287,13 @@ __global__ void __launch_bounds__(64) append_kernel(DeviceView dv, int layer, co
       for (int i = 0; i < EPL; ++i) { old_sum[0][i] = sum[i]; old_sum[1][i] = sum[D + i]; }
     }
     if (evict) {
-      Elem<T>::unpack(krow[0], fold[0]);
-      Elem<T>::unpack(krow[kPageTokens * LPR], fold[1]);
+      if constexpr (Q8) {
+        Q8Row<D>::load(at, slot, 0, lane, fold[0]);
+        Q8Row<D>::load(at, slot, 1, lane, fold[1]);
+      } else {
+        Elem<T>::unpack(krow[0], fold[0]);
+        Elem<T>::unpack(krow[kPageTokens * LPR], fold[1]);
+      }
     }
   }
   if (early_reads) cudaGridDependencySynchronize();
@@ -302,8 +318,15 @@ __global__ void __launch_bounds__(64) append_kernel(DeviceView dv, int layer, co
       }
     }
     if (slot >= 0) {
-      krow[0] = kf;
-      krow[kPageTokens * LPR] = vf;
+      if constexpr (Q8) {
+        constexpr unsigned lanes = (unsigned)((1ull << LPR) - 1);
+        float held[EPL];
+        Q8Row<D>::store(at, slot, 0, lane, kf, lanes, held);
+        Q8Row<D>::store(at, slot, 1, lane, vf, lanes, held);
+      } else {
+        krow[0] = kf;
+        krow[kPageTokens * LPR] = vf;
+      }
     }
   }
   if (active && lane == 0) {
@@ -316,7 +339,7 @@ __global__ void __launch_bounds__(64) append_kernel(DeviceView dv, int layer, co
 // Append of a round of n_tok tokens per sequence (a second prompt, a verify step): one warp per
 // (sequence, KV head) applies the single-token rule n_tok times in order, so the state afterwards is
 // what n_tok razor_append calls would leave.  k_new, v_new: [B, n_tok, Hkv, D].
-template <typename T, int D>
+template <typename T, int D, bool Q8>
 __global__ void __launch_bounds__(128) append_many_kernel(DeviceView dv, int layer, const T* __restrict__ k_new,
                                                           const T* __restrict__ v_new, int n_tok) {
   using Geo = RowGeom<T, D>;
@@ -354,16 +377,27 @@ __global__ void __launch_bounds__(128) append_many_kernel(DeviceView dv, int lay
       const uint4 kf = ((const uint4*)(k_new + row))[lane];
       const uint4 vf = ((const uint4*)(v_new + row))[lane];
       uint4* krow = nullptr;
+      uint8_t* at = nullptr;
       if (slot >= 0) {
-        const size_t page = (size_t)dv.page_table[hs * dv.max_pages + (slot >> 4)];
-        krow = (uint4*)(dv.pool + page * dv.page_bytes + (size_t)(slot & 15) * Geo::kRowBytes) + swz(slot, lane);
+        at = dv.pool + (size_t)dv.page_table[hs * dv.max_pages + (slot >> 4)] * dv.page_bytes;
+        if constexpr (!Q8) krow = (uint4*)(at + (size_t)(slot & 15) * Geo::kRowBytes) + swz(slot, lane);
       }
       if (evict || fold_new) {
-        const uint4 ok = evict ? krow[0] : kf;
-        const uint4 ov = evict ? krow[kPageTokens * LPR] : vf;
         float a[EPL], c[EPL];
-        Elem<T>::unpack(ok, a);
-        Elem<T>::unpack(ov, c);
+        if constexpr (Q8) {
+          if (evict) {
+            Q8Row<D>::load(at, slot, 0, lane, a);
+            Q8Row<D>::load(at, slot, 1, lane, c);
+          } else {
+            Elem<T>::unpack(kf, a);
+            Elem<T>::unpack(vf, c);
+          }
+        } else {
+          const uint4 ok = evict ? krow[0] : kf;
+          const uint4 ov = evict ? krow[kPageTokens * LPR] : vf;
+          Elem<T>::unpack(ok, a);
+          Elem<T>::unpack(ov, c);
+        }
         const float cnt = (float)st.n_drop;
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
@@ -375,8 +409,15 @@ __global__ void __launch_bounds__(128) append_many_kernel(DeviceView dv, int lay
         }
       }
       if (slot >= 0) {
-        krow[0] = kf;
-        krow[kPageTokens * LPR] = vf;
+        if constexpr (Q8) {
+          constexpr unsigned lanes = (unsigned)((1ull << LPR) - 1);
+          float held[EPL];
+          Q8Row<D>::store(at, slot, 0, lane, kf, lanes, held);
+          Q8Row<D>::store(at, slot, 1, lane, vf, lanes, held);
+        } else {
+          krow[0] = kf;
+          krow[kPageTokens * LPR] = vf;
+        }
       }
     }
     __syncwarp();   // a later token of the round may evict a row this one just stored
@@ -400,7 +441,7 @@ __global__ void __launch_bounds__(128) append_many_kernel(DeviceView dv, int lay
 // record (ring_sum, kept by this kernel: every slice also sums the rows it stores into the window): that sum
 // is then the old rows' share of the dropped set.  A prefill handed over in chunks of at least the window
 // length therefore reads every row once and writes it once.
-template <typename T, int D>
+template <typename T, int D, bool Q8>
 __global__ void __launch_bounds__(256) append_chunk_kernel(DeviceView dv, int layer, const T* __restrict__ k_new,
                                                            const T* __restrict__ v_new, int n_tok, int n_slices) {
   using Geo = RowGeom<T, D>;
@@ -445,25 +486,47 @@ __global__ void __launch_bounds__(256) append_chunk_kernel(DeviceView dv, int la
       const bool stays = slot >= 0, had_old = fate.evicts_old;
       float a_k[EPL], a_v[EPL];
       if (stays) {
-        const size_t page = (size_t)pt[slot >> 4];
-        uint4* dst = (uint4*)(dv.pool + page * dv.page_bytes + (size_t)(slot & 15) * Geo::kRowBytes) + swz(slot, lir);
+        uint8_t* at = dv.pool + (size_t)pt[slot >> 4] * dv.page_bytes;
+        uint4* dst = (uint4*)(at + (size_t)(slot & 15) * Geo::kRowBytes) + swz(slot, lir);
         if (had_old && !skip_old) {
-          Elem<T>::unpack(dst[0], a_k);
-          Elem<T>::unpack(dst[kPageTokens * LPR], a_v);
+          if constexpr (Q8) {
+            Q8Row<D>::load(at, slot, 0, lir, a_k);
+            Q8Row<D>::load(at, slot, 1, lir, a_v);
+          } else {
+            Elem<T>::unpack(dst[0], a_k);
+            Elem<T>::unpack(dst[kPageTokens * LPR], a_v);
+          }
 #pragma unroll
           for (int i = 0; i < EPL; ++i) { accK[i] += a_k[i]; accV[i] += a_v[i]; }
         }
-        dst[0] = kf;
-        dst[kPageTokens * LPR] = vf;
+        if constexpr (Q8) {
+          const unsigned lanes = (unsigned)((1ull << LPR) - 1) << (threadIdx.x % 32 / LPR * LPR);
+          Q8Row<D>::store(at, slot, 0, lir, kf, lanes, a_k);   // (a_k, a_v: the values held)
+          Q8Row<D>::store(at, slot, 1, lir, vf, lanes, a_v);
+        } else {
+          dst[0] = kf;
+          dst[kPageTokens * LPR] = vf;
+        }
         if (st.window >= 0 && slot >= n_sink) {   // a row of the new window
-          Elem<T>::unpack(kf, a_k);
-          Elem<T>::unpack(vf, a_v);
+          if constexpr (!Q8) {
+            Elem<T>::unpack(kf, a_k);
+            Elem<T>::unpack(vf, a_v);
+          }
 #pragma unroll
           for (int i = 0; i < EPL; ++i) { ringK[i] += a_k[i]; ringV[i] += a_v[i]; }
         }
       } else {
         Elem<T>::unpack(kf, a_k);
         Elem<T>::unpack(vf, a_v);
+        if constexpr (Q8) {
+          if (st.window > 0) {   // (token by token it would have been held for a while)
+            const unsigned lanes = (unsigned)((1ull << LPR) - 1) << (threadIdx.x % 32 / LPR * LPR);
+            uint32_t w[2];
+            float scale;
+            Q8Row<D>::quantise(kf, lanes, w, scale, a_k);
+            Q8Row<D>::quantise(vf, lanes, w, scale, a_v);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < EPL; ++i) { accK[i] += a_k[i]; accV[i] += a_v[i]; }
       }
@@ -634,9 +697,10 @@ __global__ void __launch_bounds__(128) append_tree_kernel(DeviceView dv, int lay
 // Export in logical order (ascending original position).  With T = len + n_drop tokens seen so far:
 // logical index i < N0 (or any i while nothing has been dropped) is position i in slot i; otherwise
 // j = i - N0 is the j-th oldest recent token: slot N0 + (ring_head + j) mod W, position T - W + j.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) export_kernel(DeviceView dv, int layer, int head, int32_t* kept_pos, T* K,
-                                                     T* V, float* mean_k, float* mean_v, float* sum_k, float* sum_v) {
+// 8-bit rows are given as the values they stand for, in fp32.
+template <typename T, int D, bool Q8>
+__global__ void __launch_bounds__(256) export_kernel(DeviceView dv, int layer, int head, int32_t* kept_pos, void* K,
+                                                     void* V, float* mean_k, float* mean_v, float* sum_k, float* sum_v) {
   using Geo = RowGeom<T, D>;
   constexpr int LPR = Geo::kLpr, NGRP = 256 / LPR;
   const size_t hs = (size_t)layer * dv.n_heads + head;
@@ -651,11 +715,26 @@ __global__ void __launch_bounds__(256) export_kernel(DeviceView dv, int layer, i
       slot = n_sink + (st.ring_head + j) % st.window;
       pos = total - st.window + j;
     }
-    const size_t page = (size_t)dv.page_table[hs * dv.max_pages + (slot >> 4)];
-    const uint4* src =
-        (const uint4*)(dv.pool + page * dv.page_bytes + (size_t)(slot & 15) * Geo::kRowBytes) + swz(slot, lir);
-    if (K) ((uint4*)(K + (size_t)i * D))[lir] = src[0];
-    if (V) ((uint4*)(V + (size_t)i * D))[lir] = src[kPageTokens * LPR];
+    const uint8_t* at = dv.pool + (size_t)dv.page_table[hs * dv.max_pages + (slot >> 4)] * dv.page_bytes;
+    if constexpr (Q8) {
+      float f[8];
+      if (K) {
+        Q8Row<D>::load(at, slot, 0, lir, f);
+        float4* dst = (float4*)((float*)K + (size_t)i * D) + 2 * lir;
+        dst[0] = make_float4(f[0], f[1], f[2], f[3]);
+        dst[1] = make_float4(f[4], f[5], f[6], f[7]);
+      }
+      if (V) {
+        Q8Row<D>::load(at, slot, 1, lir, f);
+        float4* dst = (float4*)((float*)V + (size_t)i * D) + 2 * lir;
+        dst[0] = make_float4(f[0], f[1], f[2], f[3]);
+        dst[1] = make_float4(f[4], f[5], f[6], f[7]);
+      }
+    } else {
+      const uint4* src = (const uint4*)(at + (size_t)(slot & 15) * Geo::kRowBytes) + swz(slot, lir);
+      if (K) ((uint4*)((T*)K + (size_t)i * D))[lir] = src[0];
+      if (V) ((uint4*)((T*)V + (size_t)i * D))[lir] = src[kPageTokens * LPR];
+    }
     if (kept_pos && lir == 0) kept_pos[i] = pos;
   }
   if (blockIdx.x == 0) {
@@ -688,18 +767,18 @@ static cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, int blo
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool Q8 = false>
 static cudaError_t compress_t(const DeviceView& dv, int layer, int n_seqs, int n_slices, int n_plan, cudaStream_t s) {
   dim3 grid(n_slices, dv.n_kv_heads, n_seqs);
   const size_t smem = sizeof(CompressSmem<T, D>);
-  cudaError_t e = cudaFuncSetAttribute(compress_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t e = cudaFuncSetAttribute(compress_kernel<T, D, Q8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   if (n_plan > 0) {
     compress_plan_kernel<<<n_plan, 256, 0, s>>>(dv, layer);
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
-  compress_kernel<T, D><<<grid, kCompressThreads, smem, s>>>(dv, layer, n_slices);
+  compress_kernel<T, D, Q8><<<grid, kCompressThreads, smem, s>>>(dv, layer, n_slices);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   compress_finalize_kernel<D><<<dim3(dv.n_kv_heads, n_seqs), 2 * D, 0, s>>>(dv, layer, n_slices);
@@ -708,6 +787,10 @@ static cudaError_t compress_t(const DeviceView& dv, int layer, int n_seqs, int n
 
 cudaError_t launch_compress(const DeviceView& dv, int dtype, int layer, int n_seqs, int n_slices, int n_plan,
                             cudaStream_t s) {
+  if (dtype == RAZOR_I8) {
+    return dv.head_dim == 128 ? compress_t<__nv_bfloat16, 128, true>(dv, layer, n_seqs, n_slices, n_plan, s)
+                              : compress_t<__nv_bfloat16, 64, true>(dv, layer, n_seqs, n_slices, n_plan, s);
+  }
   if (dtype == RAZOR_BF16) {
     return dv.head_dim == 128 ? compress_t<__nv_bfloat16, 128>(dv, layer, n_seqs, n_slices, n_plan, s)
                               : compress_t<__nv_bfloat16, 64>(dv, layer, n_seqs, n_slices, n_plan, s);
@@ -716,16 +799,20 @@ cudaError_t launch_compress(const DeviceView& dv, int dtype, int layer, int n_se
                             : compress_t<float, 64>(dv, layer, n_seqs, n_slices, n_plan, s);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool Q8 = false>
 static cudaError_t append_t(const DeviceView& dv, int layer, const void* k, const void* v, int early_reads,
                             cudaStream_t s) {
   const int warps = 2;
-  return launch_dependent(append_kernel<T, D>, (dv.n_heads + warps - 1) / warps, warps * 32, s, dv, layer, (const T*)k,
+  return launch_dependent(append_kernel<T, D, Q8>, (dv.n_heads + warps - 1) / warps, warps * 32, s, dv, layer, (const T*)k,
                           (const T*)v, early_reads);
 }
 
 cudaError_t launch_append(const DeviceView& dv, int dtype, int layer, const void* k, const void* v, int early_reads,
                           cudaStream_t s) {
+  if (dtype == RAZOR_I8) {
+    return dv.head_dim == 128 ? append_t<__nv_bfloat16, 128, true>(dv, layer, k, v, early_reads, s)
+                              : append_t<__nv_bfloat16, 64, true>(dv, layer, k, v, early_reads, s);
+  }
   if (dtype == RAZOR_BF16) {
     return dv.head_dim == 128 ? append_t<__nv_bfloat16, 128>(dv, layer, k, v, early_reads, s)
                               : append_t<__nv_bfloat16, 64>(dv, layer, k, v, early_reads, s);
@@ -734,11 +821,11 @@ cudaError_t launch_append(const DeviceView& dv, int dtype, int layer, const void
                             : append_t<float, 64>(dv, layer, k, v, early_reads, s);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool Q8 = false>
 static cudaError_t append_many_t(const DeviceView& dv, int layer, const void* k, const void* v, int n_tok, int n_slices,
                                  cudaStream_t s) {
   if (n_slices > 0) {   // a long run: parallel over the tokens
-    append_chunk_kernel<T, D><<<dim3(n_slices, dv.n_heads), 256, 0, s>>>(dv, layer, (const T*)k, (const T*)v, n_tok,
+    append_chunk_kernel<T, D, Q8><<<dim3(n_slices, dv.n_heads), 256, 0, s>>>(dv, layer, (const T*)k, (const T*)v, n_tok,
                                                                          n_slices);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
@@ -746,12 +833,16 @@ static cudaError_t append_many_t(const DeviceView& dv, int layer, const void* k,
     return cudaGetLastError();
   }
   const int warps = 4;
-  return launch_dependent(append_many_kernel<T, D>, (dv.n_heads + warps - 1) / warps, warps * 32, s, dv, layer,
+  return launch_dependent(append_many_kernel<T, D, Q8>, (dv.n_heads + warps - 1) / warps, warps * 32, s, dv, layer,
                           (const T*)k, (const T*)v, n_tok);
 }
 
 cudaError_t launch_append_many(const DeviceView& dv, int dtype, int layer, const void* k, const void* v, int n_tok,
                                int n_slices, cudaStream_t s) {
+  if (dtype == RAZOR_I8) {
+    return dv.head_dim == 128 ? append_many_t<__nv_bfloat16, 128, true>(dv, layer, k, v, n_tok, n_slices, s)
+                              : append_many_t<__nv_bfloat16, 64, true>(dv, layer, k, v, n_tok, n_slices, s);
+  }
   if (dtype == RAZOR_BF16) {
     return dv.head_dim == 128 ? append_many_t<__nv_bfloat16, 128>(dv, layer, k, v, n_tok, n_slices, s)
                               : append_many_t<__nv_bfloat16, 64>(dv, layer, k, v, n_tok, n_slices, s);
@@ -785,15 +876,20 @@ cudaError_t launch_append_tree(const DeviceView& dv, int dtype, int layer, const
                             : append_tree_t<float, 64>(dv, layer, k, v, stride_b, stride_t, path, n_nodes, n_accept, batch, s);
 }
 
-template <typename T, int D>
+template <typename T, int D, bool Q8 = false>
 static cudaError_t export_t(const DeviceView& dv, int layer, int head, int32_t* kp, void* K, void* V, float* mk,
                             float* mv, float* sk, float* sv, cudaStream_t s) {
-  export_kernel<T, D><<<64, 256, 0, s>>>(dv, layer, head, kp, (T*)K, (T*)V, mk, mv, sk, sv);
+  // (8-bit rows: a snapshot of a 128K head is bound by what it writes, so enough CTAs to fill the GPU)
+  export_kernel<T, D, Q8><<<Q8 ? 592 : 64, 256, 0, s>>>(dv, layer, head, kp, K, V, mk, mv, sk, sv);
   return cudaGetLastError();
 }
 
 cudaError_t launch_export(const DeviceView& dv, int dtype, int layer, int head, int32_t* kp, void* K, void* V,
                           float* mk, float* mv, float* sk, float* sv, cudaStream_t s) {
+  if (dtype == RAZOR_I8) {
+    return dv.head_dim == 128 ? export_t<__nv_bfloat16, 128, true>(dv, layer, head, kp, K, V, mk, mv, sk, sv, s)
+                              : export_t<__nv_bfloat16, 64, true>(dv, layer, head, kp, K, V, mk, mv, sk, sv, s);
+  }
   if (dtype == RAZOR_BF16) {
     return dv.head_dim == 128 ? export_t<__nv_bfloat16, 128>(dv, layer, head, kp, K, V, mk, mv, sk, sv, s)
                               : export_t<__nv_bfloat16, 64>(dv, layer, head, kp, K, V, mk, mv, sk, sv, s);

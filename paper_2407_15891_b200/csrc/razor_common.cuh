@@ -58,6 +58,71 @@ struct RowGeom {
 // need; row-wise readers just permute their lanes.
 __device__ __forceinline__ int swz(int token, int chunk) { return chunk ^ (token & 7); }
 
+// ---- pages of 8-bit rows.  A row x is held as codes c = round(x * (127 / top)), top its largest magnitude, and one scale
+// top / 127 in fp32: the value held is scale * c (off by at most half a step, top / 254).  Quotients, product and rounding
+// are IEEE's, to nearest even, so that anybody can compute the same codes.  A page is [16 K rows of D bytes][16 V rows][16 K
+// scales][16 V scales]; a code is stored as the byte c + 128.  Chunk placement, chosen for the fragment loads of the decode
+// kernel (eight lanes read 16 bytes each at a time): two K rows at four neighbouring chunks, or four V rows at two, meet
+// no bank twice (at D = 64 V's do, once: a row is half a line).
+constexpr __host__ __device__ int q8_page_bytes(int d) { return 2 * kPageTokens * (d + 4); }
+template <int D>
+__device__ __forceinline__ int q8_chunk(int kv, int token, int chunk) {
+  if (kv == 0) return D == 128 ? chunk ^ ((token & 1) << 2) : chunk;
+  return D == 128 ? chunk ^ (token & 7) : chunk ^ ((token >> 1) & 3);
+}
+template <int D>
+struct Q8Row {   // eight elements of a row per lane, D / 8 lanes to a row
+  static constexpr int kLpr = D / 8;
+  static __device__ __forceinline__ uint8_t* codes(uint8_t* page, int slot, int kv, int lir) {
+    const int t = slot & 15;
+    return page + (kv * kPageTokens + t) * D + q8_chunk<D>(kv, t, lir >> 1) * 16 + (lir & 1) * 8;
+  }
+  static __device__ __forceinline__ float* scale(uint8_t* page, int slot, int kv) {
+    return (float*)(page + 2 * kPageTokens * D) + kv * kPageTokens + (slot & 15);
+  }
+  static __device__ __forceinline__ void load(const uint8_t* page, int slot, int kv, int lir, float (&f)[8]) {
+    const uint2 u = *(const uint2*)codes((uint8_t*)page, slot, kv, lir);
+    const float s = *scale((uint8_t*)page, slot, kv);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = s * (float)((int)(((i < 4 ? u.x : u.y) >> (8 * (i & 3))) & 0xffu) - 128);
+  }
+  // Quantises a row whose eight bf16 elements of this lane are `raw`; the kLpr lanes of the row (`lanes`) take part.  w, s:
+  // codes and scale, held: the values they stand for.  A row whose largest magnitude is below 2^-100 is held as zeros (the
+  // quotient would leave the range of fp32), one with a value that is not finite as NaN.
+  static __device__ __forceinline__ void quantise(const uint4& raw, unsigned lanes, uint32_t (&w)[2], float& s, float (&held)[8]) {
+    float f[8];
+    Elem<__nv_bfloat16>::unpack(raw, f);
+    float top = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      top = fmaxf(top, fabsf(f[i]));
+      odd |= (__float_as_uint(f[i]) & 0x7f800000u) == 0x7f800000u;
+    }
+    if (odd) top = __uint_as_float(0x7f800000u);
+#pragma unroll
+    for (int off = kLpr / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(lanes, top, off));
+    float inv = __fdiv_rn(127.f, top);
+    s = __fdiv_rn(top, 127.f);
+    if (top < 7.888609052210118e-31f) inv = s = 0.f;
+    if (top == __uint_as_float(0x7f800000u)) s = __uint_as_float(0x7fc00000u);
+    w[0] = w[1] = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int c = __float2int_rn(__fmul_rn(f[i], inv));   // (NaN gives 0)
+      w[i >> 2] |= (uint32_t)((min(max(c, -127), 127) + 128) & 0xff) << (8 * (i & 3));
+      held[i] = s * (float)c;
+    }
+  }
+  static __device__ __forceinline__ void store(uint8_t* page, int slot, int kv, int lir, const uint4& raw, unsigned lanes, float (&held)[8]) {
+    uint32_t w[2];
+    float s;
+    quantise(raw, lanes, w, s, held);
+    *(uint2*)codes(page, slot, kv, lir) = make_uint2(w[0], w[1]);
+    if (lir == 0) *scale(page, slot, kv) = s;
+  }
+};
+
 // Streaming 16-byte load: the KV cache is read once per step, keep it out of L1.
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
   uint4 v;

@@ -28,6 +28,8 @@
 
 #include <algorithm>
 
+#include <cuda_fp16.h>
+
 #include "razor_common.cuh"
 #include "razor_sync.cuh"
 
@@ -373,6 +375,163 @@ __device__ __forceinline__ void consume_page_mma(uint32_t page_addr, int valid, 
   }
 }
 
+// ------------------------------------------------------------------------------------------ 8-bit pages
+// The same two products as above over rows held as 8-bit codes and a scale (razor_common.cuh), in fp16 instructions: a code is
+// a small whole number, exact in fp16, and so is the byte c + 128 put into the mantissa of 1024 (one byte permutation for two
+// codes) less 1152.  The scales stay out of the products:
+//   S[token][head] = k_scale[token] * (codes . q'), q' = q times a power of two that puts the row's largest magnitude just
+//                    below 2^15 (exact but for values 2^-39 below it);
+//   O[d][head]    += code * (p v_scale[token] 2^14 / R) with R a power of two above every V scale seen so far by this warp,
+//                    so that the weight is below 2^14, as an fp16 head plus an fp16 remainder: off by 2^-22 of itself, or by
+//                    2^-39 R p_max.  When R grows the accumulators are scaled with it (exactly).
+// The order of the contraction indexes is free, so it is chosen for the loads: a lane (g = lane / 4, t = lane % 4) takes the
+// 16-byte chunks t (and t + 4) of the K rows g and g + 8, and D / 8 bytes at g D / 8 of the V rows 2t, 2t + 1, 2t + 8, 2t + 9:
+// rows g and g + 8 of O^T's tile mt are the dimensions g D / 8 + 2 mt and + 2 mt + 1.
+// A page is 4224 bytes at D = 128 where a bf16 page is 8448: at the copy rate an SM gets one in 181 cycles, against some 300
+// warp instructions for it.
+constexpr float kQ8WeightTop = 16384.f;   // 2^14
+__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *(const uint32_t*)&v;
+}
+// Two of the four bytes c + 128 of `w`, picked by `sel` (0x4140 the lower two, 0x4342 the upper two), as a pair of codes.
+__device__ __forceinline__ uint32_t q8_pair(uint32_t w, uint32_t sel) {
+  const uint32_t u = __byte_perm(w, 0x64646464u, sel);   // 1024 + c + 128
+  const __half2 v = __hsub2(*(const __half2*)&u, __half2half2(__ushort_as_half((unsigned short)0x6480)));   // 0x6480 = 1152
+  return *(const uint32_t*)&v;
+}
+// The power of two above x >= 0, at least 2^-100 (a NaN counts as nothing).
+__device__ __forceinline__ uint32_t q8_range_bits(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return b >= 0x7f000000u ? 0x0d800000u : max((b & 0x7f800000u) + 0x00800000u, 0x0d800000u);
+}
+
+// q: fp16 pairs of head g in the lane's order of the dimensions; f0, f1: what turns the products of heads 2t, 2t + 1 into
+// log2-domain scores (with the token's scale); range: R of the accumulators.
+template <int D>
+__device__ __forceinline__ void consume_page_q8(const uint8_t* page, int valid, int lane, float f0, float f1,
+                                                const uint32_t (&q)[D / 16][2], MmaState<D>& S, float& range, const RoundMask& mk,
+                                                float slope0, float slope1) {
+  constexpr int KC = D / 64, MT = D / 16;   // 16-byte chunks of a K row per lane; 16-row tiles of O^T
+  const int g = lane >> 2, t = lane & 3;
+  const float* scales = (const float*)(page + 2 * kPageTokens * D);
+  const float ks0 = scales[g], ks1 = scales[g + 8];
+  float vs0 = scales[kPageTokens + g], vs1 = scales[kPageTokens + g + 8];
+  uint4 k0[KC], k1[KC];
+#pragma unroll
+  for (int c = 0; c < KC; ++c) {
+    k0[c] = *(const uint4*)(page + g * D + q8_chunk<D>(0, g, t + 4 * c) * 16);
+    k1[c] = *(const uint4*)(page + (g + 8) * D + q8_chunk<D>(0, g + 8, t + 4 * c) * 16);
+  }
+  // the V words of this lane's four tokens: D / 8 bytes each
+  uint32_t vw[4][D / 32];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int tok = 2 * t + (r & 1) + (r >> 1) * 8;
+    const uint8_t* row = page + (kPageTokens + tok) * D;
+    if constexpr (D == 128) {
+      const uint4 u = *(const uint4*)(row + q8_chunk<D>(1, tok, g) * 16);
+      vw[r][0] = u.x; vw[r][1] = u.y; vw[r][2] = u.z; vw[r][3] = u.w;
+    } else {
+      const uint2 u = *(const uint2*)(row + q8_chunk<D>(1, tok, g >> 1) * 16 + (g & 1) * 8);
+      vw[r][0] = u.x; vw[r][1] = u.y;
+    }
+  }
+  // ---- S = K Q^T, two accumulation chains
+  float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < KC; ++c) {
+    const uint32_t a0[4] = {k0[c].x, k0[c].y, k0[c].z, k0[c].w}, a1[4] = {k1[c].x, k1[c].y, k1[c].z, k1[c].w};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t a[4] = {q8_pair(a0[w], 0x4140), q8_pair(a1[w], 0x4140), q8_pair(a0[w], 0x4342), q8_pair(a1[w], 0x4342)};
+      if (w & 1) mma_f16(s1, a, q[4 * c + w][0], q[4 * c + w][1]);
+      else mma_f16(s0, a, q[4 * c + w][0], q[4 * c + w][1]);
+    }
+  }
+  float s[4];
+  s[0] = (s0[0] + s1[0]) * (ks0 * f0);
+  s[1] = (s0[1] + s1[1]) * (ks0 * f1);
+  s[2] = (s0[2] + s1[2]) * (ks1 * f0);
+  s[3] = (s0[3] + s1[3]) * (ks1 * f1);
+  const bool live0 = g < valid, live1 = g + 8 < valid;   // tokens of this page beyond the head's length may hold anything
+  if (!live0) { s[0] = s[1] = -CUDART_INF_F; vs0 = 0.f; }
+  if (!live1) { s[2] = s[3] = -CUDART_INF_F; vs1 = 0.f; }
+  if (mk.n_tok > 1 || mk.alibi || mk.q_after > 0) {
+    const int t2 = t * 2, q_first = mk.total - mk.q_after - mk.n_tok;
+    const int qp0 = q_first + t2 / mk.g_real, qp1 = q_first + (t2 + 1) / mk.g_real;
+    const int p0 = mk.pos(mk.slot0 + g), p1 = mk.pos(mk.slot0 + g + 8);
+    if (mk.alibi) {
+      s[0] += slope0 * (float)(p0 - qp0);
+      s[1] += slope1 * (float)(p0 - qp1);
+      s[2] += slope0 * (float)(p1 - qp0);
+      s[3] += slope1 * (float)(p1 - qp1);
+    }
+    if (p0 > qp0 || !live0) s[0] = -CUDART_INF_F;
+    if (p0 > qp1 || !live0) s[1] = -CUDART_INF_F;
+    if (p1 > qp0 || !live1) s[2] = -CUDART_INF_F;
+    if (p1 > qp1 || !live1) s[3] = -CUDART_INF_F;
+  }
+  // ---- online softmax of heads 2t, 2t + 1 (the eight lanes with the same t share them), range of the V scales
+  float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
+#pragma unroll
+  for (int off = 4; off < 32; off <<= 1) {
+    mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
+    mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
+  }
+  const float r_page = __uint_as_float(__reduce_max_sync(0xffffffffu, max(q8_range_bits(vs0), q8_range_bits(vs1))));
+  const float r_new = fmaxf(range, r_page);
+  const float mn0 = fmaxf(S.m[0], mx0), mn1 = fmaxf(S.m[1], mx1);
+  const float mu0 = (mn0 == -CUDART_INF_F) ? 0.f : mn0, mu1 = (mn1 == -CUDART_INF_F) ? 0.f : mn1;
+  const float corr0 = fast_exp2(S.m[0] - mu0), corr1 = fast_exp2(S.m[1] - mu1);
+  float p[4] = {fast_exp2(s[0] - mu0), fast_exp2(s[1] - mu1), fast_exp2(s[2] - mu0), fast_exp2(s[3] - mu1)};
+  S.l[0] = S.l[0] * corr0 + (p[0] + p[2]);
+  S.l[1] = S.l[1] * corr1 + (p[1] + p[3]);
+  S.m[0] = mn0;
+  S.m[1] = mn1;
+  const float grow = range / r_new, up = kQ8WeightTop / r_new;   // (powers of two)
+  range = r_new;
+  const float c0 = corr0 * grow, c1 = corr1 * grow;
+  if (__any_sync(0xffffffffu, c0 != 1.f || c1 != 1.f)) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      S.o[i][0] *= c0;
+      S.o[i][1] *= c1;
+      S.o[i][2] *= c0;
+      S.o[i][3] *= c1;
+    }
+  }
+  // (a token that a row does not see has no weight there, whatever its scale)
+  const float u0 = vs0 * up, u1 = vs1 * up;
+  p[0] = s[0] == -CUDART_INF_F ? 0.f : p[0] * u0;
+  p[1] = s[1] == -CUDART_INF_F ? 0.f : p[1] * u0;
+  p[2] = s[2] == -CUDART_INF_F ? 0.f : p[2] * u1;
+  p[3] = s[3] == -CUDART_INF_F ? 0.f : p[3] * u1;
+  float h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __half2float(__float2half_rn(p[i]));
+  const uint32_t bh0 = movmatrix_trans(pack_f16(h[0], h[1])), bh1 = movmatrix_trans(pack_f16(h[2], h[3]));
+  const uint32_t bl0 = movmatrix_trans(pack_f16(p[0] - h[0], p[1] - h[1])), bl1 = movmatrix_trans(pack_f16(p[2] - h[2], p[3] - h[3]));
+  // ---- O^T += V^T P
+#pragma unroll
+  for (int w = 0; w < D / 32; ++w) {   // a word: four dimensions, two tiles
+    const uint32_t x0 = __byte_perm(vw[0][w], vw[1][w], 0x5140), x1 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
+    const uint32_t y0 = __byte_perm(vw[2][w], vw[3][w], 0x5140), y1 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
+    const uint32_t a[4] = {q8_pair(x0, 0x4140), q8_pair(x0, 0x4342), q8_pair(y0, 0x4140), q8_pair(y0, 0x4342)};
+    const uint32_t b[4] = {q8_pair(x1, 0x4140), q8_pair(x1, 0x4342), q8_pair(y1, 0x4140), q8_pair(y1, 0x4342)};
+    mma_f16(S.o[2 * w], a, bh0, bh1);
+    mma_f16(S.o[2 * w + 1], b, bh0, bh1);
+    mma_f16(S.o[2 * w], a, bl0, bl1);
+    mma_f16(S.o[2 * w + 1], b, bl0, bl1);
+  }
+}
+
 // The part of a launch-that-appends which evicts a row: sums so far (in mean[]) + the evicted row -> new sums
 // and means (Eq. 4 over every token dropped so far), stored for later launches and left in mean[] for the
 // seed below.  Same arithmetic, in the same order, as the append kernel's.  One warp, D / 32 elements per lane.
@@ -413,13 +572,18 @@ __device__ __forceinline__ void store_new_row(uint8_t* page, uint8_t* pool_page,
 }
 
 // ------------------------------------------------------------------------------------------ the kernel
-template <typename T, int D, int G, int NC, bool MMA>
+// Bytes of a page: of rows of T, or of 8-bit rows (T: the queries' type).
+template <typename T, int D, bool Q8>
+constexpr int decode_page_bytes() { return Q8 ? q8_page_bytes(D) : RowGeom<T, D>::kPageBytes; }
+
+template <typename T, int D, int G, int NC, bool MMA, bool Q8>
 __global__ void __launch_bounds__((NC + 2) * 32, 1)
 decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, float* __restrict__ out, int n_stages) {
   static_assert(!MMA || sizeof(T) == 2, "the tensor-core path is for bf16 heads");
+  static_assert(!Q8 || MMA, "8-bit rows go through matrix instructions");
   using Geo = RowGeom<T, D>;
   constexpr int LPR = Geo::kLpr, EPL = Geo::kEpl;
-  constexpr uint32_t PB = Geo::kPageBytes;
+  constexpr uint32_t PB = decode_page_bytes<T, D, Q8>();
   using Slot = ItemSlot<T, D, G>;
   using MBuf = MergeBuf<D, G, NC>;
   constexpr int kMergeBufs = merge_bufs<G>();
@@ -771,7 +935,112 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
         if (lane == 0) mbar_arrive(&bars.merge_full[mb]);
         break;
       }
-      if constexpr (MMA) {
+      if constexpr (Q8) {
+        // ---------------------------------------------------------------- 8-bit rows
+        const int g = lane >> 2, t = lane & 3;
+        // Q fragments of head g in fp16: chunk t + 4k of the row, word w of it -> pairs (4w, 4w + 1), (4w + 2, 4w + 3),
+        // scaled by a power of two
+        float x[D / 4];
+        float top = 0.f;
+#pragma unroll
+        for (int k = 0; k < D / 64; ++k) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            x[16 * k + e] = g < G ? __bfloat162float(sl.q[g < G ? g : 0][(t + 4 * k) * 16 + e]) : 0.f;
+            top = fmaxf(top, fabsf(x[16 * k + e]));
+          }
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^e > top, e clamped from below to where 2^(15 - e) is finite
+        const int e_top = max((int)(__float_as_uint(top) >> 23) - 126, -110);
+        const float to = __uint_as_float((uint32_t)(15 - e_top + 127) << 23);
+        float back = __uint_as_float((uint32_t)(e_top - 15 + 127) << 23);
+        uint32_t qa[D / 16][2];
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          qa[k][0] = pack_f16(x[4 * k] * to, x[4 * k + 1] * to);
+          qa[k][1] = pack_f16(x[4 * k + 2] * to, x[4 * k + 3] * to);
+        }
+        back *= dv.scale_log2;
+        const float f0 = __shfl_sync(0xffffffffu, back, (2 * t) * 4), f1 = __shfl_sync(0xffffffffu, back, (2 * t + 1) * 4);
+        float slope0 = 0.f, slope1 = 0.f;
+        if (dv.alibi) {
+          const float* sl_h = dv.alibi_slopes + (size_t)layer * dv.n_kv_heads * g_real + (size_t)(d.head % dv.n_kv_heads) * g_real;
+          slope0 = sl_h[(2 * t) % g_real];
+          slope1 = sl_h[(2 * t + 1) % g_real];
+        }
+        MmaState<D> S;
+        S.clear();
+        float range = __uint_as_float(0x0d800000u);   // 2^-100
+        const bool first = warp == 0;
+        if (d.seed && first) {   // compensation token (Eq. 4, Eq. 5)
+          constexpr int PER = D / 32;
+          const float log_cnt = log2f((float)d.n_drop);
+          float v_top = 0.f;
+#pragma unroll
+          for (int e = 0; e < PER; ++e) v_top = fmaxf(v_top, fabsf(sl.mean[1][lane * PER + e]));
+          // (its values in the accumulators are like codes below 128 under this range)
+          range = __uint_as_float(__reduce_max_sync(0xffffffffu, q8_range_bits(v_top * 0.0078125f)));
+          const float up = kQ8WeightTop / range;
+#pragma unroll
+          for (int j = 0; j < G; ++j) {
+            float sc = 0.f;
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+              sc += __bfloat162float(sl.q[j][lane * PER + e]) * sl.mean[0][lane * PER + e];
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) sc += __shfl_xor_sync(0xffffffffu, sc, off);
+            if (t == (j >> 1)) {
+              S.m[j & 1] = sc * dv.scale_log2 + log_cnt;
+              S.l[j & 1] = (g == 0) ? 1.f : 0.f;
+#pragma unroll
+              for (int mt = 0; mt < D / 16; ++mt) {
+                S.o[mt][j & 1] = sl.mean[1][g * (D / 8) + 2 * mt] * up;
+                S.o[mt][2 + (j & 1)] = sl.mean[1][g * (D / 8) + 2 * mt + 1] * up;
+              }
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars.item_empty[slot]);   // this warp holds all it needs from the slot
+
+        const int n_pad = (d.n_pages + NC - 1) / NC * NC;
+        for (int i = warp; i < n_pad; i += NC) {
+          unsigned stage, use;
+          ring_slot<NC>(c + i, ns, stage, use);
+          if (!warp_wait(&bars.full[stage], use & 1)) { ok = false; break; }
+          if (i < d.n_pages) {
+            const RoundMask mk{jb.n_tok, g_real, dv.alibi, d.len + d.n_drop, jb.q_after, dv.n_sink, d.ring_head, d.window,
+                               d.n_drop, (d.page_begin + i) * kPageTokens};
+            consume_page_q8<D>(ring + (size_t)stage * PB, d.len - (d.page_begin + i) * kPageTokens, lane, f0, f1, qa, S, range,
+                               mk, slope0, slope1);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars.empty[stage]);
+        }
+        if (!ok) break;
+        c += n_pad;
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) {
+          S.l[0] += __shfl_xor_sync(0xffffffffu, S.l[0], off);
+          S.l[1] += __shfl_xor_sync(0xffffffffu, S.l[1], off);
+        }
+        // Hand the state over to the reducer.
+        if (seq >= kMergeBufs && !warp_wait(&bars.merge_free[mb], ((seq / kMergeBufs) - 1) & 1)) { ok = false; break; }
+        if (first && lane == 0) M.desc = d;
+        const float down = range * (1.f / kQ8WeightTop);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int h = 2 * t + e;
+          if (h < G) {
+            if (g == 0) M.ml[warp][h] = make_float2(S.m[e], S.l[e]);
+#pragma unroll
+            for (int mt = 0; mt < D / 16; ++mt)
+              *(float2*)&M.o[warp][h][g * (D / 8) + 2 * mt] = make_float2(S.o[mt][e] * down, S.o[mt][2 + e] * down);
+          }
+        }
+      } else if constexpr (MMA) {
         // ---------------------------------------------------------------- tensor-core consumer
         const int g = lane >> 2, t = lane & 3;
         uint32_t qa[D / 16][2];   // B fragments of Q: head g
@@ -1165,13 +1434,14 @@ cudaError_t combine_launch(const DeviceView& dv, int layer, int n_multi, int n_t
 }
 
 // ------------------------------------------------------------------------------------------ launch
+constexpr int kQ8Warps = 8;           // streaming warps over 8-bit rows
 constexpr int kSmemOptIn = 232448;   // 227 KiB: the most one CTA may hold on sm_100
 
-template <typename T, int D, int G, int NC, bool MMA>
+template <typename T, int D, int G, int NC, bool MMA, bool Q8 = false>
 cudaError_t decode_launch(const DeviceView& dv, int layer, const DecodeJobs& jb, const void* q, float* out, int n_sms,
                           const DecodeTuning& tune, cudaStream_t s) {
-  auto kern = decode_kernel<T, D, G, NC, MMA>;
-  constexpr size_t PB = RowGeom<T, D>::kPageBytes;
+  auto kern = decode_kernel<T, D, G, NC, MMA, Q8>;
+  constexpr size_t PB = decode_page_bytes<T, D, Q8>();
   constexpr size_t ring_off = decode_ring_offset<T, D, G, NC>();
   static int static_smem = -1;        // per instantiation
   static bool opted_in[64] = {};
@@ -1250,6 +1520,20 @@ cudaError_t decode_g(const DeviceView& dv, int layer, const DecodeJobs& jb, cons
   return cudaErrorInvalidValue;
 }
 
+// 8-bit rows: always the matrix instructions (a page is converted once for all the rows of a tile).
+template <int D>
+cudaError_t decode_q8(const DeviceView& dv, int layer, const DecodeJobs& jb, const void* q, float* out, int n_sms,
+                      const DecodeTuning& tune, cudaStream_t s) {
+  using T = __nv_bfloat16;
+  switch (dv.group * jb.n_tok) {
+    case 1: return decode_launch<T, D, 1, kQ8Warps, true, true>(dv, layer, jb, q, out, n_sms, tune, s);
+    case 2: return decode_launch<T, D, 2, kQ8Warps, true, true>(dv, layer, jb, q, out, n_sms, tune, s);
+    case 4: return decode_launch<T, D, 4, kQ8Warps, true, true>(dv, layer, jb, q, out, n_sms, tune, s);
+    case 8: return decode_launch<T, D, 8, kQ8Warps, true, true>(dv, layer, jb, q, out, n_sms, tune, s);
+  }
+  return cudaErrorInvalidValue;
+}
+
 // One warp waits, with the decode kernel's own bounded wait, on a barrier that nothing will ever arrive
 // on.  The wait must give up after limit_ns, raise the abort flag and report through the status word:
 // a check that the safety net under every wait of the decode kernel works, without hanging anything.
@@ -1275,6 +1559,10 @@ cudaError_t launch_wait_selftest(const DeviceView& dv, unsigned long long limit_
 
 cudaError_t launch_decode(const DeviceView& dv, int dtype, int layer, const DecodeJobs& jb, const void* q, float* out,
                           int n_sms, const DecodeTuning& tune, cudaStream_t s) {
+  if (dtype == RAZOR_I8) {
+    return dv.head_dim == 128 ? decode_q8<128>(dv, layer, jb, q, out, n_sms, tune, s)
+                              : decode_q8<64>(dv, layer, jb, q, out, n_sms, tune, s);
+  }
   if (dtype == RAZOR_BF16) {
     return dv.head_dim == 128 ? decode_g<__nv_bfloat16, 128>(dv, layer, jb, q, out, n_sms, tune, s)
                               : decode_g<__nv_bfloat16, 64>(dv, layer, jb, q, out, n_sms, tune, s);
