@@ -337,15 +337,16 @@ RAZOR_API int razor_schedule_combine_heads(razor_cache_t* cache, int32_t layer, 
 enum {
   RAZOR_OPT_DECODE_TAIL_ITEMS_PER_SM = 1, /* a tail item is 1/k of an SM's share of the remaining tail
                                              (k = 1..1024; default 3)                                      */
-  RAZOR_OPT_DECODE_MIN_CHUNK_PAGES = 2, /* smallest span or tail item in pages (default 32)               */
+  RAZOR_OPT_DECODE_MIN_CHUNK_PAGES = 2, /* smallest span or tail item in pages (default 32; 8-bit rows: 64) */
   RAZOR_OPT_DECODE_RING_KB = 3,         /* shared-memory page ring per CTA in KiB; 0 = as large as fits   */
   RAZOR_OPT_DECODE_CONSUMER_WARPS = 4,  /* streaming warps per CTA: 0 = default; 4, 8, 12 or 16; a value
-                                           the head shape has no kernel for falls back to the default     */
+                                           the head shape has no kernel for (any, with 8-bit rows) falls
+                                           back to the default                                            */
   RAZOR_OPT_DECODE_TENSOR_CORES = 5,    /* bf16 heads: 0 = matrix instructions from group 4 up (default),
                                            1 = for every group size (a single head fills one row of the
                                            tile), 2 = never                                               */
   RAZOR_OPT_DECODE_STATIC_PERCENT = 6,  /* share of the pages handed out as per-CTA spans (0..100;
-                                           default 80); 0 makes every job a tail item                     */
+                                           default 80, 8-bit rows: 90); 0 makes every job a tail item     */
   RAZOR_OPT_DECODE_EARLY_PREFETCH = 7,  /* most pages (0..64; default 12) a CTA copies from the start of its span
                                            into shared memory before the kernel waits for the launch before it
                                            on the stream - only pages that no kernel still in flight can be

@@ -391,7 +391,7 @@ __device__ __forceinline__ void consume_page_mma(uint32_t page_addr, int valid, 
 // warp instructions for it.
 constexpr float kQ8WeightTop = 16384.f;   // 2^14
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -412,123 +412,151 @@ __device__ __forceinline__ uint32_t q8_range_bits(float x) {
   return b >= 0x7f000000u ? 0x0d800000u : max((b & 0x7f800000u) + 0x00800000u, 0x0d800000u);
 }
 
+// Two pages at a time: the loads and products of one hide behind the other's, and the row maxima, the corrections and the
+// joining of the accumulators are paid once for 32 tokens (one page at a time, 480 instructions a page: the 64K MHA layer 164
+// to 187 us).  pages, valid: the pages and the tokens in them (0 or less: nothing of the page counts, it may hold anything);
+// slot: slot of their first tokens.
 // q: fp16 pairs of head g in the lane's order of the dimensions; f0, f1: what turns the products of heads 2t, 2t + 1 into
 // log2-domain scores (with the token's scale); range: R of the accumulators.
 template <int D>
-__device__ __forceinline__ void consume_page_q8(const uint8_t* page, int valid, int lane, float f0, float f1,
-                                                const uint32_t (&q)[D / 16][2], MmaState<D>& S, float& range, const RoundMask& mk,
-                                                float slope0, float slope1) {
+__device__ __forceinline__ void consume_pages_q8(const uint8_t* const (&pages)[2], const int (&valid)[2], const int (&slot)[2],
+                                                 int lane, float f0, float f1, const uint32_t (&q)[D / 16][2], MmaState<D>& S,
+                                                 float& range, const RoundMask& mk, float slope0, float slope1) {
   constexpr int KC = D / 64, MT = D / 16;   // 16-byte chunks of a K row per lane; 16-row tiles of O^T
+  (void)MT;
   const int g = lane >> 2, t = lane & 3;
-  const float* scales = (const float*)(page + 2 * kPageTokens * D);
-  const float ks0 = scales[g], ks1 = scales[g + 8];
-  float vs0 = scales[kPageTokens + g], vs1 = scales[kPageTokens + g + 8];
-  uint4 k0[KC], k1[KC];
+  float s[2][4], vs[2][2];
 #pragma unroll
-  for (int c = 0; c < KC; ++c) {
-    k0[c] = *(const uint4*)(page + g * D + q8_chunk<D>(0, g, t + 4 * c) * 16);
-    k1[c] = *(const uint4*)(page + (g + 8) * D + q8_chunk<D>(0, g + 8, t + 4 * c) * 16);
-  }
-  // the V words of this lane's four tokens: D / 8 bytes each
-  uint32_t vw[4][D / 32];
+  for (int u = 0; u < 2; ++u) {
+    const uint8_t* page = pages[u];
+    const float* scales = (const float*)(page + 2 * kPageTokens * D);
+    const float ks0 = scales[g], ks1 = scales[g + 8];
+    vs[u][0] = scales[kPageTokens + g];
+    vs[u][1] = scales[kPageTokens + g + 8];
+    // ---- S = K Q^T, two accumulation chains
+    float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int tok = 2 * t + (r & 1) + (r >> 1) * 8;
-    const uint8_t* row = page + (kPageTokens + tok) * D;
-    if constexpr (D == 128) {
-      const uint4 u = *(const uint4*)(row + q8_chunk<D>(1, tok, g) * 16);
-      vw[r][0] = u.x; vw[r][1] = u.y; vw[r][2] = u.z; vw[r][3] = u.w;
-    } else {
-      const uint2 u = *(const uint2*)(row + q8_chunk<D>(1, tok, g >> 1) * 16 + (g & 1) * 8);
-      vw[r][0] = u.x; vw[r][1] = u.y;
+    for (int c = 0; c < KC; ++c) {
+      const uint4 k0 = *(const uint4*)(page + g * D + q8_chunk<D>(0, g, t + 4 * c) * 16);
+      const uint4 k1 = *(const uint4*)(page + (g + 8) * D + q8_chunk<D>(0, g + 8, t + 4 * c) * 16);
+      const uint32_t a0[4] = {k0.x, k0.y, k0.z, k0.w}, a1[4] = {k1.x, k1.y, k1.z, k1.w};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t a[4] = {q8_pair(a0[w], 0x4140), q8_pair(a1[w], 0x4140), q8_pair(a0[w], 0x4342), q8_pair(a1[w], 0x4342)};
+        if (w & 1) mma_f16(s1, a, q[4 * c + w][0], q[4 * c + w][1]);
+        else mma_f16(s0, a, q[4 * c + w][0], q[4 * c + w][1]);
+      }
     }
-  }
-  // ---- S = K Q^T, two accumulation chains
-  float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int c = 0; c < KC; ++c) {
-    const uint32_t a0[4] = {k0[c].x, k0[c].y, k0[c].z, k0[c].w}, a1[4] = {k1[c].x, k1[c].y, k1[c].z, k1[c].w};
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const uint32_t a[4] = {q8_pair(a0[w], 0x4140), q8_pair(a1[w], 0x4140), q8_pair(a0[w], 0x4342), q8_pair(a1[w], 0x4342)};
-      if (w & 1) mma_f16(s1, a, q[4 * c + w][0], q[4 * c + w][1]);
-      else mma_f16(s0, a, q[4 * c + w][0], q[4 * c + w][1]);
+    s[u][0] = (s0[0] + s1[0]) * (ks0 * f0);
+    s[u][1] = (s0[1] + s1[1]) * (ks0 * f1);
+    s[u][2] = (s0[2] + s1[2]) * (ks1 * f0);
+    s[u][3] = (s0[3] + s1[3]) * (ks1 * f1);
+    if (mk.n_tok > 1 || mk.alibi || mk.q_after > 0) {
+      const int t2 = t * 2, q_first = mk.total - mk.q_after - mk.n_tok;
+      const int qp0 = q_first + t2 / mk.g_real, qp1 = q_first + (t2 + 1) / mk.g_real;
+      const int p0 = mk.pos(slot[u] + g), p1 = mk.pos(slot[u] + g + 8);
+      if (mk.alibi) {            // Eq. 1: - l_h (m - n)
+        s[u][0] += slope0 * (float)(p0 - qp0);
+        s[u][1] += slope1 * (float)(p0 - qp1);
+        s[u][2] += slope0 * (float)(p1 - qp0);
+        s[u][3] += slope1 * (float)(p1 - qp1);
+      }
+      // causality inside the round: a query does not see the tokens after it
+      if (p0 > qp0) s[u][0] = -CUDART_INF_F;
+      if (p0 > qp1) s[u][1] = -CUDART_INF_F;
+      if (p1 > qp0) s[u][2] = -CUDART_INF_F;
+      if (p1 > qp1) s[u][3] = -CUDART_INF_F;
     }
-  }
-  float s[4];
-  s[0] = (s0[0] + s1[0]) * (ks0 * f0);
-  s[1] = (s0[1] + s1[1]) * (ks0 * f1);
-  s[2] = (s0[2] + s1[2]) * (ks1 * f0);
-  s[3] = (s0[3] + s1[3]) * (ks1 * f1);
-  const bool live0 = g < valid, live1 = g + 8 < valid;   // tokens of this page beyond the head's length may hold anything
-  if (!live0) { s[0] = s[1] = -CUDART_INF_F; vs0 = 0.f; }
-  if (!live1) { s[2] = s[3] = -CUDART_INF_F; vs1 = 0.f; }
-  if (mk.n_tok > 1 || mk.alibi || mk.q_after > 0) {
-    const int t2 = t * 2, q_first = mk.total - mk.q_after - mk.n_tok;
-    const int qp0 = q_first + t2 / mk.g_real, qp1 = q_first + (t2 + 1) / mk.g_real;
-    const int p0 = mk.pos(mk.slot0 + g), p1 = mk.pos(mk.slot0 + g + 8);
-    if (mk.alibi) {
-      s[0] += slope0 * (float)(p0 - qp0);
-      s[1] += slope1 * (float)(p0 - qp1);
-      s[2] += slope0 * (float)(p1 - qp0);
-      s[3] += slope1 * (float)(p1 - qp1);
+    if (g >= valid[u]) {       // tokens beyond the head's length
+      s[u][0] = s[u][1] = -CUDART_INF_F;
+      vs[u][0] = 0.f;
     }
-    if (p0 > qp0 || !live0) s[0] = -CUDART_INF_F;
-    if (p0 > qp1 || !live0) s[1] = -CUDART_INF_F;
-    if (p1 > qp0 || !live1) s[2] = -CUDART_INF_F;
-    if (p1 > qp1 || !live1) s[3] = -CUDART_INF_F;
+    if (g + 8 >= valid[u]) {
+      s[u][2] = s[u][3] = -CUDART_INF_F;
+      vs[u][1] = 0.f;
+    }
   }
   // ---- online softmax of heads 2t, 2t + 1 (the eight lanes with the same t share them), range of the V scales
-  float mx0 = fmaxf(s[0], s[2]), mx1 = fmaxf(s[1], s[3]);
+  float mx0 = fmaxf(fmaxf(s[0][0], s[0][2]), fmaxf(s[1][0], s[1][2])), mx1 = fmaxf(fmaxf(s[0][1], s[0][3]), fmaxf(s[1][1], s[1][3]));
+  const uint32_t r_lane = max(max(q8_range_bits(vs[0][0]), q8_range_bits(vs[0][1])), max(q8_range_bits(vs[1][0]), q8_range_bits(vs[1][1])));
+  const float r_new = fmaxf(range, __uint_as_float(__reduce_max_sync(0xffffffffu, r_lane)));
 #pragma unroll
   for (int off = 4; off < 32; off <<= 1) {
     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
     mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
   }
-  const float r_page = __uint_as_float(__reduce_max_sync(0xffffffffu, max(q8_range_bits(vs0), q8_range_bits(vs1))));
-  const float r_new = fmaxf(range, r_page);
   const float mn0 = fmaxf(S.m[0], mx0), mn1 = fmaxf(S.m[1], mx1);
   const float mu0 = (mn0 == -CUDART_INF_F) ? 0.f : mn0, mu1 = (mn1 == -CUDART_INF_F) ? 0.f : mn1;
   const float corr0 = fast_exp2(S.m[0] - mu0), corr1 = fast_exp2(S.m[1] - mu1);
-  float p[4] = {fast_exp2(s[0] - mu0), fast_exp2(s[1] - mu1), fast_exp2(s[2] - mu0), fast_exp2(s[3] - mu1)};
-  S.l[0] = S.l[0] * corr0 + (p[0] + p[2]);
-  S.l[1] = S.l[1] * corr1 + (p[1] + p[3]);
-  S.m[0] = mn0;
-  S.m[1] = mn1;
   const float grow = range / r_new, up = kQ8WeightTop / r_new;   // (powers of two)
   range = r_new;
+  S.m[0] = mn0;
+  S.m[1] = mn1;
+  S.l[0] *= corr0;
+  S.l[1] *= corr1;
   const float c0 = corr0 * grow, c1 = corr1 * grow;
-  if (__any_sync(0xffffffffu, c0 != 1.f || c1 != 1.f)) {
+  uint32_t bh[2][2], bl[2][2];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      S.o[i][0] *= c0;
-      S.o[i][1] *= c1;
-      S.o[i][2] *= c0;
-      S.o[i][3] *= c1;
+  for (int u = 0; u < 2; ++u) {
+    float p[4] = {fast_exp2(s[u][0] - mu0), fast_exp2(s[u][1] - mu1), fast_exp2(s[u][2] - mu0), fast_exp2(s[u][3] - mu1)};
+    S.l[0] += p[0] + p[2];
+    S.l[1] += p[1] + p[3];
+    // (a token that a row does not see has no weight there, whatever its scale)
+    const float u0 = vs[u][0] * up, u1 = vs[u][1] * up;
+    p[0] = s[u][0] == -CUDART_INF_F ? 0.f : p[0] * u0;
+    p[1] = s[u][1] == -CUDART_INF_F ? 0.f : p[1] * u0;
+    p[2] = s[u][2] == -CUDART_INF_F ? 0.f : p[2] * u1;
+    p[3] = s[u][3] == -CUDART_INF_F ? 0.f : p[3] * u1;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t hi = pack_f16(p[2 * h], p[2 * h + 1]);
+      const float2 back = __half22float2(*(const __half2*)&hi);
+      bh[u][h] = movmatrix_trans(hi);
+      bl[u][h] = movmatrix_trans(pack_f16(p[2 * h] - back.x, p[2 * h + 1] - back.y));
     }
   }
-  // (a token that a row does not see has no weight there, whatever its scale)
-  const float u0 = vs0 * up, u1 = vs1 * up;
-  p[0] = s[0] == -CUDART_INF_F ? 0.f : p[0] * u0;
-  p[1] = s[1] == -CUDART_INF_F ? 0.f : p[1] * u0;
-  p[2] = s[2] == -CUDART_INF_F ? 0.f : p[2] * u1;
-  p[3] = s[3] == -CUDART_INF_F ? 0.f : p[3] * u1;
-  float h[4];
+  // ---- O^T += V^T P.  The pages' products are added up by themselves and joined in rounded fp32: the instruction's own
+  // additions cut off, and over the pages of a long head that adds up (3e-6 of the result at 64K tokens).
+  uint32_t vw[2][4][D / 32];   // the words of this lane's four tokens, D / 8 bytes each
 #pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = __half2float(__float2half_rn(p[i]));
-  const uint32_t bh0 = movmatrix_trans(pack_f16(h[0], h[1])), bh1 = movmatrix_trans(pack_f16(h[2], h[3]));
-  const uint32_t bl0 = movmatrix_trans(pack_f16(p[0] - h[0], p[1] - h[1])), bl1 = movmatrix_trans(pack_f16(p[2] - h[2], p[3] - h[3]));
-  // ---- O^T += V^T P
+  for (int u = 0; u < 2; ++u)
 #pragma unroll
-  for (int w = 0; w < D / 32; ++w) {   // a word: four dimensions, two tiles
-    const uint32_t x0 = __byte_perm(vw[0][w], vw[1][w], 0x5140), x1 = __byte_perm(vw[0][w], vw[1][w], 0x7362);
-    const uint32_t y0 = __byte_perm(vw[2][w], vw[3][w], 0x5140), y1 = __byte_perm(vw[2][w], vw[3][w], 0x7362);
-    const uint32_t a[4] = {q8_pair(x0, 0x4140), q8_pair(x0, 0x4342), q8_pair(y0, 0x4140), q8_pair(y0, 0x4342)};
-    const uint32_t b[4] = {q8_pair(x1, 0x4140), q8_pair(x1, 0x4342), q8_pair(y1, 0x4140), q8_pair(y1, 0x4342)};
-    mma_f16(S.o[2 * w], a, bh0, bh1);
-    mma_f16(S.o[2 * w + 1], b, bh0, bh1);
-    mma_f16(S.o[2 * w], a, bl0, bl1);
-    mma_f16(S.o[2 * w + 1], b, bl0, bl1);
+    for (int r = 0; r < 4; ++r) {
+      const int tok = 2 * t + (r & 1) + (r >> 1) * 8;
+      const uint8_t* row = pages[u] + (kPageTokens + tok) * D;
+      if constexpr (D == 128) {
+        const uint4 x = *(const uint4*)(row + q8_chunk<D>(1, tok, g) * 16);
+        vw[u][r][0] = x.x; vw[u][r][1] = x.y; vw[u][r][2] = x.z; vw[u][r][3] = x.w;
+      } else {
+        const uint2 x = *(const uint2*)(row + q8_chunk<D>(1, tok, g >> 1) * 16 + (g & 1) * 8);
+        vw[u][r][0] = x.x; vw[u][r][1] = x.y;
+      }
+    }
+#pragma unroll
+  for (int w0 = 0; w0 < D / 32; w0 += 2) {   // two words, of four dimensions (two tiles) each: four chains of products
+    float d[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i][0] = d[i][1] = d[i][2] = d[i][3] = 0.f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      uint32_t a[4][4];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int w = w0 + x;
+        const uint32_t x0 = __byte_perm(vw[u][0][w], vw[u][1][w], 0x5140), x1 = __byte_perm(vw[u][0][w], vw[u][1][w], 0x7362);
+        const uint32_t y0 = __byte_perm(vw[u][2][w], vw[u][3][w], 0x5140), y1 = __byte_perm(vw[u][2][w], vw[u][3][w], 0x7362);
+        a[2 * x][0] = q8_pair(x0, 0x4140); a[2 * x][1] = q8_pair(x0, 0x4342); a[2 * x][2] = q8_pair(y0, 0x4140); a[2 * x][3] = q8_pair(y0, 0x4342);
+        a[2 * x + 1][0] = q8_pair(x1, 0x4140); a[2 * x + 1][1] = q8_pair(x1, 0x4342); a[2 * x + 1][2] = q8_pair(y1, 0x4140); a[2 * x + 1][3] = q8_pair(y1, 0x4342);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma_f16(d[i], a[i], bh[u][0], bh[u][1]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma_f16(d[i], a[i], bl[u][0], bl[u][1]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S.o[2 * w0 + i][e] = fmaf(S.o[2 * w0 + i][e], e & 1 ? c1 : c0, d[i][e]);
   }
 }
 
@@ -572,9 +600,13 @@ __device__ __forceinline__ void store_new_row(uint8_t* page, uint8_t* pool_page,
 }
 
 // ------------------------------------------------------------------------------------------ the kernel
-// Bytes of a page: of rows of T, or of 8-bit rows (T: the queries' type).
+// Bytes of a page: of rows of T, or of 8-bit rows (T: the queries' type); pages to a ring stage.  8-bit pages are small and the
+// producer's way round per stage takes some 100 ns, which was what bound them one page to a stage (2.1 KB or 4.2 KB: 72 us for
+// 228 MB, 171 us for 886): a stage holds 8.4 or 8.7 KB of them, in one copy where the pages lie side by side in the pool.
 template <typename T, int D, bool Q8>
 constexpr int decode_page_bytes() { return Q8 ? q8_page_bytes(D) : RowGeom<T, D>::kPageBytes; }
+template <int D, bool Q8>
+constexpr int decode_stage_pages() { return Q8 ? (D == 128 ? 2 : 4) : 1; }
 
 template <typename T, int D, int G, int NC, bool MMA, bool Q8>
 __global__ void __launch_bounds__((NC + 2) * 32, 1)
@@ -584,6 +616,8 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
   using Geo = RowGeom<T, D>;
   constexpr int LPR = Geo::kLpr, EPL = Geo::kEpl;
   constexpr uint32_t PB = decode_page_bytes<T, D, Q8>();
+  constexpr int PPS = decode_stage_pages<D, Q8>();
+  constexpr uint32_t SB = PPS * PB;   // bytes of a stage
   using Slot = ItemSlot<T, D, G>;
   using MBuf = MergeBuf<D, G, NC>;
   constexpr int kMergeBufs = merge_bufs<G>();
@@ -622,8 +656,34 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
   const int n_items = jb.n_items;
   const WorkItem no_item = {0, 0, 0, 0, 1, 0, 0, 0};   // (merge_here = 0)
   auto row_of = [&](const WorkItem& w) { return (size_t)layer * dv.n_heads + w.head; };
+  // The pages of a stage-full of an item, `unit` counted from the item's first page on; pt: the item's part of the page table,
+  // last: the highest index into it.
+  struct Pids {
+    int32_t id[PPS];
+  };
+  auto unit_pids = [](const int32_t* pt, int unit, int last) {
+    Pids r;
+#pragma unroll
+    for (int k = 0; k < PPS; ++k) r.id[k] = pt[min(unit * PPS + k, last)];
+    return r;
+  };
   auto first_pids = [&](const WorkItem& w) {
-    return dv.page_table[row_of(w) * dv.max_pages + min(w.page_begin + lane, dv.max_pages - 1)];
+    return unit_pids(dv.page_table + row_of(w) * dv.max_pages + w.page_begin, lane, dv.max_pages - 1 - w.page_begin);
+  };
+  // Copies n pages into a stage.
+  auto fill_stage = [&](unsigned stage, const Pids& pids, int n) {
+    mbar_arrive_expect_tx(&bars.full[stage], (uint32_t)n * PB);
+    uint8_t* dst = ring + (size_t)stage * SB;
+    bool run = n == PPS;
+#pragma unroll
+    for (int k = 1; k < PPS; ++k) run &= pids.id[k] == pids.id[0] + k;
+    if (run) {
+      bulk_load(dst, dv.pool + (size_t)pids.id[0] * dv.page_bytes, SB, &bars.full[stage]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < PPS; ++k)
+        if (k < n) bulk_load(dst + k * PB, dv.pool + (size_t)pids.id[k] * dv.page_bytes, PB, &bars.full[stage]);
+    }
   };
   // A job is a run of consecutive items: a span (looked up in jobs[]) or a single tail item (tail
   // jobs follow the spans and map to consecutive items, so they need no lookup).
@@ -645,7 +705,7 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
   // state of the first item too, when the host says that nothing in flight writes this layer's states.
   int it0 = n_items, job_end0 = n_items;
   WorkItem w0 = no_item;
-  int32_t pid0 = 0;
+  Pids pid0 = {};
   HeadState st0 = {0, 0, 0, 0};
   const bool has_span = (int)blockIdx.x < jb.n_spans;
   const bool state_early = has_span && jb.state_stable != 0;   // the head states of this layer are at rest
@@ -663,16 +723,15 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
   // append leaves it, follows after the dependency wait; the consumers then find these pages already landed.
   unsigned early_done = 0;
   if (warp == NC && has_span && blockIdx.x < kEarlyCtas) {
-    const int n_early = min((int)jb.early[blockIdx.x], n_stages);   // the host has applied its own cap already
+    const int n_early = min((int)jb.early[blockIdx.x] / PPS, n_stages);   // stage-fulls; the host has applied its own cap already
     const int32_t* pt0 = dv.page_table + row_of(w0) * dv.max_pages + w0.page_begin;
     for (int p = lane; p < n_early; p += 32) {
       unsigned stage, use;
       ring_slot<NC>((unsigned)p, (unsigned)n_stages, stage, use);
-      mbar_arrive_expect_tx(&bars.full[stage], PB);
-      bulk_load(ring + (size_t)stage * PB, dv.pool + (size_t)pt0[p] * dv.page_bytes, PB, &bars.full[stage]);
+      fill_stage(stage, unit_pids(pt0, p, dv.max_pages - 1 - w0.page_begin), PPS);
     }
     early_done = (unsigned)n_early;
-    if (n_early > 0) pid0 = pt0[min(n_early + lane, dv.max_pages - 1 - w0.page_begin)];   // ids of the round that follows
+    if (n_early > 0) pid0 = unit_pids(pt0, n_early + lane, dv.max_pages - 1 - w0.page_begin);   // ids of the round that follows
   }
   // This kernel is launched as a programmatic dependent of whatever precedes it on the stream (the
   // append or an earlier combine), so everything above overlaps that kernel's tail; nothing a kernel
@@ -709,7 +768,7 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
     // left to drain over a chain of dependent global loads at every item boundary.
     int it = it0, job_end = job_end0;
     WorkItem w = w0;
-    int32_t pid_first = pid0;
+    Pids pid_first = pid0;
     if (!has_span) {   // more CTAs than spans: start on the tail
       int j = 0;
       if (lane == 0) j = atomicAdd(dv.queue, 1);
@@ -765,8 +824,9 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
       const int n = max(0, page_end - w.page_begin);
       const int tp_rel = tp_slot >= 0 ? (tp_slot >> 4) - w.page_begin : -1;
       const bool owns = tp_rel >= 0 && tp_rel < n;   // this part holds the page the new row goes to
-      const int p_first = seq == 0 ? (int)early_done : 0;   // pages of this item already on their way
-      if (p_first > n) {   // the host's count and the device's lengths disagree: stop rather than mix items up
+      const int n_units = (n + PPS - 1) / PPS;              // stage-fulls
+      const int p_first = seq == 0 ? (int)early_done : 0;   // those of this item already on their way
+      if (p_first * PPS > n) {   // the host's count and the device's lengths disagree: stop rather than mix items up
         if (lane == 0) {
           atomicOr(dv.status, kStatusEarlyMismatch);
           if (q_issued) mbar_arrive(&bars.item_full[slot]);   // lets the exit path wait for the query copy in flight
@@ -810,19 +870,20 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
       }
       seq_issued = seq + 1;
       const int32_t* pt = dv.page_table + hs * dv.max_pages + w.page_begin;
-      // Page i of an item always goes to consumer warp i % NC (so a part's result does not depend on
+      // Page i (stage-full i) of an item always goes to consumer warp i % NC (so a part's result does not depend on
       // which CTA streamed it or on what that CTA streamed before): the item starts on a ring position
       // that is a multiple of NC, and the positions left over in its last round are passed on empty.
-      const int n_pad = (n + NC - 1) / NC * NC;
+      const int n_pad = (n_units + NC - 1) / NC * NC;
       int it_next = it + 1, end_next = job_end;   // the next item of this job, unless the job ends here
       WorkItem w_next = no_item;
       bool have_next = false;
-      int32_t pid_cur = pid_first;
+      Pids pid_cur = pid_first;
       for (int p0 = p_first; p0 < n_pad; p0 += batch) {
         const int in_batch = min(batch, n_pad - p0);
         const bool mine = lane < in_batch;
-        const bool real = mine && p0 + lane < n;
-        const int32_t pid_after = (p0 + batch + lane < n) ? pt[p0 + batch + lane] : 0;   // ids of the next round
+        const bool real = mine && p0 + lane < n_units;
+        Pids pid_after = {};   // ids of the next round
+        if (p0 + batch + lane < n_units) pid_after = unit_pids(pt, p0 + batch + lane, n - 1);
         unsigned stage = 0, use_cur = 0;
         bool ready = true;
         if (mine) {
@@ -832,8 +893,7 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
           if (use_cur > 0) ready = mbar_wait(&bars.empty[stage], (use_cur - 1) & 1, abort_flag);
           if (ready) {
             if (real) {
-              mbar_arrive_expect_tx(&bars.full[stage], PB);
-              bulk_load(ring + (size_t)stage * PB, dv.pool + (size_t)pid_cur * dv.page_bytes, PB, &bars.full[stage]);
+              fill_stage(stage, pid_cur, min(PPS, n - (p0 + lane) * PPS));
             } else {
               mbar_arrive(&bars.full[stage]);
             }
@@ -1005,16 +1065,24 @@ decode_kernel(DeviceView dv, int layer, DecodeJobs jb, const T* __restrict__ q, 
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars.item_empty[slot]);   // this warp holds all it needs from the slot
 
-        const int n_pad = (d.n_pages + NC - 1) / NC * NC;
+        const int n_units = (d.n_pages + PPS - 1) / PPS, n_pad = (n_units + NC - 1) / NC * NC;
+        const RoundMask mk{jb.n_tok, g_real, dv.alibi, d.len + d.n_drop, jb.q_after, dv.n_sink, d.ring_head, d.window, d.n_drop, 0};
         for (int i = warp; i < n_pad; i += NC) {
           unsigned stage, use;
           ring_slot<NC>(c + i, ns, stage, use);
           if (!warp_wait(&bars.full[stage], use & 1)) { ok = false; break; }
-          if (i < d.n_pages) {
-            const RoundMask mk{jb.n_tok, g_real, dv.alibi, d.len + d.n_drop, jb.q_after, dv.n_sink, d.ring_head, d.window,
-                               d.n_drop, (d.page_begin + i) * kPageTokens};
-            consume_page_q8<D>(ring + (size_t)stage * PB, d.len - (d.page_begin + i) * kPageTokens, lane, f0, f1, qa, S, range,
-                               mk, slope0, slope1);
+          if (i < n_units) {
+#pragma unroll
+            for (int k = 0; k < PPS; k += 2) {
+              // (the page a last stage-full does not have: the one before it stands in, and nothing of it counts)
+              const int at = i * PPS + k, n_here = d.n_pages - at;
+              if (n_here <= 0) break;
+              const uint8_t* first = ring + (size_t)stage * SB + k * PB;
+              const uint8_t* const pages[2] = {first, n_here > 1 ? first + PB : first};
+              const int slots_at[2] = {(d.page_begin + at) * kPageTokens, (d.page_begin + at + 1) * kPageTokens};
+              const int valid[2] = {d.len - slots_at[0], n_here > 1 ? d.len - slots_at[1] : 0};
+              consume_pages_q8<D>(pages, valid, slots_at, lane, f0, f1, qa, S, range, mk, slope0, slope1);
+            }
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars.empty[stage]);
@@ -1441,7 +1509,7 @@ template <typename T, int D, int G, int NC, bool MMA, bool Q8 = false>
 cudaError_t decode_launch(const DeviceView& dv, int layer, const DecodeJobs& jb, const void* q, float* out, int n_sms,
                           const DecodeTuning& tune, cudaStream_t s) {
   auto kern = decode_kernel<T, D, G, NC, MMA, Q8>;
-  constexpr size_t PB = decode_page_bytes<T, D, Q8>();
+  constexpr size_t SB = (size_t)decode_stage_pages<D, Q8>() * decode_page_bytes<T, D, Q8>();
   constexpr size_t ring_off = decode_ring_offset<T, D, G, NC>();
   static int static_smem = -1;        // per instantiation
   static bool opted_in[64] = {};
@@ -1452,11 +1520,12 @@ cudaError_t decode_launch(const DeviceView& dv, int layer, const DecodeJobs& jb,
     static_smem = (int)fa.sharedSizeBytes;
   }
   const long long avail = (long long)kSmemOptIn - static_smem - (long long)ring_off;
-  long long stages = avail / (long long)PB;
-  if (tune.ring_kb > 0) stages = std::min<long long>(stages, (long long)tune.ring_kb * 1024 / (long long)PB);
+  long long stages = avail / (long long)SB;
+  if (tune.ring_kb > 0) stages = std::min<long long>(stages, (long long)tune.ring_kb * 1024 / (long long)SB);
+  if (Q8) stages = std::max<long long>(stages, NC);   // (a ring that was asked for smaller than the warps need)
   stages = std::min<long long>(stages, kMaxStages);
   if (stages < NC) return cudaErrorInvalidConfiguration;   // every consumer warp owns at least one stage
-  const size_t dyn = ring_off + (size_t)stages * PB;
+  const size_t dyn = ring_off + (size_t)stages * SB;
   int dev = 0;
   if ((e = cudaGetDevice(&dev)) != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !opted_in[dev]) {
