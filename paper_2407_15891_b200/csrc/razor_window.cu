@@ -46,8 +46,8 @@ constexpr int kWinThreads = 384;
 // Registers: 168 a thread at launch; the softmax threads, which hold a row of 128 scores, take over what the others give up.
 constexpr int kWinLaunchRegs = 168, kWinSoftmaxRegs = 216, kWinOtherRegs = 72;
 static_assert(256 * kWinSoftmaxRegs + 128 * kWinOtherRegs <= kWinThreads * kWinLaunchRegs, "no more than the block was launched with");
+constexpr int kParts = 2;                    // P is handed over in so many parts (32K tokens: 7.1 ms; in four parts 7.3)
 constexpr int kHalfBytes = kWinTile * 128;   // 128 rows of 64 elements
-constexpr int kWinPolyEvery = 3;             // of so many pairs of exponentials one is a polynomial (0: none)
 
 template <int D>
 struct WinCfg {
@@ -66,7 +66,8 @@ struct WinCall {
   int64_t v_stride_b, v_stride_h, v_stride_n;
   int32_t batch, n_tokens, n_ctx, n_q_heads, n_kv_heads, group, tpt;   // tpt: query tokens of a tile
   int32_t n_sink, n_units, pairs, spans;   // spans: 1: the steps are cut into spans; 0: units from the queue
-  int32_t rec_rows;         // rows of a record
+  int32_t rec_rows;         // rows of a record: those of two tiles
+  int32_t rec_tile;         // query tokens of a tile in it
   float scale_log2;
   // workspace
   int32_t* queue;
@@ -86,7 +87,7 @@ struct WinItem {
 struct WinCtl {
   uint64_t q_full[2], q_empty[2];
   uint64_t k_full[4], k_empty[4], v_full[4], v_clean[4], v_empty[4];
-  uint64_t s_full[2], p_full[2][2], o_full[2];   // (P in two halves: its product begins with the first)
+  uint64_t s_full[2], p_full[2][kParts], o_full[2];   // (P in parts: its product begins with the first)
   uint64_t item_full[2], item_empty[2];
   uint64_t drain;
   WinItem item[2];
@@ -121,6 +122,15 @@ __device__ __forceinline__ void win_tmem_st32(uint32_t taddr, const uint32_t* v)
         "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
       : "memory");
 }
+__device__ __forceinline__ void win_tmem_st16(uint32_t taddr, const uint32_t* o) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+      :
+      : "r"(taddr), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "r"(o[8]),
+        "r"(o[9]), "r"(o[10]), "r"(o[11]), "r"(o[12]), "r"(o[13]), "r"(o[14]), "r"(o[15])
+      : "memory");
+}
 // Scales 16 columns of this thread's lane.
 __device__ __forceinline__ void win_tmem_scale16(uint32_t taddr, float f) {
   uint32_t o[16];
@@ -137,13 +147,7 @@ __device__ __forceinline__ void win_tmem_scale16(uint32_t taddr, float f) {
     asm volatile("" : "+r"(o[e]));
     o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
   }
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-      :
-      : "r"(taddr), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "r"(o[8]),
-        "r"(o[9]), "r"(o[10]), "r"(o[11]), "r"(o[12]), "r"(o[13]), "r"(o[14]), "r"(o[15])
-      : "memory");
+  win_tmem_st16(taddr, o);
 }
 __device__ __forceinline__ void win_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t win_pack2(float lo, float hi) {
@@ -239,20 +243,54 @@ __global__ void __launch_bounds__(kWinThreads, 1)
   volatile int* abort_flag = &ctl->abort_flag;
 
   cudaTriggerProgrammaticLaunchCompletion();   // (the combine kernel waits for this whole grid before it reads)
+  if (threadIdx.x < 3 * 32 && lane == 0)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(warp == 0 ? &map_q : (warp == 1 ? &map_k : &map_v)) : "memory");
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&ctl->q_full[i], 1);
+      mbar_init(&ctl->q_empty[i], 1);
+      mbar_init(&ctl->s_full[i], 1);
+      for (int k = 0; k < kParts; ++k) mbar_init(&ctl->p_full[i][k], 128);
+      mbar_init(&ctl->o_full[i], 1);
+      mbar_init(&ctl->item_full[i], 1);
+      mbar_init(&ctl->item_empty[i], kItemReaders);
+    }
+    for (int s = 0; s < 4; ++s) {
+      mbar_init(&ctl->k_full[s], 1);
+      mbar_init(&ctl->k_empty[s], 1);
+      mbar_init(&ctl->v_full[s], 1);
+      mbar_init(&ctl->v_clean[s], 64);
+      mbar_init(&ctl->v_empty[s], 1);
+    }
+    mbar_init(&ctl->drain, 1);
+    ctl->abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 9) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
+                 "r"(kTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
   long long total = 0, span_end = 0, span_at = 0;   // steps of the launch; this CTA's span
   int n_spans = 1;
   if (c.spans) {
-    // ---- prefix sums of the units' weights: three units to a thread
+    // ---- prefix sums of the units' weights, three consecutive units to a thread.  (The weights are put down in the K stages,
+    // which nothing fills yet.)
     constexpr int PER = (kWinSpanUnits + kWinThreads - 1) / kWinThreads;
-    long long w[PER], sum = 0;
+    int* weights = (int*)k_tile;
+#pragma unroll 1
+    for (int unit = threadIdx.x; unit < c.n_units; unit += kWinThreads) {
+      int b, g, window, ctx;
+      weights[unit] = find_unit(c, unit, b, g, window, ctx).weight();
+    }
+    __syncthreads();
+    int w[PER];
+    long long sum = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
       const int unit = (int)threadIdx.x * PER + i;
-      w[i] = 0;
-      if (unit < c.n_units) {
-        int b, g, window, ctx;
-        w[i] = find_unit(c, unit, b, g, window, ctx).weight();
-      }
+      w[i] = unit < c.n_units ? weights[unit] : 0;
       sum += w[i];
     }
     long long upto = sum;
@@ -280,49 +318,22 @@ __global__ void __launch_bounds__(kWinThreads, 1)
         at += w[i];
       }
     }
-    if (total == 0) return;
-    if ((int)blockIdx.x >= n_spans) return;
-    span_at = win_span_begin(total, n_spans, blockIdx.x);
-    span_end = win_span_begin(total, n_spans, blockIdx.x + 1);
+    if (total > 0 && (int)blockIdx.x < n_spans) {
+      span_at = win_span_begin(total, n_spans, blockIdx.x);
+      span_end = win_span_begin(total, n_spans, blockIdx.x + 1);
+    }   // (otherwise there is nothing for this CTA: it goes through the motions with no item)
     long long at = before;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if (span_at >= at && span_at < at + w[i]) {
+      if (span_at < span_end && span_at >= at && span_at < at + w[i]) {
         ctl->first_unit = (int)threadIdx.x * PER + i;
         ctl->first_step = (int)(span_at - at);
       }
       at += w[i];
     }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // (the weights have been read: TMA may write there)
   }
 
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&ctl->q_full[i], 1);
-      mbar_init(&ctl->q_empty[i], 1);
-      mbar_init(&ctl->s_full[i], 1);
-      mbar_init(&ctl->p_full[i][0], 128);
-      mbar_init(&ctl->p_full[i][1], 128);
-      mbar_init(&ctl->o_full[i], 1);
-      mbar_init(&ctl->item_full[i], 1);
-      mbar_init(&ctl->item_empty[i], kItemReaders);
-    }
-    for (int s = 0; s < 4; ++s) {
-      mbar_init(&ctl->k_full[s], 1);
-      mbar_init(&ctl->k_empty[s], 1);
-      mbar_init(&ctl->v_full[s], 1);
-      mbar_init(&ctl->v_clean[s], 64);
-      mbar_init(&ctl->v_empty[s], 1);
-    }
-    mbar_init(&ctl->drain, 1);
-    ctl->abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
-                 "r"(kTmemCols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -360,8 +371,8 @@ __global__ void __launch_bounds__(kWinThreads, 1)
         ++n_s;
         tc_fence_after();
         if (!warp_live) {   // nobody reads these rows
-          mbar_arrive(&ctl->p_full[ti][0]);
-          mbar_arrive(&ctl->p_full[ti][1]);
+#pragma unroll
+          for (int h = 0; h < kParts; ++h) mbar_arrive(&ctl->p_full[ti][h]);
           continue;
         }
         uint32_t v[kWinTile];
@@ -405,26 +416,22 @@ __global__ void __launch_bounds__(kWinThreads, 1)
         const uint64_t scale2 = f2_pack(scale_log2, scale_log2), neg_m2 = f2_pack(-m_use, -m_use);
         uint64_t psum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t p[32];
+        for (int h = 0; h < kParts; ++h) {
+          constexpr int PAIRS = kWinTile / kParts / 2;
+          uint32_t p[PAIRS];
 #pragma unroll
-          for (int e2 = 0; e2 < 32; ++e2) {
-            const int e = h * 64 + e2 * 2;
+          for (int e2 = 0; e2 < PAIRS; ++e2) {
+            const int e = (h * PAIRS + e2) * 2;
             const uint64_t t2 = f2_fma(f2_pack(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), scale2, neg_m2);
-            uint64_t w2;
-            if (kWinPolyEvery > 0 && e2 % (kWinPolyEvery > 0 ? kWinPolyEvery : 1) == kWinPolyEvery - 1) {
-              w2 = f2_exp2_poly(t2);
-            } else {
-              float t0, t1;
-              f2_unpack(t2, t0, t1);
-              w2 = f2_pack(fast_exp2(t0), fast_exp2(t1));
-            }
-            psum[e2 & 1] = f2_add(psum[e2 & 1], w2);
             float w0, w1;
-            f2_unpack(w2, w0, w1);
+            f2_unpack(t2, w0, w1);
+            w0 = fast_exp2(w0);
+            w1 = fast_exp2(w1);
+            psum[e2 & 1] = f2_add(psum[e2 & 1], f2_pack(w0, w1));
             p[e2] = win_pack2(w0, w1);
           }
-          win_tmem_st32(s_addr + (uint32_t)(h * 32), p);
+          static_assert(PAIRS == 32, "a part is one store");
+          win_tmem_st32(s_addr + (uint32_t)(h * PAIRS), p);
           win_tmem_st_wait();
           tc_fence_before();
           mbar_arrive(&ctl->p_full[ti][h]);
@@ -446,7 +453,7 @@ __global__ void __launch_bounds__(kWinThreads, 1)
       if (!ok) inv = CUDART_NAN_F;
       const int tok = t.tok + r_tok;
       __nv_bfloat16* dst = c.out + (((size_t)it.b * c.n_tokens + tok) * c.n_q_heads + (size_t)it.g * G + r_head) * D;
-      const size_t rec = (size_t)max(it.slot, 0) * c.rec_rows + (size_t)(ti * c.tpt + r_tok) * G + r_head;
+      const size_t rec = (size_t)max(it.slot, 0) * c.rec_rows + (size_t)(ti * c.rec_tile + r_tok) * G + r_head;
       if (warp_live) {
 #pragma unroll
         for (int k = 0; k < D / 32; ++k) {
@@ -525,6 +532,7 @@ __global__ void __launch_bounds__(kWinThreads, 1)
             else step = (int)z;
             if (!some) continue;
             w.slot = w.j0 == 0 && w.j1 == w.u.n_steps ? -1 : 2 * (int)blockIdx.x + (w.j0 == 0 ? 1 : 0);
+            if (w.slot >= 0 && w.u.live <= c.tpt) w.u.share_steps();
           } else {
             w.j0 = 0;
             w.j1 = w.u.n_steps;
@@ -621,8 +629,8 @@ __global__ void __launch_bounds__(kWinThreads, 1)
           const uint32_t more = left_p[i] != cnt[i];   // the accumulator holds products of this item
 #pragma unroll
           for (int kk = 0; kk < kWinTile / 16; ++kk) {   // 16 tokens per instruction: 8 columns of bf16 pairs
-            if (kk % (kWinTile / 32) == 0) {
-              if (!mbar_wait(&ctl->p_full[i][kk / (kWinTile / 32)], np[i] & 1, abort_flag)) return false;
+            if (kk % (kWinTile / 16 / kParts) == 0) {
+              if (!mbar_wait(&ctl->p_full[i][kk / (kWinTile / 16 / kParts)], np[i] & 1, abort_flag)) return false;
               tc_fence_after();
             }
             win_umma_tmem_a(tmem + 2 * kWinTile + (uint32_t)(i * kWinTile), s_col + (uint32_t)(kk * 8),
@@ -738,23 +746,25 @@ __global__ void __launch_bounds__(256) window_combine_kernel(const __grid_consta
   const WinUnit u = find_unit(c, blockIdx.x, b, g, window, ctx);
   const int rows = u.live * c.group;   // (query token of the unit, query head)
   for (int row = blockIdx.y * 8 + warp; row < rows; row += gridDim.y * 8) {
+  // (a unit whose queries fit a tile has been shared by both: two records a part)
+  const int per = u.live <= c.tpt ? 2 : 1, records = parts * per;
   float m = -CUDART_INF_F, l = 0.f;
   LaneVec<D> acc;
   acc.zero();
   constexpr int U = 8;
-  for (int p0 = 0; p0 < parts; p0 += U) {
+  for (int p0 = 0; p0 < records; p0 += U) {
     float2 mls[U];
     LaneVec<D> os[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int p = min(p0 + i, parts - 1);   // beyond the end: read again, unused
-      const size_t r = (size_t)(2 * (s0 + p) + (p == 0 ? 1 : 0)) * c.rec_rows + row;
+      const int p = min(p0 + i, records - 1), part = p / per;   // beyond the end: read again, unused
+      const size_t r = (size_t)(2 * (s0 + part) + (part == 0 ? 1 : 0)) * c.rec_rows + (size_t)(p % per) * c.rec_tile * c.group + row;
       mls[i] = __ldcg(&c.rec_ml[r]);
       os[i].load_l2(c.rec_o + r * D, lane);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      if (p0 + i >= parts) break;
+      if (p0 + i >= records) break;
       const float2 ml = mls[i];
       const float mn = fmaxf(m, ml.x);
       const float mu = (mn == -CUDART_INF_F) ? 0.f : mn;
@@ -850,7 +860,7 @@ int win_layout(int batch, int n_q_heads, int n_kv_heads, int head_dim, int n_tok
   l.pairs = (n_tokens + 2 * l.tpt - 1) / (2 * l.tpt);
   l.units = (long long)l.pairs * batch * n_kv_heads;
   if (l.units > (1LL << 30)) return RAZOR_E_CAPACITY;
-  l.rec_rows = std::min(2 * l.tpt, n_tokens) * l.group;
+  l.rec_rows = 2 * std::min(l.tpt, n_tokens) * l.group;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   size_t off = 256;
   l.table = l.rec_ml = l.rec_o = off;
@@ -911,6 +921,7 @@ extern "C" int razor_window_attention(const void* q, int64_t q_stride_b, int64_t
   c.group = l.group; c.tpt = l.tpt; c.n_sink = n_sink; c.n_units = (int)l.units; c.pairs = l.pairs;
   c.spans = l.units <= kWinSpanUnits;
   c.rec_rows = l.rec_rows;
+  c.rec_tile = std::min(l.tpt, n_tokens);
   c.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)head_dim) : sm_scale) * 1.4426950408889634f;
   uint8_t* ws = (uint8_t*)workspace;
   c.queue = (int32_t*)ws;

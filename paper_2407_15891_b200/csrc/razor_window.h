@@ -20,15 +20,20 @@ constexpr int kWinMinSpan = 4;         // steps that a span has at least
 constexpr int kWinUnitCost = 3;        // what a unit costs beside its steps (its queries' way in, its results' way out), in steps
 
 // One tile of a unit: its live tokens [tok, tok + n_tok) and the steps that it takes part in, [0, sink_end) and
-// [win_begin, win_end).
+// [win_begin, win_end); with parity 0 or 1 only the even or the odd ones of them.
 struct WinTileSteps {
   int32_t tok, n_tok, pos;             // pos: position of token `tok`
   int32_t sink_end, win_begin, win_end;
-  RAZOR_HD bool active(int j) const { return j < sink_end || (j >= win_begin && j < win_end); }
+  int32_t parity;                      // -1: every step
+  RAZOR_HD bool active(int j) const {
+    return (j < sink_end || (j >= win_begin && j < win_end)) && (parity < 0 || (j & 1) == parity);
+  }
+  RAZOR_HD int count(int a, int b) const {   // its steps among a .. b - 1, 0 <= a
+    if (b <= a) return 0;
+    return parity < 0 ? b - a : (b + 1 - parity) / 2 - (a + 1 - parity) / 2;
+  }
   RAZOR_HD int steps_in(int a, int b) const {
-    const int s = (b < sink_end ? b : sink_end) - a;
-    const int w = (b < win_end ? b : win_end) - (a > win_begin ? a : win_begin);
-    return (s > 0 ? s : 0) + (w > 0 ? w : 0);
+    return count(a, b < sink_end ? b : sink_end) + count(a > win_begin ? a : win_begin, b < win_end ? b : win_end);
   }
 };
 struct WinUnit {
@@ -45,6 +50,13 @@ struct WinUnit {
     j0 = a > kWinUnitCost ? (int)(a - kWinUnitCost) : 0;
     j1 = z > kWinUnitCost ? (int)(z - kWinUnitCost) : 0;
     return n_steps == 0 ? a == 0 && z > 0 : j1 > j0;
+  }
+  // A unit whose queries fit one tile leaves the other idle.  Where it is cut up anyway (its records are folded later), both
+  // tiles take its queries, one the even and one the odd steps.
+  RAZOR_HD void share_steps() {
+    tile[1] = tile[0];
+    tile[0].parity = 0;
+    tile[1].parity = 1;
   }
 };
 
@@ -77,6 +89,7 @@ RAZOR_HD inline WinUnit win_unit(int tok0, int tpt, int q_len, int ctx, int wind
     t.n_tok = left < 0 ? 0 : (left < tpt ? left : tpt);
     t.pos = pos0 + i * tpt;
     t.sink_end = t.win_begin = t.win_end = 0;
+    t.parity = -1;
     const int t_last = t.pos + t.n_tok - 1;
     if (!any || t.n_tok == 0 || t_last < 0) continue;
     const int hi = t_last / kWinTile;
@@ -107,10 +120,17 @@ RAZOR_HD inline int win_n_spans(long long total, int ctas) {
   const long long most = total / kWinMinSpan;
   return (int)(most < 1 ? 1 : (most < ctas ? most : ctas));
 }
-RAZOR_HD inline long long win_span_begin(long long total, int n_spans, int c) { return total * c / n_spans; }
+RAZOR_HD inline long long win_span_begin(long long total, int n_spans, int c) {   // total * c / n_spans
+  if (total < (1LL << 31)) {   // (in 32 bits where they do: a division of 64 takes ten times as long)
+    const uint32_t each = (uint32_t)total / (uint32_t)n_spans, rest = (uint32_t)total % (uint32_t)n_spans;
+    return (long long)each * c + rest * (uint32_t)c / (uint32_t)n_spans;
+  }
+  return total * c / n_spans;
+}
 // The span that place s lies in.
 RAZOR_HD inline int win_span_of(long long total, int n_spans, long long s) {
-  int c = (int)(s * n_spans / total);
+  int c = (int)((double)s / (double)total * n_spans);   // (a guess)
+  if (c >= n_spans) c = n_spans - 1;
   while (c + 1 < n_spans && win_span_begin(total, n_spans, c + 1) <= s) ++c;
   while (c > 0 && win_span_begin(total, n_spans, c) > s) --c;
   return c;

@@ -59,6 +59,19 @@ int main() {
       }
     }
   }
+  // a unit of one tile shared by both: every step goes to exactly one of them
+  for (int at = 0; at < 3000; ++at) {
+    WinUnit u = win_unit(0, 128, rnd(1, 128), rnd(1, 1500), rnd(0, 2) ? rnd(0, 700) : -1, rnd(0, 300));
+    const WinTileSteps whole = u.tile[0];
+    u.share_steps();
+    for (int j = 0; j < u.n_steps; ++j) CHECK((int)u.tile[0].active(j) + (int)u.tile[1].active(j) == (int)whole.active(j));
+    const int a = rnd(0, u.n_steps), b = rnd(a, u.n_steps);
+    for (int i = 0; i < 2; ++i) {
+      int n = 0;
+      for (int j = a; j < b; ++j) n += u.tile[i].active(j);
+      CHECK(u.tile[i].steps_in(a, b) == n);
+    }
+  }
   for (int at = 0; at < 20000; ++at) {
     const long long total = rnd(1, 5) == 1 ? rnd(1, 30) : (long long)rnd(1, 2000000) * rnd(1, 3000);
     const int ctas = rnd(1, kWinMaxSpans), n = win_n_spans(total, ctas);
