@@ -122,6 +122,16 @@ def test_strides_scale_and_a_fused_projection():
     _check(q[:1, :, :2], K[:1, :1], V[:1, :1], one, 4)
 
 
+@pytest.mark.parametrize("T,N", [(200, 260), (1, 9000)])
+def test_out_at_a_16_byte_boundary(T, N):
+    q, K, V = _inputs(1, T, N, 4, 2, 128, seed=9)
+    buffer = torch.zeros(q.numel() + 16, dtype=torch.bfloat16, device=DEV)
+    out = buffer[8:8 + q.numel()].view(q.shape)
+    assert out.data_ptr() % 32 == 16
+    rz.razor_window_attention(q, K, V, 4, out=out)
+    assert torch.equal(out, rz.razor_window_attention(q, K, V, 4)) and not buffer[:8].any() and not buffer[-8:].any()
+
+
 @pytest.mark.parametrize("T,N,Hq,Hk,D,ctx", [(1, 40000, 8, 2, 128, [40000, 33]), (2, 20011, 2, 2, 64, [20011, 20000]),
                                              (130, 9000, 4, 1, 128, [9000, 8000])])
 def test_few_queries_over_a_long_context_are_cut_into_spans(T, N, Hq, Hk, D, ctx):
