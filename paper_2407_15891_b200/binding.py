@@ -460,6 +460,7 @@ def razor_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], inv_freq: n
     x = q if q is not None else k
     B, T, _, D = x.shape
     dev, dtype = x.device, x.dtype
+    assert x.is_cuda
     assert q is None or k is None or (k.shape[:2] == q.shape[:2] and k.shape[3] == D and k.dtype is dtype and k.device == dev)
     assert inv_freq.dtype == np.float64 and inv_freq.ndim == 1 and inv_freq.strides == (8,)
     if positions is not None:
@@ -494,7 +495,7 @@ def razor_window_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, n_
     (B, T, Hq, D), (_, Hk, N, _), dev = q.shape, K.shape, q.device
     q_b, q_t, q_h, q_d = q.stride()
     kv = K.stride()
-    assert q.dtype is torch.bfloat16 and K.dtype is torch.bfloat16 and V.dtype is torch.bfloat16
+    assert q.is_cuda and q.dtype is torch.bfloat16 and K.dtype is torch.bfloat16 and V.dtype is torch.bfloat16
     assert K.shape == V.shape == (B, Hk, N, D) and kv == V.stride() and kv[3] == 1 and q_d == 1 and (Hq == 1 or q_h == D)
     assert K.device == dev and V.device == dev
     for x, shape in ((window, (B, Hk)), (q_len, (B,)), (ctx_len, (B,))):

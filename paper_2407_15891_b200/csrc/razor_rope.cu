@@ -223,7 +223,7 @@ int take_side(const razor_rope_rows_t* r, int batch, int n_tokens, int head_dim,
     for (int d = 0; d < 3; ++d) {
       int64_t& x = st[side][d];
       if (n[d] <= 1) x = 0;
-      if (x < 0 || x > (1LL << 40)) return RAZOR_E_INVALID_ARG;
+      if (x < 0 || x > (1LL << 40) || (x > 0 && n[d] > (1LL << 52) / x)) return RAZOR_E_INVALID_ARG;   // (no such memory)
       // two rows of the output in one place would be written twice (a repeated input row is fine)
       if (side == 1 && n[d] > 1 && x < head_dim) return RAZOR_E_INVALID_ARG;
       misaligned |= ((x * es) & 15) != 0;
@@ -295,7 +295,7 @@ extern "C" int razor_rope(const razor_rope_rows_t* q, const razor_rope_rows_t* k
                           int32_t interleaved, int32_t inverse, void* stream) {
   using namespace razor;
   if (!inv_freq) return RAZOR_E_NULL_PTR;
-  if (batch < 1 || n_tokens < 0 || !std::isfinite(gain)) return RAZOR_E_INVALID_ARG;
+  if (batch < 1 || n_tokens < 0 || (int64_t)batch * n_tokens > (1LL << 40) || !std::isfinite(gain)) return RAZOR_E_INVALID_ARG;
   if (dtype != RAZOR_F32 && dtype != RAZOR_BF16) return RAZOR_E_UNSUPPORTED_DIM;
   const int es = dtype == RAZOR_BF16 ? 2 : 4;
   if (head_dim < 2 || head_dim > kRopeMaxDim || (head_dim * es) % 16) return RAZOR_E_UNSUPPORTED_DIM;

@@ -122,6 +122,28 @@ def test_strides_scale_and_a_fused_projection():
     _check(q[:1, :, :2], K[:1, :1], V[:1, :1], one, 4)
 
 
+def test_a_large_batch_of_single_tokens_captured():
+    """More units than the spans are made for, lengths that change between replays."""
+    q, K, V = _inputs(65, 1, 300, 32, 16, 64, seed=3)
+    rng = np.random.default_rng(1)
+    window = rng.integers(-1, 200, (65, 16)).tolist()
+    out, ctx = torch.zeros_like(q), _dev([300] * 65)
+    w = _dev(window)
+    ws = torch.empty(rz.razor_window_attention_workspace_bytes(65, 32, 16, 64, 1), dtype=torch.uint8, device=DEV)
+    rz.razor_window_attention(q, K, V, 4, w, None, ctx, out=out, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        rz.razor_window_attention(q, K, V, 4, w, None, ctx, out=out, workspace=ws)
+    for _ in range(2):
+        lens = rng.integers(0, 301, 65).tolist()
+        ctx.copy_(_dev(lens))
+        graph.replay()
+        torch.cuda.synchronize()
+        _check(q, K, V, out, 4, window, None, lens)
+
+
 @pytest.mark.parametrize("T,N", [(200, 260), (1, 9000)])
 def test_out_at_a_16_byte_boundary(T, N):
     q, K, V = _inputs(1, T, N, 4, 2, 128, seed=9)
