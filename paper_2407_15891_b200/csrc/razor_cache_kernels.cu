@@ -137,6 +137,25 @@ __global__ void __launch_bounds__(kCompressThreads) compress_kernel(DeviceView d
           __syncwarp();
           if (lane == 0) mbar_arrive(&sm.empty[s]);
         }
+        // (Q8) The largest magnitudes of all the rows at once: sixteen chains of exchanges side by side instead of one after the
+        // other.  (A block of dropped rows has no use for them.)
+        float top[CH][2];
+        if constexpr (Q8) {
+          if (keep_all || p0 < n_sink || p0 + kPageTokens > recent0) {
+#pragma unroll
+            for (int it = 0; it < CH; ++it) {
+              top[it][0] = Q8Row<D>::lane_top(kf[it]);
+              top[it][1] = Q8Row<D>::lane_top(vf[it]);
+            }
+#pragma unroll
+            for (int off = LPR / 2; off > 0; off >>= 1)
+#pragma unroll
+              for (int it = 0; it < CH; ++it) {
+                top[it][0] = max_nan(top[it][0], __shfl_xor_sync(0xffffffffu, top[it][0], off));
+                top[it][1] = max_nan(top[it][1], __shfl_xor_sync(0xffffffffu, top[it][1], off));
+              }
+          }
+        }
 #pragma unroll
         for (int it = 0; it < CH; ++it) {
           const int t = RG * (c * CH + it) + par, p = p0 + t;
@@ -149,10 +168,9 @@ __global__ void __launch_bounds__(kCompressThreads) compress_kernel(DeviceView d
             const size_t page = (size_t)pt[slot >> 4];
             if constexpr (Q8) {
               uint8_t* at = dv.pool + page * dv.page_bytes;
-              const unsigned lanes = (unsigned)((1ull << LPR) - 1) << (par * LPR);
               float held[EPL];
-              Q8Row<D>::store(at, slot, 0, lir, kf[it], lanes, held);
-              Q8Row<D>::store(at, slot, 1, lir, vf[it], lanes, held);
+              Q8Row<D>::store(at, slot, 0, lir, kf[it], top[it][0], held);
+              Q8Row<D>::store(at, slot, 1, lir, vf[it], top[it][1], held);
             } else {
               uint4* dst = (uint4*)(dv.pool + page * dv.page_bytes + (size_t)(slot & 15) * RB) + swz(slot, lir);
               dst[0] = kf[it];
@@ -321,8 +339,8 @@ __global__ void __launch_bounds__(64) append_kernel(DeviceView dv, int layer, co
       if constexpr (Q8) {
         constexpr unsigned lanes = (unsigned)((1ull << LPR) - 1);
         float held[EPL];
-        Q8Row<D>::store(at, slot, 0, lane, kf, lanes, held);
-        Q8Row<D>::store(at, slot, 1, lane, vf, lanes, held);
+        Q8Row<D>::store(at, slot, 0, lane, kf, Q8Row<D>::row_top(kf, lanes), held);
+        Q8Row<D>::store(at, slot, 1, lane, vf, Q8Row<D>::row_top(vf, lanes), held);
       } else {
         krow[0] = kf;
         krow[kPageTokens * LPR] = vf;
@@ -412,8 +430,8 @@ __global__ void __launch_bounds__(128) append_many_kernel(DeviceView dv, int lay
         if constexpr (Q8) {
           constexpr unsigned lanes = (unsigned)((1ull << LPR) - 1);
           float held[EPL];
-          Q8Row<D>::store(at, slot, 0, lane, kf, lanes, held);
-          Q8Row<D>::store(at, slot, 1, lane, vf, lanes, held);
+          Q8Row<D>::store(at, slot, 0, lane, kf, Q8Row<D>::row_top(kf, lanes), held);
+          Q8Row<D>::store(at, slot, 1, lane, vf, Q8Row<D>::row_top(vf, lanes), held);
         } else {
           krow[0] = kf;
           krow[kPageTokens * LPR] = vf;
@@ -501,8 +519,8 @@ __global__ void __launch_bounds__(256) append_chunk_kernel(DeviceView dv, int la
         }
         if constexpr (Q8) {
           const unsigned lanes = (unsigned)((1ull << LPR) - 1) << (threadIdx.x % 32 / LPR * LPR);
-          Q8Row<D>::store(at, slot, 0, lir, kf, lanes, a_k);   // (a_k, a_v: the values held)
-          Q8Row<D>::store(at, slot, 1, lir, vf, lanes, a_v);
+          Q8Row<D>::store(at, slot, 0, lir, kf, Q8Row<D>::row_top(kf, lanes), a_k);   // (a_k, a_v: the values held)
+          Q8Row<D>::store(at, slot, 1, lir, vf, Q8Row<D>::row_top(vf, lanes), a_v);
         } else {
           dst[0] = kf;
           dst[kPageTokens * LPR] = vf;
@@ -523,8 +541,8 @@ __global__ void __launch_bounds__(256) append_chunk_kernel(DeviceView dv, int la
             const unsigned lanes = (unsigned)((1ull << LPR) - 1) << (threadIdx.x % 32 / LPR * LPR);
             uint32_t w[2];
             float scale;
-            Q8Row<D>::quantise(kf, lanes, w, scale, a_k);
-            Q8Row<D>::quantise(vf, lanes, w, scale, a_v);
+            Q8Row<D>::quantise(kf, Q8Row<D>::row_top(kf, lanes), w, scale, a_k);
+            Q8Row<D>::quantise(vf, Q8Row<D>::row_top(vf, lanes), w, scale, a_v);
           }
         }
 #pragma unroll

@@ -58,6 +58,12 @@ struct RowGeom {
 // need; row-wise readers just permute their lanes.
 __device__ __forceinline__ int swz(int token, int chunk) { return chunk ^ (token & 7); }
 
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 // ---- pages of 8-bit rows.  A row x is held as codes c = round(x * (127 / top)), top its largest magnitude, and one scale
 // top / 127 in fp32: the value held is scale * c (off by at most half a step, top / 254).  Quotients, product and rounding
 // are IEEE's, to nearest even, so that anybody can compute the same codes.  A page is [16 K rows of D bytes][16 V rows][16 K
@@ -86,38 +92,48 @@ struct Q8Row {   // eight elements of a row per lane, D / 8 lanes to a row
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = s * (float)((int)(((i < 4 ? u.x : u.y) >> (8 * (i & 3))) & 0xffu) - 128);
   }
-  // Quantises a row whose eight bf16 elements of this lane are `raw`; the kLpr lanes of the row (`lanes`) take part.  w, s:
-  // codes and scale, held: the values they stand for.  A row whose largest magnitude is below 2^-100 is held as zeros (the
-  // quotient would leave the range of fp32), one with a value that is not finite as NaN.
-  static __device__ __forceinline__ void quantise(const uint4& raw, unsigned lanes, uint32_t (&w)[2], float& s, float (&held)[8]) {
+  // The largest magnitude among this lane's eight elements; of the whole row it is the maximum over its kLpr lanes.  NaN if
+  // an element is.
+  static __device__ __forceinline__ float lane_top(const uint4& raw) {
+    float f[8], top = 0.f;
+    Elem<__nv_bfloat16>::unpack(raw, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(f[i]));
+    return top;
+  }
+  static __device__ __forceinline__ float row_top(const uint4& raw, unsigned lanes) {
+    float top = lane_top(raw);
+#pragma unroll
+    for (int off = kLpr / 2; off > 0; off >>= 1) top = max_nan(top, __shfl_xor_sync(lanes, top, off));
+    return top;
+  }
+  // Quantises the eight bf16 elements `raw` of a row whose largest magnitude is `top`.  w, s: codes and scale, held: the
+  // values they stand for.  A row whose largest magnitude is below 2^-100 is held as zeros (the quotient would leave the
+  // range of fp32), one with a value that is not finite as NaN.
+  static __device__ __forceinline__ void quantise(const uint4& raw, float top, uint32_t (&w)[2], float& s, float (&held)[8]) {
     float f[8];
     Elem<__nv_bfloat16>::unpack(raw, f);
-    float top = 0.f;
-    bool odd = false;
+    const bool fine = top < __uint_as_float(0x7f800000u), some = top >= 7.888609052210118e-31f;
+    const float inv = fine && some ? __fdiv_rn(127.f, top) : 0.f;
+    s = !fine ? __uint_as_float(0x7fc00000u) : (some ? __fdiv_rn(top, 127.f) : 0.f);
+    // A product of at most 127 and a bit, plus 1.5 * 2^23: rounded to a whole number, half to even, which is in the low bits.
+    // (Conversions to integers take the slow unit; a 32K fill was bound by them and the packing.)
+    constexpr float kMagic = 12582912.f;
+    uint32_t r[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      top = fmaxf(top, fabsf(f[i]));
-      odd |= (__float_as_uint(f[i]) & 0x7f800000u) == 0x7f800000u;
+      const float x = __fadd_rn(__fmul_rn(f[i], inv), kMagic);
+      r[i] = __float_as_uint(x);
+      held[i] = s * (x - kMagic);
     }
-    if (odd) top = __uint_as_float(0x7f800000u);
 #pragma unroll
-    for (int off = kLpr / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(lanes, top, off));
-    float inv = __fdiv_rn(127.f, top);
-    s = __fdiv_rn(top, 127.f);
-    if (top < 7.888609052210118e-31f) inv = s = 0.f;
-    if (top == __uint_as_float(0x7f800000u)) s = __uint_as_float(0x7fc00000u);
-    w[0] = w[1] = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int c = __float2int_rn(__fmul_rn(f[i], inv));   // (NaN gives 0)
-      w[i >> 2] |= (uint32_t)((min(max(c, -127), 127) + 128) & 0xff) << (8 * (i & 3));
-      held[i] = s * (float)c;
-    }
+    for (int i = 0; i < 2; ++i)
+      w[i] = __byte_perm(__byte_perm(r[4 * i], r[4 * i + 1], 0x0040), __byte_perm(r[4 * i + 2], r[4 * i + 3], 0x0040), 0x5410) ^ 0x80808080u;
   }
-  static __device__ __forceinline__ void store(uint8_t* page, int slot, int kv, int lir, const uint4& raw, unsigned lanes, float (&held)[8]) {
+  static __device__ __forceinline__ void store(uint8_t* page, int slot, int kv, int lir, const uint4& raw, float top, float (&held)[8]) {
     uint32_t w[2];
     float s;
-    quantise(raw, lanes, w, s, held);
+    quantise(raw, top, w, s, held);
     *(uint2*)codes(page, slot, kv, lir) = make_uint2(w[0], w[1]);
     if (lir == 0) *scale(page, slot, kv) = s;
   }
