@@ -36,7 +36,8 @@ struct CompressSmem {
   int abort_flag;
 };
 
-// Q8: the kept rows are quantised as they are packed (dropped rows are summed as they came).
+// Q8: the kept rows are quantised as they are packed (dropped rows are summed as they came).  2 x 32 heads of 32768 tokens:
+// 290 us where bf16 rows, of which twice the bytes are written, take 240.
 template <typename T, int D, bool Q8>
 __global__ void __launch_bounds__(kCompressThreads) compress_kernel(DeviceView dv, int layer, int n_slices) {
   using Geo = RowGeom<T, D>;

@@ -387,8 +387,10 @@ __device__ __forceinline__ void consume_page_mma(uint32_t page_addr, int valid, 
 // The order of the contraction indexes is free, so it is chosen for the loads: a lane (g = lane / 4, t = lane % 4) takes the
 // 16-byte chunks t (and t + 4) of the K rows g and g + 8, and D / 8 bytes at g D / 8 of the V rows 2t, 2t + 1, 2t + 8, 2t + 9:
 // rows g and g + 8 of O^T's tile mt are the dimensions g D / 8 + 2 mt and + 2 mt + 1.
-// A page is 4224 bytes at D = 128 where a bf16 page is 8448: at the copy rate an SM gets one in 181 cycles, against some 300
-// warp instructions for it.
+// A page is 4224 bytes at D = 128 where a bf16 page is 8192: at the copy rate an SM gets one in 181 cycles, against some 430
+// warp instructions for it (waits included).  64K MHA layer (886 MB): 149 us where one cache is read again and again, 170 over
+// caches that change, 5.2-5.9 TB/s (0.80-0.91 of the measured copy rate; in bf16 1718 MB in 240); without the arithmetic the
+// copies alone take 130.  More streaming warps (10, 12, 14) and products in longer independent chains changed nothing.
 constexpr float kQ8WeightTop = 16384.f;   // 2^14
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm(

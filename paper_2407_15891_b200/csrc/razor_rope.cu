@@ -14,7 +14,8 @@
 // Bound by memory: every value is read once and written once.  A thread owns a chunk of E pairs (two 16-byte pieces of a
 // row), works out its sines and cosines once per token and walks over the heads of queries and keys alike with them, four
 // heads' loads in flight; a token's heads are spread over as many threads as it takes to fill the GPU, so a decode step is
-// one short pass.
+// one short pass.  8192 tokens of 32 + 8 heads, bf16: 32.9 us, 5.1 TB/s (0.78 of the measured copy rate); 8004 tokens of 40 + 40
+// heads, fp32, half of each turned: 119 us, 5.5 TB/s (0.84).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>

@@ -12,8 +12,7 @@
 //   * warp 8: TMA copies (Q per tile, a ring of K tiles, a ring of V tiles, 128-byte swizzle) and the walk over the units;
 //   * warp 9, one thread: the matrix instructions.  S_i = Q_i K^T (both operands in shared memory), O_i += P_i V (P out of
 //     tensor memory, as soon as its first half is there).  While one tile is in its softmax the other one's products run:
-//     PV_0, QK_0, PV_1, QK_1, ..  (An issuing thread for each tile was tried: the tiles then drift into step, both in their
-//     softmax at once, and 32K tokens took 9.0 ms for 8.5.)
+//     PV_0, QK_0, PV_1, QK_1, ..;
 //   * warps 10, 11: look over the V tiles that are partly masked.  A weight of zero times a NaN or an infinity is a NaN, so
 //     such values are zeroed in shared memory, and put back into the rows that do see them at the end (rows that a mask
 //     hides from a token are never touched by it, whatever it holds).
@@ -25,6 +24,18 @@
 // live there): a long context with few queries is spread over all SMs, and equal units fill the last wave.  Units that were
 // cut leave partial records (m, l, o) per row, which window_combine_kernel folds in order.  More units than that are handed
 // out whole from a queue, longest first.
+//
+// What bounds it.  Long contexts, D = 128: a step of both tiles is 2048 cycles of products (128 x 128 x 16 in 64 cycles) and
+// takes 3500: a tile's softmax (2000: 128 exponentials a thread, as many again for scale, maximum, sum and conversion) and its
+// way through the products (1450) follow each other, and two tiles fill no more than that.  32768 tokens, 32 query heads over
+// 8, all in sight: 7.1 ms in short runs (1235 TFLOP/s, 0.79 of the measured cuBLAS burst rate), 8.3 under continuous load,
+// where the power cap holds the clock (1060 TFLOP/s, 0.79 of cuBLAS's sustained rate); 8192 tokens 0.53 ms, a window of 1024 at
+// 32768 0.68 ms.  Short units pay their start (8500 cycles to the first scores of a launch, about half of it before the first
+// copy) and their results' way out (4400 cycles: a thread writes a row of its own).  One token over dense K and V is bound by the
+// same chain, a tile's step being short of rows but not of latency: 164 MB in 50 us.
+// Tried and dropped: an issuing thread for each tile (9.0 ms for 8.5 as it stood then: the tiles drift into step); sixteen
+// softmax warps, two threads to a row (10.3 ms for 7.6: the threads' exchange, twice the waits); every third, fifth or eighth
+// pair of exponentials as a polynomial (7.6, 7.6, 7.5 ms for 7.1: instructions are shorter than the unit); P in four parts.
 //
 // Every wait is bounded in time; a wait that runs out ends the CTA through the common exit (copies and instructions in flight
 // are waited for, tensor memory is released) and leaves NaN in the rows it was working on.
