@@ -31,7 +31,7 @@
  *     off by at most top / 254.  A row with top < 2^-100 is held as zeros, one with a value that is not finite as NaN.
  *     A kept token takes 2 (D + 4) bytes a KV head.  Rows that a compression drops are summed (Eq. 4) as they came, and so
  *     are new tokens of a head without a window; a row that leaves the window counts as the values it was held with.  razor_decode_attention, _step and _multi attend to
- *     the values held, in fp32 accuracy (a NaN in a cached K or V row, now the whole row, shows in the query rows that see it
+ *     the values held, in fp32 accuracy (razor_decode_step takes two launches; a NaN in a cached K or V row, now the whole row, shows in the query rows that see it
  *     and in no other); a round of more than 8 query rows per KV head runs block by block, each block reading the cache once.
  *     razor_cache_export gives the values held (K and V in fp32).  The tree calls refuse such a cache (UNSUPPORTED_DIM).
  *   - The cache and attention calls never apply rotary embeddings: K and q arrive after the rotary transformation,
