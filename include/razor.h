@@ -21,8 +21,8 @@
  *   - Work is enqueued on the CUDA stream passed as `stream` (a cudaStream_t cast to void*; NULL is
  *     the default stream) and is asynchronous with respect to the host.  All calls on one cache
  *     must be stream-ordered with respect to each other (they share scratch buffers).
- *   - Made for CUDA graphs: razor_decode_attention_tree and razor_verify_tree.  The other calls on a cache keep plans
- *     and lengths on the host, which a replay does not repeat.
+ *   - Made for CUDA graphs: razor_decode_attention_tree, razor_verify_tree, razor_rope and razor_window_attention.  The
+ *     other calls on a cache keep plans and lengths on the host, which a replay does not repeat.
  *   - Storage dtype of K, V and q is config.dtype; compensation sums/means and outputs are fp32.
  *   - A cache of 8-bit rows (config.dtype RAZOR_I8): K, V and q are bf16 everywhere in the calls; a row that is kept is
  *     quantised as it is written - by razor_compress, razor_compress_seq, razor_append, razor_append_many or
