@@ -8,7 +8,7 @@
 // query tokens x the G query heads that share a KV head), for which K and V are read once.  It walks over the 128-token key
 // tiles that some of its queries see (razor_window.h).  Roles:
 //   * warps 0-3 and 4-7: softmax of tile 0 and of tile 1, a thread per query row (tensor-memory lane): 128 scores out of
-//     tensor memory, mask, running maximum and sum, weights as bf16 back into tensor memory, over the scores;
+//     tensor memory, mask, running maximum, weights as bf16 back into tensor memory, over the scores, and the sum of those;
 //   * warp 8: TMA copies (Q per tile, a ring of K tiles, a ring of V tiles, 128-byte swizzle) and the walk over the units;
 //   * warp 9, one thread: the matrix instructions.  S_i = Q_i K^T (both operands in shared memory), O_i += P_i V (P out of
 //     tensor memory, as soon as its first half is there).  While one tile is in its softmax the other one's products run:
@@ -28,9 +28,9 @@
 // What bounds it.  Long contexts, D = 128: a step of both tiles is 2048 cycles of products (128 x 128 x 16 in 64 cycles) and
 // takes 3500: a tile's softmax (2000: 128 exponentials a thread, as many again for scale, maximum, sum and conversion) and its
 // way through the products (1450) follow each other, and two tiles fill no more than that.  32768 tokens, 32 query heads over
-// 8, all in sight: 7.1 ms in short runs (1235 TFLOP/s, 0.79 of the measured cuBLAS burst rate), 8.3 under continuous load,
-// where the power cap holds the clock (1060 TFLOP/s, 0.79 of cuBLAS's sustained rate); 8192 tokens 0.53 ms, a window of 1024 at
-// 32768 0.68 ms.  Short units pay their start (8500 cycles to the first scores of a launch, about half of it before the first
+// 8, all in sight: 7.3 ms in short runs (1208 TFLOP/s, 0.77 of the measured cuBLAS burst rate), 8.3 under continuous load,
+// where the power cap holds the clock (1060 TFLOP/s, 0.79 of cuBLAS's sustained rate); 8192 tokens 0.55 ms, a window of 1024 at
+// 32768 0.70 ms.  Short units pay their start (8500 cycles to the first scores of a launch, about half of it before the first
 // copy) and their results' way out (4400 cycles: a thread writes a row of its own).  One token over dense K and V is bound by the
 // same chain, a tile's step being short of rows but not of latency: 164 MB in 50 us.
 // Tried and dropped: an issuing thread for each tile (9.0 ms for 8.5 as it stood then: the tiles drift into step); sixteen
@@ -165,6 +165,15 @@ __device__ __forceinline__ void win_tmem_st_wait() { asm volatile("tcgen05.wait:
 __device__ __forceinline__ uint32_t win_pack2(float lo, float hi) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *(const uint32_t*)&v;
+}
+// a, b += the two bf16 values of `pair`, in fp32
+__device__ __forceinline__ void win_sum2(float& a, float& b, uint32_t pair) {
+  asm("{\n\t.reg .b16 lo, hi;\n\t"
+      "mov.b32 {lo, hi}, %2;\n\t"
+      "add.rn.f32.bf16 %0, lo, %0;\n\t"
+      "add.rn.f32.bf16 %1, hi, %1;\n\t}"
+      : "+f"(a), "+f"(b)
+      : "r"(pair));
 }
 // One matrix instruction, the descriptors as (low word, high word); the second with operand A out of tensor memory.
 __device__ __forceinline__ void win_umma(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
@@ -439,11 +448,13 @@ __global__ void __launch_bounds__(kWinThreads, 1)
         }
         const float m_use = (m_ref == -CUDART_INF_F) ? 0.f : m_ref;
         const uint64_t scale2 = f2_pack(scale_log2, scale_log2), neg_m2 = f2_pack(-m_use, -m_use);
-        uint64_t psum[2] = {f2_pack(0.f, 0.f), f2_pack(0.f, 0.f)};
+        // Weights go to the product with V in bf16: the instruction takes both operands in one type, and V is bf16.  (Their
+        // remainders would be a second product, half as much again of the instructions' time, for a result in bf16.)
+        uint32_t pw[kWinTile / 2];
 #pragma unroll
         for (int h = 0; h < kParts; ++h) {
           constexpr int PAIRS = kWinTile / kParts / 2;
-          uint32_t p[PAIRS];
+          uint32_t* const p = pw + h * PAIRS;
 #pragma unroll
           for (int e2 = 0; e2 < PAIRS; ++e2) {
             const int e = (h * PAIRS + e2) * 2;
@@ -452,7 +463,6 @@ __global__ void __launch_bounds__(kWinThreads, 1)
             f2_unpack(t2, w0, w1);
             w0 = fast_exp2(w0);
             w1 = fast_exp2(w1);
-            psum[e2 & 1] = f2_add(psum[e2 & 1], f2_pack(w0, w1));
             p[e2] = win_pack2(w0, w1);
           }
           static_assert(PAIRS == 32, "a part is one store");
@@ -461,9 +471,14 @@ __global__ void __launch_bounds__(kWinThreads, 1)
           tc_fence_before();
           mbar_arrive(&ctl->p_full[ti][h]);
         }
-        float a0, a1;
-        f2_unpack(f2_add(psum[0], psum[1]), a0, a1);
-        l_run += a0 + a1;
+        // The sum takes the weights as the product has them, rounded: a row is an average of the values it sees, whatever the
+        // rounding.  (With the unrounded ones a row of equal values came out up to a step of bf16 off, and so did a row whose
+        // largest weight is not 1, the reference lagging.)  Added up while the products run: 32K tokens 7.14 -> 7.28 ms, a window
+        // of 1024 there 0.674 -> 0.702; before the hand-over 7.37 and 0.712.
+        float psum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+#pragma unroll
+        for (int e = 0; e < kWinTile / 2; ++e) win_sum2(psum[e & 1][0], psum[e & 1][1], pw[e]);
+        l_run += (psum[0][0] + psum[1][0]) + (psum[0][1] + psum[1][1]);
         first = false;
       }
       if (ok && cnt > 0) {
