@@ -105,6 +105,7 @@ struct WinCtl {
   WinItem item[2];
   uint32_t tmem_base;
   int abort_flag;
+  unsigned issued_k, issued_v, issued_q[2];   // copies, by the copying thread when it leaves
   int first_unit, first_step;        // of this CTA's span
   long long scan[kWinThreads / 32];
 };
@@ -618,12 +619,10 @@ __global__ void __launch_bounds__(kWinThreads, 1)
           ++vc;
         }
       }
-      if (*abort_flag) {   // the copies in flight must land before the CTA may exit
-        for (int i = 0; i < 2; ++i)
-          if (nq[i] > 0) (void)mbar_wait_drain(&ctl->q_full[i], (nq[i] - 1) & 1);
-        for (unsigned x = kc > KS ? kc - KS : 0; x < kc; ++x) (void)mbar_wait_drain(&ctl->k_full[x % KS], (x / KS) & 1);
-        for (unsigned x = vc > VS ? vc - VS : 0; x < vc; ++x) (void)mbar_wait_drain(&ctl->v_full[x % VS], (x / VS) & 1);
-      }
+      ctl->issued_k = kc;
+      ctl->issued_v = vc;
+      ctl->issued_q[0] = nq[0];
+      ctl->issued_q[1] = nq[1];
     }
     __syncwarp();
   } else if (warp == 9) {
@@ -710,10 +709,6 @@ __global__ void __launch_bounds__(kWinThreads, 1)
           }
         }
       }
-      if (!ok) {   // leaving early: let the instructions in flight finish before tensor memory is released
-        umma_commit(&ctl->drain);
-        (void)mbar_wait_drain(&ctl->drain, 0);
-      }
     }
     __syncwarp();
   } else {
@@ -767,6 +762,23 @@ __global__ void __launch_bounds__(kWinThreads, 1)
   }
   tc_fence_before();
   __syncthreads();
+  // Every role has left, so the flag and the counts are final.  A role that gave up may have left behind copies or instructions
+  // that nobody waited for, of roles that had long ended well: the copies must land before the CTA may exit, the instructions
+  // finish before tensor memory is released.
+  if (*abort_flag) {
+    if (warp == 8 && lane == 0) {
+      const unsigned kc = ctl->issued_k, vc = ctl->issued_v;
+      for (int i = 0; i < 2; ++i)
+        if (ctl->issued_q[i] > 0) (void)mbar_wait_drain(&ctl->q_full[i], (ctl->issued_q[i] - 1) & 1);
+      for (unsigned x = kc > KS ? kc - KS : 0; x < kc; ++x) (void)mbar_wait_drain(&ctl->k_full[x % KS], (x / KS) & 1);
+      for (unsigned x = vc > VS ? vc - VS : 0; x < vc; ++x) (void)mbar_wait_drain(&ctl->v_full[x % VS], (x / VS) & 1);
+    }
+    if (warp == 9 && lane == 0) {
+      umma_commit(&ctl->drain);
+      (void)mbar_wait_drain(&ctl->drain, 0);
+    }
+    __syncwarp();
+  }
   if (warp == 9) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
