@@ -457,6 +457,8 @@ RAZOR_API int razor_rope(const razor_rope_rows_t* q, const razor_rope_rows_t* k,
  * may run at the same time need their own (captured graphs that are replayed side by side too).
  * The lengths and windows are read on the device: a replay of a captured call uses what they hold then.
  * Every wait in the kernel is bounded in time; should one ever run out, rows of the call are left NaN or as they were.
+ * razor_window_attention_wait_selftest is the same call in which thread block `cta` (>= 0; one that the launch does not have
+ * does nothing) gives up its waits at once, as if one had run out: a check of that.
  * Errors: NULL_PTR, INVALID_ARG, UNSUPPORTED_DIM, MISALIGNED, POOL_TOO_SMALL (workspace), CAPACITY (over 2^30 units of work), CUDA.
  */
 RAZOR_API int razor_window_attention_workspace_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -467,6 +469,12 @@ RAZOR_API int razor_window_attention(const void* q, int64_t q_stride_b, int64_t 
                                      int32_t n_ctx, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                                      int32_t n_sink, float sm_scale, void* out, void* workspace, size_t workspace_bytes,
                                      void* stream);
+RAZOR_API int razor_window_attention_wait_selftest(const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* K,
+                                     const void* V, int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_n,
+                                     const int32_t* window, const int32_t* q_len, const int32_t* ctx_len, int32_t batch,
+                                     int32_t n_tokens, int32_t n_ctx, int32_t n_q_heads, int32_t n_kv_heads,
+                                     int32_t head_dim, int32_t dtype, int32_t n_sink, float sm_scale, void* out,
+                                     void* workspace, size_t workspace_bytes, int32_t cta, void* stream);
 
 /*
  * Retrieval-head identification, the arithmetic of Section 3.3.  The model is run (by the caller) on

@@ -32,7 +32,7 @@ SYMBOLS = [
     "razor_schedule_query", "razor_schedule_combine_heads", "razor_cache_set_option", "razor_cache_device_status", "razor_cache_wait_selftest", "razor_cache_set_alibi", "razor_cache_set_head_windows",
     "razor_compensation_mean_static", "razor_head_scores_scratch_bytes", "razor_head_scores",
     "razor_select_retrieval_heads", "razor_rope_frequencies", "razor_rope",
-    "razor_window_attention_workspace_bytes", "razor_window_attention", "razor_cache_reset", "razor_cache_destroy", "razor_status_string",
+    "razor_window_attention_workspace_bytes", "razor_window_attention", "razor_window_attention_wait_selftest", "razor_cache_reset", "razor_cache_destroy", "razor_status_string",
     "razor_last_cuda_error", "razor_version",
 ]
 
@@ -108,6 +108,7 @@ def load() -> C.CDLL:
     lib.razor_window_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, C.POINTER(sz)]
     lib.razor_window_attention.argtypes = [vp, i64, i64, vp, vp, i64, i64, i64, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32,
                                            i32, C.c_float, vp, vp, sz, vp]
+    lib.razor_window_attention_wait_selftest.argtypes = [*lib.razor_window_attention.argtypes[:-1], i32, vp]
     lib.razor_cache_reset.argtypes = [vp]
     lib.razor_cache_destroy.argtypes = [vp]
     lib.razor_status_string.argtypes = [C.c_int]
@@ -492,6 +493,20 @@ def razor_window_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, n_
     [B, Hkv], q_len, ctx_len int32 [B] on the device or None.  -> out bf16 [B, T, Hq, D]; rows beyond a sequence's queries are
     left as they are (zeros when `out` is not given).  workspace: uint8, razor_window_attention_workspace_bytes long; one is
     allocated when none is given (on the current stream: give one with a `stream` of your own)."""
+    return _window_attention("razor_window_attention", (), q, K, V, n_sink, window, q_len, ctx_len, sm_scale, out, workspace, stream)
+
+
+def razor_window_attention_wait_selftest(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, n_sink: int, cta: int,
+                                         window: Optional[torch.Tensor] = None, q_len: Optional[torch.Tensor] = None,
+                                         ctx_len: Optional[torch.Tensor] = None, sm_scale: float = 0.0,
+                                         out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                         stream=None) -> torch.Tensor:
+    """razor_window_attention in which thread block `cta` gives up its waits at once: its rows are NaN or as they were."""
+    return _window_attention("razor_window_attention_wait_selftest", (cta,), q, K, V, n_sink, window, q_len, ctx_len, sm_scale,
+                             out, workspace, stream)
+
+
+def _window_attention(name, more, q, K, V, n_sink, window, q_len, ctx_len, sm_scale, out, workspace, stream) -> torch.Tensor:
     (B, T, Hq, D), (_, Hk, N, _), dev = q.shape, K.shape, q.device
     q_b, q_t, q_h, q_d = q.stride()
     kv = K.stride()
@@ -509,11 +524,10 @@ def razor_window_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, n_
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         assert workspace.device == dev and workspace.is_contiguous()
-        _check(load().razor_window_attention(q.data_ptr(), q_b, q_t, K.data_ptr(), V.data_ptr(), *kv[:3], _ptr(window),
-                                             _ptr(q_len), _ptr(ctx_len), B, T, N, Hq, Hk, D, RAZOR_BF16, n_sink, sm_scale,
-                                             out.data_ptr(), workspace.data_ptr(),
-                                             workspace.numel() * workspace.element_size(), _stream(stream)),
-               "razor_window_attention")
+        _check(getattr(load(), name)(q.data_ptr(), q_b, q_t, K.data_ptr(), V.data_ptr(), *kv[:3], _ptr(window), _ptr(q_len),
+                                     _ptr(ctx_len), B, T, N, Hq, Hk, D, RAZOR_BF16, n_sink, sm_scale, out.data_ptr(),
+                                     workspace.data_ptr(), workspace.numel() * workspace.element_size(), *more,
+                                     _stream(stream)), name)
     return out
 
 

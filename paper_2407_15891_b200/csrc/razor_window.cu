@@ -38,7 +38,8 @@
 // pair of exponentials as a polynomial (7.6, 7.6, 7.5 ms for 7.1: instructions are shorter than the unit); P in four parts.
 //
 // Every wait is bounded in time; a wait that runs out ends the CTA through the common exit (copies and instructions in flight
-// are waited for, tensor memory is released) and leaves NaN in the rows it was working on.
+// are waited for, tensor memory is released).  Rows that it was working on, and those of cut units that it had a part of, are
+// NaN; rows of its own that it had not come to stay as they were.
 #include <cuda.h>
 #include <math_constants.h>
 
@@ -81,8 +82,10 @@ struct WinCall {
   int32_t rec_tile;         // query tokens of a tile in it
   int32_t out_whole;        // out begins at a 32-byte boundary
   float scale_log2;
+  int32_t stopped_cta;      // -1; a self-test has this CTA give up its waits at once
   // workspace
   int32_t* queue;
+  uint8_t* done;            // [CTAs]: this CTA came to its end without giving up a wait
   int2* table;              // [n_units]: the first span with a part of the unit, and its parts (0: no query in it)
   float2* rec_ml;           // [2 * kWinMaxSpans][rec_rows]
   float* rec_o;             // [2 * kWinMaxSpans][rec_rows][D]
@@ -297,7 +300,7 @@ __global__ void __launch_bounds__(kWinThreads, 1)
       mbar_init(&ctl->v_empty[s], 1);
     }
     mbar_init(&ctl->drain, 1);
-    ctl->abort_flag = 0;
+    ctl->abort_flag = (int)blockIdx.x == c.stopped_cta;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) {
@@ -779,14 +782,15 @@ __global__ void __launch_bounds__(kWinThreads, 1)
     }
     __syncwarp();
   }
+  if (c.spans && threadIdx.x == 0) c.done[blockIdx.x] = *abort_flag == 0;
   if (warp == 9) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
   }
 }
 
-// Folds the records of the units that spans have cut, part by part in order: a warp per row.  grid = (units, row blocks),
-// block = 256.
+// Folds the records of the units that spans have cut, part by part in order: a warp per row.  A CTA that gave up has left
+// records unwritten, so a unit with a part of such a one is NaN.  grid = (units, row blocks), block = 256.
 template <int D>
 __global__ void __launch_bounds__(256) window_combine_kernel(const __grid_constant__ WinCall c) {
   cudaGridDependencySynchronize();
@@ -794,6 +798,9 @@ __global__ void __launch_bounds__(256) window_combine_kernel(const __grid_consta
   const int2 spans = __ldcg(&c.table[blockIdx.x]);
   const int s0 = spans.x, parts = spans.y;
   if (parts <= 1) return;   // in one piece
+  bool lost = false;
+  for (int p = lane; p < parts; p += 32) lost |= __ldcg(&c.done[s0 + p]) == 0;
+  lost = __any_sync(0xffffffffu, lost);
   int b, g, window, ctx;
   const WinUnit u = find_unit(c, blockIdx.x, b, g, window, ctx);
   const int rows = u.live * c.group;   // (query token of the unit, query head)
@@ -827,7 +834,7 @@ __global__ void __launch_bounds__(256) window_combine_kernel(const __grid_consta
       m = mn;
     }
   }
-  acc.scale(m == -CUDART_INF_F && !isnan(l) ? 0.f : 1.f / l);
+  acc.scale(lost ? CUDART_NAN_F : (m == -CUDART_INF_F && !isnan(l) ? 0.f : 1.f / l));
   __nv_bfloat16* dst = c.out + (((size_t)b * c.n_tokens + u.tile[0].tok + row / c.group) * c.n_q_heads + (size_t)g * c.group + row % c.group) * D;
   if constexpr (D == 128) {
     *(uint2*)(dst + lane * 4) = make_uint2(win_pack2(acc.v.x, acc.v.y), win_pack2(acc.v.z, acc.v.w));
@@ -897,7 +904,9 @@ cudaError_t launch_window(const WinCall& c, const void* q, int64_t q_b, int64_t 
   return cudaLaunchKernelEx(&cfg, window_combine_kernel<D>, c);
 }
 
-// Workspace: queue | table of units | (m, l) records | o records.
+// Workspace: queue and `done` (256 bytes) | table of units | (m, l) records | o records.
+constexpr size_t kWinDoneOffset = 64;
+static_assert(kWinDoneOffset + kWinMaxSpans <= 256, "beside the queue");
 struct WinLayout {
   size_t table, rec_ml, rec_o, total;
   int group, tpt, pairs, rec_rows;
@@ -940,12 +949,12 @@ extern "C" int razor_window_attention_workspace_bytes(int32_t batch, int32_t n_q
   return RAZOR_OK;
 }
 
-extern "C" int razor_window_attention(const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* K, const void* V,
-                                      int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_n, const int32_t* window,
-                                      const int32_t* q_len, const int32_t* ctx_len, int32_t batch, int32_t n_tokens, int32_t n_ctx,
-                                      int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t n_sink,
-                                      float sm_scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
-  using namespace razor;
+namespace razor {
+namespace {
+int window_call(const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* K, const void* V, int64_t kv_stride_b,
+                int64_t kv_stride_h, int64_t kv_stride_n, const int32_t* window, const int32_t* q_len, const int32_t* ctx_len,
+                int32_t batch, int32_t n_tokens, int32_t n_ctx, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                int32_t n_sink, float sm_scale, void* out, void* workspace, size_t workspace_bytes, int32_t stopped_cta, void* stream) {
   WinLayout l;
   const int rc = win_layout(batch, n_q_heads, n_kv_heads, head_dim, n_tokens, l);
   if (rc) return rc;
@@ -976,8 +985,10 @@ extern "C" int razor_window_attention(const void* q, int64_t q_stride_b, int64_t
   c.rec_rows = l.rec_rows;
   c.rec_tile = std::min(l.tpt, n_tokens);
   c.scale_log2 = (sm_scale == 0.f ? 1.0f / sqrtf((float)head_dim) : sm_scale) * 1.4426950408889634f;
+  c.stopped_cta = stopped_cta;
   uint8_t* ws = (uint8_t*)workspace;
   c.queue = (int32_t*)ws;
+  c.done = ws + kWinDoneOffset;
   c.table = (int2*)(ws + l.table);
   c.rec_ml = (float2*)(ws + l.rec_ml);
   c.rec_o = (float*)(ws + l.rec_o);
@@ -993,4 +1004,30 @@ extern "C" int razor_window_attention(const void* q, int64_t q_stride_b, int64_t
     return RAZOR_E_CUDA;
   }
   return RAZOR_OK;
+}
+
+}  // namespace
+}  // namespace razor
+
+extern "C" int razor_window_attention(const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* K, const void* V,
+                                      int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_n, const int32_t* window,
+                                      const int32_t* q_len, const int32_t* ctx_len, int32_t batch, int32_t n_tokens, int32_t n_ctx,
+                                      int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t n_sink,
+                                      float sm_scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  return razor::window_call(q, q_stride_b, q_stride_t, K, V, kv_stride_b, kv_stride_h, kv_stride_n, window, q_len, ctx_len, batch,
+                            n_tokens, n_ctx, n_q_heads, n_kv_heads, head_dim, dtype, n_sink, sm_scale, out, workspace,
+                            workspace_bytes, -1, stream);
+}
+
+extern "C" int razor_window_attention_wait_selftest(const void* q, int64_t q_stride_b, int64_t q_stride_t, const void* K,
+                                                    const void* V, int64_t kv_stride_b, int64_t kv_stride_h, int64_t kv_stride_n,
+                                                    const int32_t* window, const int32_t* q_len, const int32_t* ctx_len,
+                                                    int32_t batch, int32_t n_tokens, int32_t n_ctx, int32_t n_q_heads,
+                                                    int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t n_sink,
+                                                    float sm_scale, void* out, void* workspace, size_t workspace_bytes,
+                                                    int32_t cta, void* stream) {
+  if (cta < 0) return RAZOR_E_INVALID_ARG;
+  return razor::window_call(q, q_stride_b, q_stride_t, K, V, kv_stride_b, kv_stride_h, kv_stride_n, window, q_len, ctx_len, batch,
+                            n_tokens, n_ctx, n_q_heads, n_kv_heads, head_dim, dtype, n_sink, sm_scale, out, workspace,
+                            workspace_bytes, cta, stream);
 }
