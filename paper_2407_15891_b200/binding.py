@@ -159,6 +159,16 @@ def _stream(stream) -> Optional[int]:
     return int(stream) or None
 
 
+def _new(make, shape, dtype, dev, stream) -> torch.Tensor:
+    """torch.empty or torch.zeros for a call on `stream`: allocated there, so that memory still in use on the current stream is
+    not taken, and filled there, so that the fill comes before the call's kernels."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=dev)
+    s = int(stream)
+    with torch.cuda.stream(torch.cuda.ExternalStream(0 if s == 1 else s, device=dev)):   # (1: the legacy default stream by name)
+        return make(shape, dtype=dtype, device=dev)
+
+
 def make_config(batch, n_layers, n_q_heads, n_kv_heads, head_dim, dtype, n_sink, max_ctx_len, max_new_tokens,
                 use_compensation=1, page_shuffle_seed=0, sm_scale=0.0, page_tokens=16) -> RazorConfig:
     dt = {torch.float32: RAZOR_F32, torch.bfloat16: RAZOR_BF16, torch.int8: RAZOR_I8, "f32": RAZOR_F32, "bf16": RAZOR_BF16,
@@ -297,7 +307,7 @@ def razor_verify_tree(target: torch.Tensor, draft: Optional[torch.Tensor], token
     assert u_accept.shape == tokens.shape and u_sample.shape == (B,)
     assert tokens.is_contiguous() and parent.is_contiguous() and u_accept.is_contiguous() and u_sample.is_contiguous()
     assert tokens.device == dev and parent.device == dev and u_accept.device == dev and u_sample.device == dev
-    accepted, token, path = torch.empty(B * (T + 2), dtype=torch.int32, device=dev).split_with_sizes([B, B, B * T])
+    accepted, token, path = _new(torch.empty, B * (T + 2), torch.int32, dev, stream).split_with_sizes([B, B, B * T])
     path = path.view(B, T)
     with _on(dev):
         q_ptr, q_b, q_row = (draft.data_ptr(), draft.stride(0), draft.stride(1)) if draft is not None else (None, 0, 0)
@@ -413,9 +423,9 @@ def razor_head_scores(Q: torch.Tensor, K: torch.Tensor, period: int, sm_scale: f
     H, N, D = Q.shape
     need = C.c_size_t(0)
     _check(load().razor_head_scores_scratch_bytes(H, N, C.byref(need)), "razor_head_scores_scratch_bytes")
-    scratch = torch.empty(need.value, dtype=torch.uint8, device=Q.device)
-    echo = torch.empty(H, dtype=torch.float32, device=Q.device)
-    induction = torch.empty(H, dtype=torch.float32, device=Q.device)
+    scratch = _new(torch.empty, need.value, torch.uint8, Q.device, stream)
+    echo = _new(torch.empty, H, torch.float32, Q.device, stream)
+    induction = _new(torch.empty, H, torch.float32, Q.device, stream)
     _check(load().razor_head_scores(_ptr(Q), _ptr(K), H, N, D, RAZOR_BF16, period, sm_scale, _ptr(echo),
                                     _ptr(induction), _ptr(scratch), need.value, _stream(stream)), "razor_head_scores")
     return echo, induction
@@ -457,7 +467,7 @@ def razor_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], inv_freq: n
                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None):
     """q, k (either may be None): device [B, T, heads, D] fp32 or bf16, strided, innermost dimension contiguous; inv_freq host
     float64 [R / 2]; positions device int32 [B, T] (None: 0, 1, ..).  -> (q_out, k_out): the tensors given (the inputs
-    themselves turn in place), or new contiguous ones."""
+    themselves turn in place), or new contiguous ones, allocated on `stream`."""
     x = q if q is not None else k
     B, T, _, D = x.shape
     dev, dtype = x.device, x.dtype
@@ -468,9 +478,9 @@ def razor_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], inv_freq: n
         assert positions.shape == (B, T) and positions.dtype is torch.int32 and positions.is_contiguous()
         assert positions.device == dev
     if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=dtype, device=dev)
+        q_out = _new(torch.empty, q.shape, dtype, dev, stream)
     if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=dtype, device=dev)
+        k_out = _new(torch.empty, k.shape, dtype, dev, stream)
     rq, rk = _rope_rows(q, q_out), _rope_rows(k, k_out)
     with _on(dev):
         _check(load().razor_rope(rq, rk, _ptr(positions), B, T, D, 2 * inv_freq.size, _VERIFY_DTYPES[dtype],
@@ -492,7 +502,7 @@ def razor_window_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, n_
     """q bf16 [B, T, Hq, D] (strided over b and t), K, V bf16 [B, Hkv, N, D] (strided, the same strides); window int32
     [B, Hkv], q_len, ctx_len int32 [B] on the device or None.  -> out bf16 [B, T, Hq, D]; rows beyond a sequence's queries are
     left as they are (zeros when `out` is not given).  workspace: uint8, razor_window_attention_workspace_bytes long; one is
-    allocated when none is given (on the current stream: give one with a `stream` of your own)."""
+    allocated when none is given.  What is not given is allocated and filled on `stream`."""
     return _window_attention("razor_window_attention", (), q, K, V, n_sink, window, q_len, ctx_len, sm_scale, out, workspace, stream)
 
 
@@ -516,13 +526,13 @@ def _window_attention(name, more, q, K, V, n_sink, window, q_len, ctx_len, sm_sc
     for x, shape in ((window, (B, Hk)), (q_len, (B,)), (ctx_len, (B,))):
         assert x is None or (x.shape == shape and x.dtype is torch.int32 and x.is_contiguous() and x.device == dev)
     if out is None:
-        out = torch.zeros((B, T, Hq, D), dtype=torch.bfloat16, device=dev)
+        out = _new(torch.zeros, (B, T, Hq, D), torch.bfloat16, dev, stream)
     else:
         assert out.shape == q.shape and out.dtype is torch.bfloat16 and out.is_contiguous() and out.device == dev
     need = razor_window_attention_workspace_bytes(B, Hq, Hk, D, T)
     with _on(dev):
         if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+            workspace = _new(torch.empty, need, torch.uint8, dev, stream)
         assert workspace.device == dev and workspace.is_contiguous()
         _check(getattr(load(), name)(q.data_ptr(), q_b, q_t, K.data_ptr(), V.data_ptr(), *kv[:3], _ptr(window), _ptr(q_len),
                                      _ptr(ctx_len), B, T, N, Hq, Hk, D, RAZOR_BF16, n_sink, sm_scale, out.data_ptr(),
