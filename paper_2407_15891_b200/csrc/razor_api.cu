@@ -1089,7 +1089,8 @@ int razor_decode_step(razor_cache_t* c, int32_t layer, const void* k_new, const 
   if (!c || !k_new || !v_new || !q || !out) return RAZOR_E_NULL_PTR;
   int rc = layer_ready(c, layer);
   if (rc) return rc;
-  if (((uintptr_t)k_new | (uintptr_t)v_new) & 15) return RAZOR_E_MISALIGNED;
+  // (all of them here: a call that is refused must not have appended)
+  if (((uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)q | (uintptr_t)out) & 15) return RAZOR_E_MISALIGNED;
   LayerHost& L = c->layers[layer];
   if (L.appended_max() >= c->cfg.max_new_tokens) return RAZOR_E_CAPACITY;
   // A head with no recent window at all drops the new token at once (nothing is stored, only the sums change):
