@@ -15,7 +15,8 @@
 //     PV_0, QK_0, PV_1, QK_1, ..;
 //   * warps 10, 11: look over the V tiles that are partly masked.  A weight of zero times a NaN or an infinity is a NaN, so
 //     such values are zeroed in shared memory, and put back into the rows that do see them at the end (rows that a mask
-//     hides from a token are never touched by it, whatever it holds).
+//     hides from a token are never touched by it, whatever it holds).  Where no query of the unit sees one there is nothing to
+//     put back: one token over 4 x 8000, NaN behind them, 63 us for 58 (looked through all the same, 759).
 // Tensor memory: S_0, S_1 (P over their lower halves), O_0, O_1: 4 x 128 columns, all there is.
 // The reference maximum of a row may lag behind the true one by a factor of 2^8; only a row that outruns it has its
 // accumulator rescaled, by its own softmax thread: when S_i of a step is there, the product of the step before has run.
@@ -28,9 +29,9 @@
 // What bounds it.  Long contexts, D = 128: a step of both tiles is 2048 cycles of products (128 x 128 x 16 in 64 cycles) and
 // takes 3500: a tile's softmax (2000: 128 exponentials a thread, as many again for scale, maximum, sum and conversion) and its
 // way through the products (1450) follow each other, and two tiles fill no more than that.  32768 tokens, 32 query heads over
-// 8, all in sight: 7.3 ms in short runs (1208 TFLOP/s, 0.77 of the measured cuBLAS burst rate), 8.3 under continuous load,
-// where the power cap holds the clock (1060 TFLOP/s, 0.79 of cuBLAS's sustained rate); 8192 tokens 0.55 ms, a window of 1024 at
-// 32768 0.70 ms.  Short units pay their start (8500 cycles to the first scores of a launch, about half of it before the first
+// 8, all in sight: 7.25 ms in short runs (1213 TFLOP/s, 0.78 of the measured cuBLAS burst rate), 8.3 under continuous load,
+// where the power cap holds the clock (1060 TFLOP/s, 0.79 of cuBLAS's sustained rate); 8192 tokens 0.54 ms, a window of 1024 at
+// 32768 0.68 ms.  Short units pay their start (8500 cycles to the first scores of a launch, about half of it before the first
 // copy) and their results' way out (4400 cycles: a thread writes a row of its own).  One token over dense K and V is bound by the
 // same chain, a tile's step being short of rows but not of latency: 164 MB in 50 us.
 // Tried and dropped: an issuing thread for each tile (9.0 ms for 8.5 as it stood then: the tiles drift into step); sixteen
@@ -235,8 +236,16 @@ __device__ __forceinline__ WinUnit find_unit(const WinCall& c, int unit, int& b,
   return win_unit(pr * 2 * c.tpt, c.tpt, q_len, ctx, window, c.n_sink);
 }
 
+// Zeroes the bf16 values of `w` that are not finite.
+__device__ __forceinline__ uint32_t finite_or_zero2(uint32_t w) {
+  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
+  return w;
+}
+
 // Infinities and NaNs of V that were zeroed for the sake of rows that do not see them, added to a row that does: positions
-// of the masked tiles among the row's steps.  Rare, and slow.
+// of the masked tiles among the row's steps.  Slow (a thread looks through them by itself), and only where a query of the unit
+// sees such a value: what lies behind the end of a context or before the windows costs next to nothing.
 template <int D, typename Add>
 __device__ __forceinline__ void restore_non_finite(const WinCall& c, const WinItem& it, const WinTileSteps& t, int pos, Add add) {
   const __nv_bfloat16* v = c.v + it.b * c.v_stride_b + it.g * c.v_stride_h;
@@ -254,9 +263,14 @@ __device__ __forceinline__ void restore_non_finite(const WinCall& c, const WinIt
     for (int n = kt * kWinTile; n < kt * kWinTile + kWinTile && n <= pos; ++n) {
       if (!(it.window < 0 || n < c.n_sink || pos - n < it.window)) continue;
       const __nv_bfloat16* row = v + (int64_t)n * c.v_stride_n;
+#pragma unroll 4
+      for (int d = 0; d < D; d += 8) {
+        const uint4 u = __ldg((const uint4*)(row + d));
+        if (finite_or_zero2(u.x) == u.x && finite_or_zero2(u.y) == u.y && finite_or_zero2(u.z) == u.z && finite_or_zero2(u.w) == u.w) continue;
 #pragma unroll 1
-      for (int d = 0; d < D; ++d)
-        if (!finite_bf16(row[d])) add(d, __bfloat162float(row[d]));
+        for (int x = d; x < d + 8; ++x)
+          if (!finite_bf16(row[x])) add(x, __bfloat162float(row[x]));
+      }
     }
   }
 }
@@ -747,12 +761,24 @@ __global__ void __launch_bounds__(kWinThreads, 1)
             acc = __hfma2(*(const __nv_bfloat162*)&u.w, zero, acc);
           }
           if (!finite_bf16(acc.x) || !finite_bf16(acc.y)) {
-            __nv_bfloat16* e = (__nv_bfloat16*)p;
-            for (int k = me; k < TB / 16; k += 64)
-              for (int x = 0; x < 8; ++x)
-                if (!finite_bf16(e[k * 8 + x])) e[k * 8 + x] = __float2bfloat16_rn(0.f);
-            *(volatile int*)&it.poison = 1;
-            __threadfence_block();
+            // zeroed; whether a query of the unit sees one of them decides on the looking for them later
+            bool seen = false;
+            for (int k = me; k < TB / 16; k += 64) {
+              const uint4 u = p[k];
+              const uint4 f = make_uint4(finite_or_zero2(u.x), finite_or_zero2(u.y), finite_or_zero2(u.z), finite_or_zero2(u.w));
+              if (f.x == u.x && f.y == u.y && f.z == u.z && f.w == u.w) continue;
+              p[k] = f;
+              const int n = kt * kWinTile + k * 16 % kHalfBytes / 128;   // (the swizzle stays within a row)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const WinTileSteps& t = it.u.tile[i];
+                seen |= t.active(j) && win_seen(n, t.pos, t.pos + t.n_tok - 1, it.window, c.n_sink);
+              }
+            }
+            if (seen) {
+              *(volatile int*)&it.poison = 1;
+              __threadfence_block();
+            }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }

@@ -115,6 +115,11 @@ RAZOR_HD inline bool win_masked(int kt, int first, int last, int window, int n_s
   return !(b <= first && (window < 0 || b < n_sink || (long long)a > (long long)last - window));
 }
 
+// Is key n in sight of some query at the positions first .. last (some position, first <= last)?
+RAZOR_HD inline bool win_seen(long long n, int first, int last, int window, int n_sink) {
+  return n <= last && (n < n_sink || window < 0 || (first > n ? first : n) - n < window);
+}
+
 // Spans: the units' weights end to end, cut into n_spans pieces of equal length.
 RAZOR_HD inline int win_n_spans(long long total, int ctas) {
   const long long most = total / kWinMinSpan;
