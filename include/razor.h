@@ -404,7 +404,8 @@ RAZOR_API int razor_cache_set_head_windows(razor_cache_t* cache, int32_t layer, 
  *   head_dim   up to 256, a multiple of 16 bytes; dtype RAZOR_F32 or RAZOR_BF16
  *   rotated    R: the first R values of a row turn (even, 2 <= R <= head_dim), the others are carried over
  *   inv_freq   host double [R / 2]: angle per position of each pair, in radians (razor_rope_frequencies gives the usual
- *              ones); angles are right to 32 bits at any position an int32 can hold
+ *              ones); whole turns drop out exactly at any position an int32 can hold, and the sine takes what is left of
+ *              the angle (half a turn at most) rounded once to fp32
  *   gain       factor on the turned values
  *   interleaved  0: pair i is (x_i, x_(i + R/2)); 1: (x_2i, x_(2i+1))
  *   inverse    1: turns back (the transposed rotation, the gradient with respect to x); gain applies as it is

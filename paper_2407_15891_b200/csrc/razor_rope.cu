@@ -9,13 +9,14 @@
 // Far positions: p w_i in 32 bits would be off by p 2^-24 radians (0.06 at a million).  Only the fraction of a turn
 // matters, so a frequency is kept as a 64-bit fraction of a turn per position, F = w / 2 pi * 2^64, and p F in 64-bit integer
 // arithmetic, which drops whole turns by itself, is the phase: off by at most |p| 2^-65 turns (and by what w has lost in its
-// own 53 bits).
+// own 53 bits).  The sine takes it as half turns in fp32, rounded from all 64 bits: off by 2^-24 of itself, at most 2^-26 turns.
+// (Its upper half alone would be cut off at 2^-32 turns: an angle of 1e-6 would have lost a thousandth of itself.)
 //
 // Bound by memory: every value is read once and written once.  A thread owns a chunk of E pairs (two 16-byte pieces of a
 // row), works out its sines and cosines once per token and walks over the heads of queries and keys alike with them, four
 // heads' loads in flight; a token's heads are spread over as many threads as it takes to fill the GPU, so a decode step is
-// one short pass.  8192 tokens of 32 + 8 heads, bf16: 32.9 us, 5.1 TB/s (0.78 of the measured copy rate); 8004 tokens of 40 + 40
-// heads, fp32, half of each turned: 113 us, 5.8 TB/s (0.88).
+// one short pass.  8192 tokens of 32 + 8 heads, bf16: 33.2 us, 5.05 TB/s (0.77 of the measured copy rate); 8004 tokens of 40 + 40
+// heads, fp32, half of each turned: 114 us, 5.7 TB/s (0.88).
 // (A block that works out its tokens' sines once for all, with four heads to a thread, was tried: 105 us for the latter, but 41
 // for the former.)
 #include <cuda_bf16.h>
@@ -69,8 +70,8 @@ __device__ __forceinline__ void pack<__nv_bfloat16>(const float (&f)[8], uint4& 
 
 __device__ __forceinline__ void turn_of(const RopeCall& c, int pair, int32_t p, float& cs, float& sn) {
   const uint64_t phase = (uint64_t)(int64_t)p * c.turn[pair];
-  // the nearest whole turn dropped: half turns in [-1, 1)
-  sincospif((float)(int32_t)(phase >> 32) * 4.656612873077393e-10f, &sn, &cs);
+  // the nearest whole turn dropped: half turns in [-1, 1], rounded once (a small angle keeps its 24 bits)
+  sincospif((float)(int64_t)phase * 1.0842021724855044e-19f, &sn, &cs);
   cs *= c.gain;
   sn *= c.inverse ? -c.gain : c.gain;
 }
@@ -181,7 +182,9 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const __grid_constan
   }
 }
 
-// Any even `rotated` <= head_dim: a thread per pair of values.
+// Any even `rotated` <= head_dim: a thread per pair of values, so accesses of 2 or 4 bytes and one head in flight.  8192 tokens of
+// 32 + 8 heads, bf16, 102 of 128 values turned: 74.5 us (0.34 of the measured copy rate); 8004 tokens of 40 + 40 heads, fp32, 58 turned:
+// 149 us (0.67).
 template <typename T>
 __global__ void __launch_bounds__(kRopeThreads) rope_pairs_kernel(const __grid_constant__ RopeCall c) {
   const int cols = c.head_dim / 2;
