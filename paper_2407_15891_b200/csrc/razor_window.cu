@@ -945,7 +945,9 @@ int win_layout(int batch, int n_q_heads, int n_kv_heads, int head_dim, int n_tok
   l.group = n_q_heads / n_kv_heads;
   l.tpt = kWinTile / l.group;
   l.pairs = (n_tokens + 2 * l.tpt - 1) / (2 * l.tpt);
-  l.units = (long long)l.pairs * batch * n_kv_heads;
+  l.units = (long long)l.pairs * batch;
+  if (l.units > (1LL << 30)) return RAZOR_E_CAPACITY;   // (before the next factor: all three need not fit 64 bits)
+  l.units *= n_kv_heads;
   if (l.units > (1LL << 30)) return RAZOR_E_CAPACITY;
   l.rec_rows = 2 * std::min(l.tpt, n_tokens) * l.group;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
