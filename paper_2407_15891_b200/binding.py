@@ -499,10 +499,11 @@ def razor_window_attention(q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, n_
                            window: Optional[torch.Tensor] = None, q_len: Optional[torch.Tensor] = None,
                            ctx_len: Optional[torch.Tensor] = None, sm_scale: float = 0.0, out: Optional[torch.Tensor] = None,
                            workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """q bf16 [B, T, Hq, D] (strided over b and t), K, V bf16 [B, Hkv, N, D] (strided, the same strides); window int32
-    [B, Hkv], q_len, ctx_len int32 [B] on the device or None.  -> out bf16 [B, T, Hq, D]; rows beyond a sequence's queries are
-    left as they are (zeros when `out` is not given).  workspace: uint8, razor_window_attention_workspace_bytes long; one is
-    allocated when none is given.  What is not given is allocated and filled on `stream`."""
+    """q bf16 [B, T, Hq, D] (strided over b and t), K, V bf16 [B, Hkv, N, D] (strided, with the same strides in dimensions longer
+    than one); window int32 [B, Hkv], q_len, ctx_len int32 [B] on the device or None.  -> out bf16 [B, T, Hq, D]; rows beyond a
+    sequence's queries are left as they are (zeros when `out` is not given).  workspace: uint8,
+    razor_window_attention_workspace_bytes long; one is allocated when none is given.  What is not given is allocated and filled
+    on `stream`."""
     return _window_attention("razor_window_attention", (), q, K, V, n_sink, window, q_len, ctx_len, sm_scale, out, workspace, stream)
 
 
@@ -521,7 +522,9 @@ def _window_attention(name, more, q, K, V, n_sink, window, q_len, ctx_len, sm_sc
     q_b, q_t, q_h, q_d = q.stride()
     kv = K.stride()
     assert q.is_cuda and q.dtype is torch.bfloat16 and K.dtype is torch.bfloat16 and V.dtype is torch.bfloat16
-    assert K.shape == V.shape == (B, Hk, N, D) and kv == V.stride() and kv[3] == 1 and q_d == 1 and (Hq == 1 or q_h == D)
+    assert K.shape == V.shape == (B, Hk, N, D) and kv[3] == 1 and q_d == 1 and (Hq == 1 or q_h == D)
+    # (a stride that separates nothing may be anything)
+    assert all(a == b or n == 1 for a, b, n in zip(kv, V.stride(), K.shape))
     assert K.device == dev and V.device == dev
     for x, shape in ((window, (B, Hk)), (q_len, (B,)), (ctx_len, (B,))):
         assert x is None or (x.shape == shape and x.dtype is torch.int32 and x.is_contiguous() and x.device == dev)
