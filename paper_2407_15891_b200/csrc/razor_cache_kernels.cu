@@ -898,8 +898,15 @@ cudaError_t launch_append_tree(const DeviceView& dv, int dtype, int layer, const
 template <typename T, int D, bool Q8 = false>
 static cudaError_t export_t(const DeviceView& dv, int layer, int head, int32_t* kp, void* K, void* V, float* mk,
                             float* mv, float* sk, float* sv, cudaStream_t s) {
-  // (8-bit rows: a snapshot of a 128K head is bound by what it writes, so enough CTAs to fill the GPU)
-  export_kernel<T, D, Q8><<<Q8 ? 592 : 64, 256, 0, s>>>(dv, layer, head, kp, K, V, mk, mv, sk, sv);
+  int ctas = 64;
+  if (Q8) {   // a snapshot of a 128K head is bound by what it writes: four CTAs to an SM
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&ctas, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    ctas *= 4;
+  }
+  export_kernel<T, D, Q8><<<ctas, 256, 0, s>>>(dv, layer, head, kp, K, V, mk, mv, sk, sv);
   return cudaGetLastError();
 }
 
