@@ -28,12 +28,16 @@
  *     quantised as it is written - by razor_compress, razor_compress_seq, razor_append, razor_append_many or
  *     razor_decode_step - and held as D codes and one scale, K and V each their own: with top the row's largest magnitude,
  *       scale = top / 127,  code = round_half_even(x * (127 / top)),  value held = scale * code   (all in fp32, IEEE),
- *     off by at most top / 254.  A row with top < 2^-100 is held as zeros, one with a value that is not finite as NaN.
- *     A kept token takes 2 (D + 4) bytes a KV head.  Rows that a compression drops are summed (Eq. 4) as they came, and so
- *     are new tokens of a head without a window; a row that leaves the window counts as the values it was held with.  razor_decode_attention, _step and _multi attend to
- *     the values held, in fp32 accuracy (razor_decode_step takes two launches; a NaN in a cached K or V row, now the whole row, shows in the query rows that see it
- *     and in no other); a round of more than 8 query rows per KV head runs block by block, each block reading the cache once.
- *     razor_cache_export gives the values held (K and V in fp32).  The tree calls refuse such a cache (UNSUPPORTED_DIM).
+ *     off by at most top / 254 + 2^-22 top (half a step, and what the three quotients and products round).  A row with
+ *     top < 2^-100 is held as zeros, one with a value that is not finite as NaN.  A kept token takes 2 (D + 4) bytes a KV head.
+ *     Rows that a compression drops are summed (Eq. 4) as they came, and so are new tokens of a head without a window; a row
+ *     that leaves the window counts as the values it was held with.  razor_decode_attention, _step and _multi attend to the
+ *     values held, in fp32 accuracy but for tokens whose V is far smaller than another's that the call reads, hidden ones
+ *     included: a token's part of the result is off by 2^-22 of itself or 2^-38 of the largest |V| read times the row's largest
+ *     weight, whichever is more.  razor_decode_step takes two launches.  A NaN in a cached K or V row, now the whole row, shows in
+ *     the query rows that see it and in no other.  A round of more than 8 query rows per KV head runs block by block, each
+ *     block reading the cache once.  razor_cache_export gives the values held (K and V in fp32).  The tree calls refuse such a
+ *     cache (UNSUPPORTED_DIM).
  *   - The cache and attention calls never apply rotary embeddings: K and q arrive after the rotary transformation,
  *     as in the paper's cache (Section 3.2, text below Eq. 4).  razor_rope applies it.
  */

@@ -65,8 +65,9 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 }
 
 // ---- pages of 8-bit rows.  A row x is held as codes c = round(x * (127 / top)), top its largest magnitude, and one scale
-// top / 127 in fp32: the value held is scale * c (off by at most half a step, top / 254).  Quotients, product and rounding
-// are IEEE's, to nearest even, so that anybody can compute the same codes.  A page is [16 K rows of D bytes][16 V rows][16 K
+// top / 127 in fp32: the value held is scale * c, off by at most half a step, top / 254, and 2^-22 top (127 / top and its product
+// with x move a code by up to 127 2^-23, scale and value round once each).  Quotients, product and rounding are IEEE's, to
+// nearest even, so that anybody can compute the same codes.  A page is [16 K rows of D bytes][16 V rows][16 K
 // scales][16 V scales]; a code is stored as the byte c + 128.  Chunk placement, chosen for the fragment loads of the decode
 // kernel (eight lanes read 16 bytes each at a time): two K rows at four neighbouring chunks, or four V rows at two, meet
 // no bank twice (at D = 64 V's do, once: a row is half a line).
@@ -108,8 +109,8 @@ struct Q8Row {   // eight elements of a row per lane, D / 8 lanes to a row
     return top;
   }
   // Quantises the eight bf16 elements `raw` of a row whose largest magnitude is `top`.  w, s: codes and scale, held: the
-  // values they stand for.  A row whose largest magnitude is below 2^-100 is held as zeros (the quotient would leave the
-  // range of fp32), one with a value that is not finite as NaN.
+  // values they stand for.  A row whose largest magnitude is below 2^-100 is held as zeros (127 / top leaves the range of fp32
+  // below 2^-121: a bound chosen with room), one with a value that is not finite as NaN.
   static __device__ __forceinline__ void quantise(const uint4& raw, float top, uint32_t (&w)[2], float& s, float (&held)[8]) {
     float f[8];
     Elem<__nv_bfloat16>::unpack(raw, f);
