@@ -453,10 +453,12 @@ RAZOR_API int razor_rope(const razor_rope_rows_t* q, const razor_rope_rows_t* k,
  *   out        device bf16 [B, n_tokens, Hq, D] contiguous; rows at or beyond q_len[b] are left as they were
  * Query t of sequence b sits at position m = ctx_len[b] - q_len[b] + t (a prompt's later chunk attends to what came before it;
  * a single token is a decode step over a context that is not compressed) and sees key n when n <= m and (n < n_sink or
- * window < 0 or m - n < window).  out = softmax(sm_scale q.k) v over those, in fp32 with weights rounded to bf16 (an
- * average over the rounded weights: off by at most 2^-8 of sum p |v| beside the rounding of out); zeros when there are none.  sm_scale 0 means 1/sqrt(head_dim).
- * What is not finite shows in the rows that see it and in no other: a NaN or an infinity in q or in a K makes rows NaN, one in
- * a V appears in its dimension.  Rows of K and V that no query sees may hold anything.
+ * window < 0 or m - n < window).  out = softmax(sm_scale q.k) v over those, in fp32 with weights rounded to bf16 (an average
+ * over the rounded weights: off by at most 2^-8 of sum p |v - out| before out is rounded); zeros when there are none.  sm_scale
+ * 0 means 1/sqrt(head_dim).
+ * What is not finite shows in the rows that see it and in no other: a score that is NaN or +infinity makes a row NaN, one of
+ * -infinity hides its key (a row with no other key in sight is zeros); a NaN or an infinity in a V appears in its dimension.
+ * Rows of K and V that no query sees may hold anything.
  * head_dim 64 or 128; Hq / Hkv up to 128.  Bases 16-byte aligned, strides multiples of 16 bytes and at least head_dim (of a
  * dimension of size one they are not looked at); workspace 256-byte aligned, its content on entry does not matter, calls that
  * may run at the same time need their own (captured graphs that are replayed side by side too).

@@ -1,6 +1,5 @@
 """Calls of the prompt attention that its documentation allows: strides of dimensions of one, a buffer for every call, scores of
 -infinity."""
-import numpy as np
 import pytest
 import torch
 
@@ -19,3 +18,24 @@ def test_strides_of_dimensions_of_one_do_not_matter(B, Hk, N):
     K2, V2 = (x.as_strided(x.shape, [odd if n == 1 else s for n, s in zip(x.shape, x.stride())]) for x, odd in ((K, 24), (V, 7)))
     assert K2.stride() != V2.stride()
     assert torch.equal(rz.razor_window_attention(q, K2, V2, 4), want)
+
+
+@pytest.mark.parametrize("T,N", [(300, 300), (1, 9000), (64, 5000)])
+def test_a_score_of_minus_infinity_hides_its_key(T, N):
+    """Keys with an infinity against queries that are negative there: the oracle's weights of such keys are zero as well."""
+    q, K, V = _inputs(1, T, N, 4, 2, 128, seed=8)
+    q[..., 17] = -q[..., 17].abs() - 0.25
+    for n in sorted({0, 3, 40, N // 2, N - 60, N - 1}):
+        K[:, :, n, 17] = float("inf")
+    window = [[90, -1]]
+    out = rz.razor_window_attention(q, K, V, 3, _dev(window))
+    assert torch.isfinite(out).all()
+    _check(q, K, V, out, 3, window)
+
+
+def test_a_row_whose_keys_are_all_hidden_is_zeros():
+    q, K, V = _inputs(2, 4, 4, 2, 1, 64, seed=2)
+    q[..., 5], K[..., 5] = -1, float("inf")
+    assert not rz.razor_window_attention(q, K, V, 4).any()
+    q[..., 5] = 1
+    assert rz.razor_window_attention(q, K, V, 4).isnan().all()
