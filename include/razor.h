@@ -461,7 +461,9 @@ RAZOR_API int razor_rope(const razor_rope_rows_t* q, const razor_rope_rows_t* k,
  * Rows of K and V that no query sees may hold anything.
  * head_dim 64 or 128; Hq / Hkv up to 128.  Bases 16-byte aligned, strides multiples of 16 bytes and at least head_dim (of a
  * dimension of size one they are not looked at); workspace 256-byte aligned, its content on entry does not matter, calls that
- * may run at the same time need their own (captured graphs that are replayed side by side too).
+ * may run at the same time need their own (captured graphs that are replayed side by side too).  What a call needs does not
+ * grow with its sizes (few units of work are cut up and leave records, many are not): a buffer for several calls is as large
+ * as the largest of their needs, or 42607872 bytes (head_dim 64: 21635328), which serve any.
  * The lengths and windows are read on the device: a replay of a captured call uses what they hold then.
  * Every wait in the kernel is bounded in time; should one ever run out, rows of the call are left NaN or as they were.
  * razor_window_attention_wait_selftest is the same call in which thread block `cta` (>= 0; one that the launch does not have

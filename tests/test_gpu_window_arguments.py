@@ -39,3 +39,15 @@ def test_a_row_whose_keys_are_all_hidden_is_zeros():
     assert not rz.razor_window_attention(q, K, V, 4).any()
     q[..., 5] = 1
     assert rz.razor_window_attention(q, K, V, 4).isnan().all()
+
+
+@pytest.mark.parametrize("D,size", [(64, 21635328), (128, 42607872)])
+def test_one_buffer_serves_calls_of_all_sizes(D, size):
+    ws = torch.full((size,), 0x7f, dtype=torch.uint8, device=DEV)
+    calls = []
+    for B, T, N, Hq, Hk in ((1, 600, 600, 32, 8), (1, 1, 5000, 8, 2), (70, 1, 100, 16, 16), (4, 1, 3000, 32, 8), (1, 257, 900, 2, 1)):
+        q, K, V = _inputs(B, T, N, Hq, Hk, D, seed=T)
+        calls.append((q, K, V, rz.razor_window_attention(q, K, V, 4)))
+    for _ in range(2):
+        for q, K, V, want in calls:
+            assert torch.equal(rz.razor_window_attention(q, K, V, 4, workspace=ws), want)
