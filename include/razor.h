@@ -441,9 +441,10 @@ RAZOR_API int razor_rope(const razor_rope_rows_t* q, const razor_rope_rows_t* k,
                          int32_t interleaved, int32_t inverse, void* stream);
 
 /*
- * Attention of prompt tokens over dense K and V: what a prefill computes from the rows that razor_compress packs
- * afterwards.  Causal, with a sliding window and the first n_sink tokens for each KV head - the sets Algorithm 1 keeps -, or
- * everything (a retrieval head).  No cache is needed.
+ * Attention of prompt tokens over dense K and V, the rows that razor_compress packs afterwards.  Causal, with a sliding
+ * window and the first n_sink tokens for each KV head, or everything.  The method's own prefill sees everything (window NULL):
+ * only its decode steps see the compressed sets.  Windows here are a model's own, or Algorithm 1's sets taken over into the
+ * prefill, which is another model's result (and has no compensation token).  No cache is needed.
  *   q          device bf16 [B, n_tokens, Hq, D], element strides q_stride_b / q_stride_t, the heads of a token contiguous
  *   K, V       device bf16 [B, Hkv, n_ctx, D], element strides kv_stride_b / _h / _n (razor_compress's buffers)
  *   window     device int32 [B, Hkv]: recent tokens a head's queries see, their own included; < 0: everything (the queries

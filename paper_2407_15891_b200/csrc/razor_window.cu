@@ -24,7 +24,9 @@
 // Work: up to 1024 units are laid end to end, step by step, and cut into one span per CTA, on the device (lengths and windows
 // live there): a long context with few queries is spread over all SMs, and equal units fill the last wave.  Units that were
 // cut leave partial records (m, l, o) per row, which window_combine_kernel folds in order.  More units than that are handed
-// out whole from a queue, longest first.
+// out whole from a queue, the last queries first: the longest first among equal sequences and heads, but a unit of a head that
+// sees everything is not put before one of a short window.  (1024: units then come to seven waves and their ends even out.  What
+// is lost at the border, and with ragged lengths behind it, has not been measured.)
 //
 // What bounds it.  Long contexts, D = 128: a step of both tiles is 2048 cycles of products (128 x 128 x 16 in 64 cycles) and
 // takes 3500: a tile's softmax (2000: 128 exponentials a thread, as many again for scale, maximum, sum and conversion) and its
@@ -222,8 +224,7 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
 }
 __device__ __forceinline__ bool finite_bf16(__nv_bfloat16 x) { return (__bfloat16_as_ushort(x) & 0x7f80) != 0x7f80; }
 
-// Unit number -> its place and steps.  Units run over (sequence, KV head) fastest; `order` 1: the last queries (the
-// longest rows) first.
+// Unit number -> its place and steps.  Units run over (sequence, KV head) fastest; out of the queue the last queries come first.
 __device__ __forceinline__ WinUnit find_unit(const WinCall& c, int unit, int& b, int& g, int& window, int& ctx) {
   const int bh = unit % (c.batch * c.n_kv_heads);
   int pr = unit / (c.batch * c.n_kv_heads);
