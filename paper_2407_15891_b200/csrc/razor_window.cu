@@ -29,7 +29,7 @@
 // is lost at the border, and with ragged lengths behind it, has not been measured.)
 //
 // What bounds it.  Long contexts, D = 128: a step of both tiles is 2048 cycles of products (128 x 128 x 16 in 64 cycles) and
-// takes 3500: a tile's softmax (2000: 128 exponentials a thread, as many again for scale, maximum, sum and conversion) and its
+// takes 3550: a tile's softmax (2000: 128 exponentials a thread, as many again for scale, maximum, sum and conversion) and its
 // way through the products (1450) follow each other, and two tiles fill no more than that.  32768 tokens, 32 query heads over
 // 8, all in sight: 7.25 ms in short runs (1213 TFLOP/s, 0.78 of the measured cuBLAS burst rate), 8.3 under continuous load,
 // where the power cap holds the clock (1060 TFLOP/s, 0.79 of cuBLAS's sustained rate); 8192 tokens 0.54 ms, a window of 1024 at
@@ -61,7 +61,7 @@ constexpr int kWinThreads = 384;
 // Registers: 168 a thread at launch; the softmax threads, which hold a row of 128 scores, take over what the others give up.
 constexpr int kWinLaunchRegs = 168, kWinSoftmaxRegs = 216, kWinOtherRegs = 72;
 static_assert(256 * kWinSoftmaxRegs + 128 * kWinOtherRegs <= kWinThreads * kWinLaunchRegs, "no more than the block was launched with");
-constexpr int kParts = 2;                    // P is handed over in so many parts (32K tokens: 7.1 ms; in four parts 7.3)
+constexpr int kParts = 2;                    // P is handed over in so many parts (32K tokens, before the sums of rounded weights: 7.1 ms; in four parts 7.3)
 constexpr int kHalfBytes = kWinTile * 128;   // 128 rows of 64 elements
 
 template <int D>
